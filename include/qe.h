@@ -17,7 +17,7 @@
  *  - Calls are stream-ordered and asynchronous on `stream` (a cudaStream_t;
  *    NULL = legacy default stream).  Argument errors are returned
  *    synchronously before anything is enqueued.  Errors found on the device
- *    (non-finite input, a device-side wait that gave up) are latched in a
+ *    (non-finite input, an index out of range, a device-side wait that gave up) are latched in a
  *    per-device error word and reported by qe_sync_status().
  *  - Scratch memory: taken from opts->workspace when given (at least
  *    qe_workspace_size() bytes, 256-byte aligned), otherwise allocated with
@@ -39,15 +39,15 @@ typedef struct CUstream_st *qe_stream_t;
 
 typedef enum {
     QE_OK = 0,
-    QE_ERR_INVALID_ARG = 1,   /* bad size, pointer, alignment or option */
+    QE_ERR_INVALID_ARG = 1,   /* bad size, pointer, alignment or option; an index found out of range on the device */
     QE_ERR_CUDA = 2,          /* a CUDA runtime/driver call failed */
     QE_ERR_OOM = 3,           /* workspace allocation failed or too small */
-    QE_ERR_NUMERIC = 4,       /* non-finite value in W or Sigma (device-detected) */
+    QE_ERR_NUMERIC = 4,       /* non-finite value in W, Sigma, K or V (device-detected) */
     QE_ERR_TIMEOUT = 5,       /* a bounded device-side wait gave up (device-detected) */
     QE_ERR_UNSUPPORTED = 6    /* option or layout not implemented */
 } qe_status;
 
-typedef enum { QE_F32 = 0, QE_BF16 = 1 } qe_dtype;
+typedef enum { QE_F32 = 0, QE_BF16 = 1, QE_F16 = 2 /* the key/value cache only */ } qe_dtype;
 
 typedef enum {
     QE_FEATURE_MAJOR = 0,     /* X is p x n row-major: the paper's X (Sec. 2.1) */
@@ -352,8 +352,108 @@ qe_status qe_hard_threshold_workspace(int64_t N, size_t *bytes);
 qe_status qe_hard_threshold(const float *T, int64_t N, int64_t s, int64_t *idx, float *val, int64_t *nnz,
                             void *workspace, size_t workspace_bytes, qe_stream_t stream);
 
+/*
+ * The key/value cache in 4 bits (the paper quantizes the weights of a model's
+ * linear layers; this is the same kind of grid for the other large array of a
+ * model that answers: the keys and values of the tokens seen so far).
+ *
+ * x^ = s (c - z) with one grid (s, z) for each token, kv head and group of
+ * group_size channels, c in 0 .. 15.  For a group with values x, in binary32:
+ *     lo = min(x, 0), hi = max(x, 0), s = bf16((hi - lo) / 15) but at least 2^-126,
+ *     z = round(-lo / s), c = clamp(round(x / s) + z, 0, 15)   (ties to even)
+ * A cached channel takes 4 + 32 / group_size bits.
+ *
+ * Pages: the cache holds `pages` pages of page_size tokens; slot = page *
+ * page_size + position inside the page.  Which pages belong to a sequence, in
+ * which order, is the caller's page table; a cache without paging is one page
+ * per sequence.
+ *   data        device, 256-byte aligned, qe_cache_size() bytes, owned by the
+ *               caller; need not be initialised.  Its layout is the library's.
+ *   page_size   a power of two, 16 .. 65536.
+ *   head_dim    a multiple of 8 up to 128 (held as 64, 96 or 128 channels).
+ *   group_size  32, 64 or 128, a divisor of the channels held.
+ * Other values of these three are QE_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    void *data;
+    size_t bytes;
+    int64_t pages;
+    int page_size, kv_heads, head_dim, group_size;
+} qe_cache;
+
+/* Bytes of a cache's data. */
+qe_status qe_cache_size(int64_t pages, int page_size, int kv_heads, int head_dim, int group_size, size_t *bytes);
+
+/*
+ * Quantizes the keys and values of `tokens` tokens into the cache.
+ *   K, V     device, token i's head h at K + i * k_token + h * k_head (elements;
+ *            channels are contiguous), fp32, bf16 or fp16.  Any strides; where
+ *            pointer and strides are multiples of 4 channels the loads are wide.
+ *   slots    device, int64 per token: where it goes.  A negative slot is skipped
+ *            (padding); one past the cache is skipped and latches
+ *            QE_ERR_INVALID_ARG.  No two tokens of a call share a slot.
+ * A token's head with a NaN, an infinity or a magnitude above 2^126 in its keys
+ * or values is marked bad and latches QE_ERR_NUMERIC: it reads back as NaN, and
+ * every row of attention that sees the token becomes NaN (no other does).
+ * Asynchronous on `stream`; allocates nothing.
+ */
+qe_status qe_cache_append(const qe_cache *cache, const void *K, int64_t k_token, int64_t k_head, const void *V,
+                          int64_t v_token, int64_t v_head, qe_dtype dtype, const int64_t *slots, int64_t tokens,
+                          qe_stream_t stream);
+
+/*
+ * The values that the cache holds at `slots`, s (c - z) rounded once to dtype.
+ * K or V may be NULL (not wanted).  A negative slot gives zeros; one past the
+ * cache gives zeros and latches QE_ERR_INVALID_ARG.
+ */
+qe_status qe_cache_read(const qe_cache *cache, const int64_t *slots, int64_t tokens, void *K, int64_t k_token,
+                        int64_t k_head, void *V, int64_t v_token, int64_t v_head, qe_dtype dtype, qe_stream_t stream);
+
+/*
+ * Attention over the cache for a ragged batch of sequences:
+ *     out_i = sum_j softmax_j(scale q_i . k^_j) v^_j
+ * Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1 and kv_len[b]
+ * cached tokens, its own rows' among them (append first, then attend).  With n
+ * rows and L tokens, row i sits at position L - n + i.  It sees all L tokens
+ * (causal = 0), or those up to its position (causal = 1), of which with
+ * window = W > 0 the last W.  Query head h reads kv head h / (q_heads / kv_heads).
+ * A row that sees no token is zero, with lse -inf.
+ */
+typedef struct {
+    int64_t seqs;                /* 1 .. 65535 */
+    int64_t rows;                /* query rows in all: Q and out have this many */
+    int q_heads;                 /* a multiple of the cache's kv_heads */
+    int causal;
+    int64_t window;              /* 0 = none; needs causal */
+    float scale;                 /* 0 = 1 / sqrt(head_dim) */
+    int64_t max_q;               /* no sequence has more query rows (more latch QE_ERR_INVALID_ARG and are left out) */
+    int64_t max_kv;              /* about the longest kv_len: plans the work, right or not */
+    const int32_t *q_start;      /* device, seqs + 1 values, ascending */
+    const int32_t *kv_len;       /* device, seqs values */
+    const int32_t *page_table;   /* device, seqs x table_ld: token j of sequence b is in page [b][j / page_size] */
+    int64_t table_ld;            /* kv_len above table_ld * page_size latches QE_ERR_INVALID_ARG and is cut */
+} qe_attention;
+
+/* Bytes of workspace qe_cache_attention needs (0 where it needs none). */
+qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention *at, size_t *bytes);
+
+/*
+ *   Q, out    device, bf16 or fp16 (fp32 is QE_ERR_UNSUPPORTED): row i's head h
+ *             at Q + i * q_row + h * q_head (elements; channels contiguous).
+ *   lse       device, rows x q_heads fp32, or NULL: log sum_j exp(scale q_i . k^_j).
+ *   workspace device, 256-byte aligned, workspace_bytes; NULL: allocated and
+ *             freed on `stream` inside the call.  Not used across calls, need
+ *             not be initialised.
+ * Page ids out of range latch QE_ERR_INVALID_ARG and their tokens count as not
+ * there.  Only pages that hold a token some row sees are looked up.
+ * Asynchronous on `stream`.
+ */
+qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, const void *Q, int64_t q_row, int64_t q_head,
+                             void *out, int64_t o_row, int64_t o_head, qe_dtype dtype, float *lse, void *workspace,
+                             size_t workspace_bytes, qe_stream_t stream);
+
 /* Waits for `stream`, then returns and clears the error latched on the current
- * device (QE_ERR_NUMERIC / QE_ERR_TIMEOUT), or QE_ERR_CUDA if the stream failed.
+ * device (QE_ERR_NUMERIC / QE_ERR_TIMEOUT / QE_ERR_INVALID_ARG for an index out of range), or QE_ERR_CUDA if the stream failed.
  * The error word is a file-scope device variable whose address the library looks
  * up once per device and caches; calling the library on a device after a
  * cudaDeviceReset of that device is not supported. */

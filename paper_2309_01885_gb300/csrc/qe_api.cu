@@ -857,6 +857,7 @@ qe_status qe_sync_status(qe_stream_t stream) {
         return QE_ERR_CUDA;
     }
     if (v & ERR_TIMEOUT) return QE_ERR_TIMEOUT;
+    if (v & ERR_RANGE) return QE_ERR_INVALID_ARG;
     if (v & ERR_NUMERIC) return QE_ERR_NUMERIC;
     return QE_OK;
 }

@@ -11,7 +11,7 @@
 namespace qe {
 
 // ---- device error word ------------------------------------------------------
-enum : unsigned { ERR_NUMERIC = 1u, ERR_TIMEOUT = 2u };
+enum : unsigned { ERR_NUMERIC = 1u, ERR_TIMEOUT = 2u, ERR_RANGE = 4u };
 
 // Every device-side wait gives up after this many nanoseconds of %globaltimer.
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;

@@ -17,14 +17,15 @@ LIB_PATH = os.path.join(_HERE, "_build", "libqe.so")
 
 QE_OK, QE_ERR_INVALID_ARG, QE_ERR_CUDA, QE_ERR_OOM, QE_ERR_NUMERIC, QE_ERR_TIMEOUT, \
     QE_ERR_UNSUPPORTED = range(7)
-QE_F32, QE_BF16 = 0, 1
+QE_F32, QE_BF16, QE_F16 = 0, 1, 2
 QE_FEATURE_MAJOR, QE_TOKEN_MAJOR = 0, 1
 
 EXPORTED = ("qe_build_sigma", "qe_quantize_layer", "qe_quantize_layer_outlier",
             "qe_workspace_size", "qe_sync_status", "qe_status_string", "qe_version",
             "qe_build_sigma_static", "qe_timer_create", "qe_timer_read", "qe_timer_reset",
             "qe_timer_destroy", "qe_build_sigma_host", "qe_pack_codes", "qe_unpack_codes",
-            "qe_hard_threshold", "qe_hard_threshold_workspace")
+            "qe_hard_threshold", "qe_hard_threshold_workspace", "qe_cache_size", "qe_cache_append",
+            "qe_cache_read", "qe_cache_attention", "qe_cache_attention_workspace")
 QE_KERNEL_PINIT_GEMM, QE_KERNEL_RESIDUAL_GEMM, QE_KERNEL_TRAIL_GEMM, QE_KERNEL_CD_BLOCK, \
     QE_KERNEL_CD_LISTS, QE_KERNEL_COUNT = range(6)
 
@@ -45,6 +46,21 @@ class QEOpts(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("timer", ctypes.c_void_p),
                 ("switch_below", ctypes.c_int64), ("sweep_forms", ctypes.c_void_p),
                 ("wait_test", ctypes.c_int), ("tie_eps", ctypes.c_float)]
+
+
+class QECache(ctypes.Structure):
+    """Mirror of ``qe_cache``."""
+    _fields_ = [("data", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("group_size", ctypes.c_int)]
+
+
+class QEAttention(ctypes.Structure):
+    """Mirror of ``qe_attention``."""
+    _fields_ = [("seqs", ctypes.c_int64), ("rows", ctypes.c_int64), ("q_heads", ctypes.c_int),
+                ("causal", ctypes.c_int), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64), ("q_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("table_ld", ctypes.c_int64)]
 
 
 _lib = None
@@ -98,6 +114,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.qe_timer_reset.restype = st
     L.qe_timer_destroy.argtypes = [vp]
     L.qe_timer_destroy.restype = st
+    L.qe_cache_size.argtypes = [i64, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_cache_size.restype = st
+    L.qe_cache_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, i32, vp, i64, vp]
+    L.qe_cache_append.restype = st
+    L.qe_cache_read.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, i64, i32, vp]
+    L.qe_cache_read.restype = st
+    L.qe_cache_attention_workspace.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_cache_attention_workspace.restype = st
+    L.qe_cache_attention.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp, vp, ctypes.c_size_t, vp]
+    L.qe_cache_attention.restype = st
     _lib = L
     return L
 
@@ -370,4 +396,136 @@ def qe_quantize_layer_outlier(W: torch.Tensor, Sigma: torch.Tensor, bits: int, i
         out["sweep_codes"] = sweep
     if want_norm:
         out["wx_norm2"] = norm
+    return out
+
+
+# ---- the key/value cache in 4 bits ------------------------------------------------------------
+
+_CACHE_DTYPES = {torch.float32: QE_F32, torch.bfloat16: QE_BF16, torch.float16: QE_F16}
+
+
+def qe_cache_size(pages: int, page_size: int, kv_heads: int, head_dim: int, group_size: int = 32) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().qe_cache_size(pages, page_size, kv_heads, head_dim, group_size, ctypes.byref(n)), "qe_cache_size")
+    return n.value
+
+
+class KVCache:
+    """Keys and values of `pages` pages of `page_size` tokens, 4 bits a channel: one grid (scale, zero)
+    for each token, kv head and group of `group_size` channels.  `data` is the caller's uint8 device
+    tensor of qe_cache_size() bytes (allocated here when not given)."""
+
+    def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, group_size: int = 32,
+                 data: torch.Tensor | None = None, device="cuda"):
+        need = qe_cache_size(pages, page_size, kv_heads, head_dim, group_size)
+        if data is None:
+            data = torch.empty(need, dtype=torch.uint8, device=device)
+        if not data.is_cuda or data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() < need:
+            raise ValueError(f"expected a contiguous uint8 device tensor of at least {need} bytes")
+        self.pages, self.page_size, self.kv_heads = pages, page_size, kv_heads
+        self.head_dim, self.group_size, self.data, self.device = head_dim, group_size, data, data.device
+        self._c = QECache(data.data_ptr(), data.numel(), pages, page_size, kv_heads, head_dim, group_size)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _cache_heads(cache: KVCache, t: torch.Tensor, heads: int, what: str):
+    """Strides (row, head) of a rows x heads x head_dim tensor on the cache's device."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim or (stride[2] != 1 and shape[2] != 1):
+        raise ValueError(f"{what}: expected rows x {heads} x {cache.head_dim} with contiguous channels")
+    if t.device != cache.device:
+        raise ValueError(f"{what}: not on the cache's device")
+    return stride[0], stride[1]
+
+
+def _cache_index(cache: KVCache, t: torch.Tensor, dtype: torch.dtype, dims: int, what: str):
+    if t.dtype != dtype or t.dim() != dims or t.device != cache.device or t.stride(-1) != 1:
+        raise ValueError(f"{what}: expected a {dims}-dimensional {dtype} tensor on the cache's device, contiguous along its last axis")
+    return t.data_ptr()
+
+
+def _cache_dtype(t) -> int:
+    d = _CACHE_DTYPES.get(t)
+    if d is None:
+        raise TypeError(f"unsupported dtype {t}: fp32, bf16 or fp16")
+    return d
+
+
+def _raw_stream(device, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def qe_cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """Quantize keys and values (tokens x kv_heads x head_dim, any row and head strides) into the
+    cache's `slots` (int64 per token: page * page_size + position in the page; negative = skip)."""
+    ks, vs = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
+    n = slots.shape[0]
+    if k.shape[0] != n or v.shape[0] != n or k.dtype != v.dtype:
+        raise ValueError("k, v and slots hold the same tokens, k and v the same dtype")
+    st = load().qe_cache_append(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _cache_dtype(k.dtype),
+                                _cache_index(cache, slots, torch.int64, 1, "slots"), n, _raw_stream(cache.device, stream))
+    if st != QE_OK:
+        raise QEError(st, "qe_cache_append")
+
+
+def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, k: torch.Tensor | None = None,
+                  v: torch.Tensor | None = None, stream=None) -> tuple:
+    """(keys, values) of the cache's `slots`, tokens x kv_heads x head_dim, rounded once to `dtype`;
+    written into `k` and `v` where given (any row and head strides)."""
+    n = slots.shape[0]
+    if k is None:
+        k = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device)
+    if v is None:
+        v = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device)
+    ks, vs = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
+    if k.shape[0] != n or v.shape[0] != n or k.dtype != dtype or v.dtype != dtype:
+        raise ValueError("k and v hold the tokens of slots, in dtype")
+    st = load().qe_cache_read(cache._ref, _cache_index(cache, slots, torch.int64, 1, "slots"), n, k.data_ptr(), ks[0],
+                              ks[1], v.data_ptr(), vs[0], vs[1], _cache_dtype(dtype), _raw_stream(cache.device, stream))
+    if st != QE_OK:
+        raise QEError(st, "qe_cache_read")
+    return k, v
+
+
+def qe_cache_attention_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int) -> int:
+    """Bytes of workspace qe_cache_attention takes for such a batch."""
+    at = QEAttention(seqs=seqs, rows=rows, q_heads=q_heads, causal=1, max_q=max_q, max_kv=max_kv)
+    n = ctypes.c_size_t(0)
+    _check(load().qe_cache_attention_workspace(cache._ref, ctypes.addressof(at), ctypes.byref(n)),
+           "qe_cache_attention_workspace")
+    return n.value
+
+
+def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                       page_table: torch.Tensor, max_q: int, max_kv: int, *, causal: bool = True, window: int = 0,
+                       scale: float = 0.0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of q (rows x q_heads x head_dim, bf16 or fp16) over the cache.  Sequence b has the rows
+    q_start[b] .. q_start[b + 1] - 1 (int32, seqs + 1) and kv_len[b] (int32) cached tokens, the rows' own
+    among them; its token j is in page page_table[b, j // page_size] (int32).  No sequence has more than
+    max_q rows; max_kv is about the longest kv_len.  causal / window (0 = none) / scale (0 = 1 /
+    sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x q_heads, written.  workspace: optional
+    uint8 tensor of qe_cache_attention_workspace() bytes."""
+    rows, heads = q.shape[0], q.shape[1]
+    qs = _cache_heads(cache, q, heads, "q")
+    if out is None:
+        out = torch.empty(rows, heads, cache.head_dim, dtype=q.dtype, device=cache.device)
+    os_ = _cache_heads(cache, out, heads, "out")
+    if out.dtype != q.dtype or out.shape[0] != rows:
+        raise ValueError("out has q's shape and dtype")
+    seqs = kv_len.shape[0]
+    if q_start.shape[0] != seqs + 1 or page_table.shape[0] != seqs:
+        raise ValueError("q_start holds seqs + 1 values, page_table seqs rows")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()):
+        raise ValueError("lse: expected a contiguous fp32 tensor, rows x q_heads")
+    at = QEAttention(seqs, rows, heads, causal, window, scale, max_q, max_kv,
+                     _cache_index(cache, q_start, torch.int32, 1, "q_start"),
+                     _cache_index(cache, kv_len, torch.int32, 1, "kv_len"),
+                     _cache_index(cache, page_table, torch.int32, 2, "page_table"), page_table.stride(0))
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    st = load().qe_cache_attention(cache._ref, ctypes.addressof(at), q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0],
+                                   os_[1], _cache_dtype(q.dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
+                                   _raw_stream(cache.device, stream))
+    if st != QE_OK:
+        raise QEError(st, "qe_cache_attention")
     return out
