@@ -28,10 +28,8 @@
 // memory at the end.  The steps of the whole batch are dealt out evenly over one
 // wave of CTAs (ragged lengths, few or many sequences alike), and items that
 // fall to several CTAs are joined by a second kernel.
-#include <cuda_fp16.h>
-#include <math_constants.h>
-
 #include "qe_attend.h"
+#include "qe_attend_out.cuh"
 #include "qe_internal.h"
 
 namespace qe {
@@ -40,15 +38,7 @@ namespace {
 // Two warps a CTA, so that while the warps of one meet and turn to their next item the
 // other CTAs of the SM compute (four: 64 single tokens over 1K .. 8K 100 us, two: 92).
 constexpr int kWarps = 2;
-constexpr float kRaise = 8.0f;            // log2 of how far a score may exceed the running maximum
-constexpr float kFloor = -1.0e30f;        // the running maximum before the first visible score
 constexpr int kScaleRoom = 7;             // log2 of how far a value scale may exceed the power of two it is taken relative to
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     uint32_t y;
@@ -61,16 +51,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
 }
 
 __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
@@ -106,62 +86,6 @@ __device__ __forceinline__ void lds_words(const uint8_t *p, uint32_t (&w)[N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
     }
-}
-
-// One query row's eight channels from `at`, as floats; channels past `dim` are zero.
-__device__ __forceinline__ void load_q8(const AttendArgs &a, int64_t row, int head, int at, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    if (at >= a.g.dim) return;            // dim is a multiple of 8
-    const int64_t off = row * a.q_row + head * a.q_head + at;
-    if (a.half) {
-        const __half *p = reinterpret_cast<const __half *>(a.Q) + off;
-        if (a.q_vec) {
-            union { uint4 u; __half e[8]; } t;
-            t.u = *reinterpret_cast<const uint4 *>(p);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __half2float(t.e[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __half2float(p[i]);
-        }
-    } else {
-        const __nv_bfloat16 *p = reinterpret_cast<const __nv_bfloat16 *>(a.Q) + off;
-        if (a.q_vec) {
-            union { uint4 u; __nv_bfloat16 e[8]; } t;
-            t.u = *reinterpret_cast<const uint4 *>(p);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __bfloat162float(t.e[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __bfloat162float(p[i]);
-        }
-    }
-}
-
-
-// Four channels of a finished row, from the unnormalised sums relative to the maximum `m` (log2 units).
-__device__ __forceinline__ void finish(const AttendArgs &a, int64_t row, int head, int d, const float4 &v, float m, float l) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;       // a row that sees nothing is zero; NaN stays
-    uint16_t *to = reinterpret_cast<uint16_t *>(a.out) + row * a.o_row + head * a.o_head + d;
-    uint2 w;
-    if (a.half) {
-        w.x = pack_f16(v.x * inv, v.y * inv);
-        w.y = pack_f16(v.z * inv, v.w * inv);
-    } else {
-        w.x = pack_bf16(v.x * inv, v.y * inv);
-        w.y = pack_bf16(v.z * inv, v.w * inv);
-    }
-    if (a.o_vec) {
-        *reinterpret_cast<uint2 *>(to) = w;
-    } else {
-        to[0] = static_cast<uint16_t>(w.x);
-        to[1] = static_cast<uint16_t>(w.x >> 16);
-        to[2] = static_cast<uint16_t>(w.y);
-        to[3] = static_cast<uint16_t>(w.y >> 16);
-    }
-    if (d == 0 && a.lse)
-        a.lse[row * a.q_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945309f;
 }
 
 // CTAs of an SM, by registers: 128, 168 and 255 a thread.
@@ -239,9 +163,9 @@ __global__ void __launch_bounds__(kWarps * 32, rows_blocks(C, NT)) k_attend_rows
         const int64_t page_bytes = a.g.kv_heads * a.g.block_bytes;
 
         unsigned gone = 0u;                               // 2 bits a stage: halves whose page id is out of range
-        auto page_of = [&](int k) {                       // (halves past the last visible token repeat its page)
+        auto page_of = [&](int k) {                       // (halves without a visible token take the nearest one's page)
             int j = j_begin + kRowsUnit * (warp + kWarps * k) + 16 * half_of;
-            if (j >= hi) j = hi - 1;
+            j = max(min(j, hi - 1), lo & ~15);
             return k < my_steps ? table[j >> a.g.page_shift] : 0;
         };
         auto issue = [&](int k, int32_t page) {
@@ -293,12 +217,8 @@ __global__ void __launch_bounds__(kWarps * 32, rows_blocks(C, NT)) k_attend_rows
             }
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            // 2^e with big 2^-e in [2^14, 2^15): exponents from the bits (zeros and subnormals keep a finite factor)
-            int e = static_cast<int>(__float_as_uint(big) >> 23) - 127 - 14;
-            if (e < -126) e = -126;
-            if (e > 113) e = 113;                            // inf or NaN: the row becomes NaN below
-            const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-            const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+            float down, up;
+            q_powers(big, down, up);
             float sum[NG];
 #pragma unroll
             for (int g = 0; g < NG; ++g) sum[g] = 0.0f;
@@ -807,7 +727,8 @@ namespace {
 
 // How a call is cut up.
 struct AttendPlan {
-    int tiles, rows_cap, ctas, min_units;
+    int tiles;                // 0: many rows, tiles of 128
+    int rows_cap, ctas, min_units, splits;
     int64_t items;            // at most
 };
 
@@ -822,9 +743,24 @@ int sm_count() {
     return n;
 }
 
+constexpr int64_t kFewPairs = 32;         // (query row, head) pairs of a kv head up to which the row kernel takes a call
+
 AttendPlan attend_plan(const CacheGeom &g, int q_heads, int64_t seqs, int64_t max_q, int64_t max_kv) {
     AttendPlan p;
     const int64_t pairs = max_q * (q_heads / g.kv_heads);
+    p.splits = 1;
+    if (pairs > kFewPairs) {
+        p.tiles = 0;
+        p.rows_cap = 256;
+        p.items = seqs * ceil_div(pairs, 256) * g.kv_heads;
+        p.ctas = 0;
+        p.min_units = 4;
+        const int64_t steps = ceil_div(max_kv, 128), want = sm_count() / p.items;
+        const int64_t most = steps / p.min_units;
+        p.splits = static_cast<int>(want < most ? want : most);
+        if (p.splits < 1) p.splits = 1;
+        return p;
+    }
     // registers: a tile of 8 rows costs 2 D / 32 accumulators and as much again for Q, so D > 64 takes two at most
     p.tiles = pairs <= 8 ? 1 : (pairs <= 16 || g.D > 64) ? 2 : 4;
     p.rows_cap = 8 * p.tiles;
@@ -837,6 +773,7 @@ AttendPlan attend_plan(const CacheGeom &g, int q_heads, int64_t seqs, int64_t ma
 }
 
 size_t attend_bytes(const AttendPlan &p, const CacheGeom &g) {
+    if (p.tiles == 0) return p.splits == 1 ? 0 : static_cast<size_t>(p.items) * p.splits * p.rows_cap * (g.D + 2) * sizeof(float);
     if (p.ctas == 1) return 0;
     return static_cast<size_t>(2) * p.ctas * p.rows_cap * (g.D + 2) * sizeof(float);
 }
@@ -920,6 +857,7 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
     a.rows_cap = p.rows_cap;
     a.ctas = p.ctas;
     a.items = p.items;
+    a.splits = p.splits;
     a.min_units = p.min_units;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const size_t need = attend_bytes(p, a.g);
@@ -936,7 +874,7 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
             a.part = static_cast<float *>(own);
         }
     }
-    const cudaError_t e = launch_attend_rows(a, p.tiles, s);
+    const cudaError_t e = p.tiles == 0 ? launch_attend_tiles(a, s) : launch_attend_rows(a, p.tiles, s);
     if (own) cudaFreeAsync(own, s);
     if (e != cudaSuccess) {
         cudaGetLastError();

@@ -25,7 +25,8 @@ struct AttendArgs {
     int rows_cap;             // (query row, head) pairs that an item of work holds
     int ctas;                 // workers among which the units are dealt out
     int64_t items;            // how many items there may be
-    int min_units;            // a worker takes at least this many
+    int min_units;            // a worker (or a piece) takes at least this many
+    int splits;               // tiles of 128 rows: pieces of an item's tokens
     float *part;              // unfinished items: [2 ctas][rows_cap x D sums, rows_cap maxima, rows_cap totals]
     unsigned *err;
 };
@@ -163,5 +164,8 @@ __device__ __forceinline__ int64_t worker_units(const AttendArgs &a, int64_t tot
 // few query rows per kv head: `tiles` x 8 pairs an item; then the items that workers share are joined
 cudaError_t launch_attend_rows(const AttendArgs &a, int tiles, cudaStream_t s);
 constexpr int kRowsUnit = 32;
+
+// many query rows per kv head: tiles of 128 rows on the tensor cores
+cudaError_t launch_attend_tiles(const AttendArgs &a, cudaStream_t s);
 
 }  // namespace qe

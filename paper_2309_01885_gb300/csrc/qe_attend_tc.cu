@@ -1,0 +1,628 @@
+// Attention over the 4-bit key/value cache, many query rows per kv head (chunks of
+// prompts, whole prompts): the fifth-generation tensor cores, codes turned into
+// operands on the way.
+//
+// A CTA takes 256 (query row, head) pairs that read one kv head, as two tiles of
+// 128 rows, and walks its visible tokens in steps of 128.  Bound by the tensor
+// cores' 4 x 128^2 x D products a step and, nearly as much, by issuing what
+// softmax (256 x 128 exponentials) and the turning of 2 x 128 x D codes cost; two
+// row tiles share each turned step.  Roles:
+//   warps 0-3, 4-7   softmax of row tile 0 and 1, a thread a row: scores from
+//                    tensor memory twice (maximum, then exponentials), P back in
+//                    place of the scores as the A operand of the second product;
+//   warps 8-11       codes to fp16 operands in shared memory (128-byte swizzle):
+//                    K as [token][channel], V as [channel][token];
+//   warp 12          one lane issues the products.  While one row tile is in
+//                    softmax the other one's products run.
+// Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16,
+// with powers of two for each 32 tokens that bring the largest scale to [1, 2); Q's
+// rows likewise.  2^F and the row's power of two go into the score's multiplier, E
+// into the exponent of P and 2^-E into the row sum, so that no magnitude leaves
+// fp16's range.  The running maximum is raised only when it is exceeded by 2^8, so
+// the accumulator in tensor memory is rarely rescaled.  Sums are fp32.
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "qe_attend.h"
+#include "qe_attend_out.cuh"
+#include "qe_internal.h"
+
+namespace qe {
+namespace {
+
+constexpr int kTile = 128;                // rows of a tile, tokens of a step
+constexpr int kThreads = 416;
+constexpr int kTurnWarp = 8, kMmaWarp = 12;
+constexpr int kInfos = 4;                // the turning warps are at most two steps ahead of softmax
+
+__device__ __forceinline__ void mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+        "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const float (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+        "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]),
+        "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]),
+        "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// What the softmax warps need to know of a turned step.
+struct StepInfo {
+    float key_up[4];          // 2^F of 32 tokens each
+    float val_exp[4];         // E
+    float val_down[4];        // 2^-E
+    uint8_t gone[4];          // of each 32 tokens, a bit for either 16: their page id is out of range
+    __device__ __forceinline__ unsigned gone_bits() const {
+        return static_cast<unsigned>(gone[0]) | gone[1] << 2 | gone[2] << 4 | gone[3] << 6;
+    }
+};
+
+template <int C, int GC>
+struct TcCfg {
+    static constexpr int D = 32 * C, NG = C / GC, DQ = D <= 64 ? 64 : 128;   // DQ: channels in whole swizzle atoms of 64
+    static constexpr int Q_BYTES = kTile * DQ * 2;        // one row tile
+    static constexpr int K_BYTES = kTile * DQ * 2;
+    static constexpr int V_BYTES = D * kTile * 2;
+    static constexpr int VPAIRS = 4 * 16 * NG * 8;        // (s, s'), (z, z') of the step's pairs of tokens
+    static constexpr int BAR_OFF = 2 * Q_BYTES + 2 * K_BYTES + 2 * V_BYTES + VPAIRS;
+    static constexpr int SMEM = 1024 + BAR_OFF + kInfos * static_cast<int>(sizeof(StepInfo)) + 2 * kTile * 4 + 256;
+    // one CTA an SM: it takes all of tensor memory
+    static constexpr int SMEM_ASKED = SMEM > 120 * 1024 ? SMEM : 120 * 1024;
+};
+
+template <int C, int GC>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a) {
+    using F = TcCfg<C, GC>;
+    constexpr int D = F::D, NG = F::NG;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
+    uint8_t *smem = smem_raw + pad;
+    uint8_t *sq = smem, *sk = sq + 2 * F::Q_BYTES, *sv_ = sk + 2 * F::K_BYTES, *spairs = sv_ + 2 * F::V_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + F::BAR_OFF);
+    uint64_t *q_full = bars, *k_full = bars + 1, *k_empty = bars + 3, *v_full = bars + 5, *v_empty = bars + 7;
+    uint64_t *s_full = bars + 9, *p_full = bars + 11, *pv_done = bars + 13, *drain = bars + 15;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 16);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    StepInfo *info = reinterpret_cast<StepInfo *>(bars + 18);
+    float *row_up = reinterpret_cast<float *>(info + kInfos);  // [2][kTile]
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // ---- this CTA's rows and tokens (uniform) ----
+    const int chunks = static_cast<int>(gridDim.x / static_cast<unsigned>(a.g.kv_heads));
+    const int chunk = chunks - 1 - static_cast<int>(blockIdx.x / static_cast<unsigned>(a.g.kv_heads));   // longest first
+    const int kvh = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.g.kv_heads));
+    const SeqView sv = seq_view(a, blockIdx.z, blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0);
+    const int all = sv.n * a.per_kv, first = chunk * 2 * kTile;
+    if (first >= all) return;
+    const int rows = all - first < 2 * kTile ? all - first : 2 * kTile;
+    const int tiles = rows > kTile ? 2 : 1;
+    int lo, hi;
+    visible(a, sv, first / a.per_kv, (first + rows - 1) / a.per_kv, lo, hi);
+    int begin = lo & ~(kTile - 1), steps = hi > lo ? (hi - begin + kTile - 1) / kTile : 0;
+    int pieces = 1;
+    if (a.splits > 1 && steps > 0) {                      // this piece's share of the steps
+        const int per = max((steps + a.splits - 1) / a.splits, a.min_units);
+        pieces = (steps + per - 1) / per;
+        if (static_cast<int>(blockIdx.y) >= pieces) return;
+        begin += static_cast<int>(blockIdx.y) * per * kTile;
+        steps = min(per, steps - static_cast<int>(blockIdx.y) * per);
+    } else if (blockIdx.y > 0) {
+        return;
+    }
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 128);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&k_full[s], 128);
+            mbar_init(&k_empty[s], 1);
+            mbar_init(&v_full[s], 128);
+            mbar_init(&v_empty[s], 1);
+            mbar_init(&s_full[s], 1);
+            mbar_init(&p_full[s], 128);
+            mbar_init(&pv_done[s], 1);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == kMmaWarp) tmem_alloc(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // the same answer for the whole warp, whose lanes go on together
+    auto wait_warp = [&](uint64_t *bar, unsigned parity) {
+        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag)) != 0;
+    };
+    auto give_up = [&]() {
+        *abort_flag = 1;
+        set_error(a.err, ERR_TIMEOUT);
+    };
+
+    if (warp == kMmaWarp) {
+        if (lane == 0) {
+            constexpr uint32_t id_s = idesc_f16_f32(kTile, kTile), id_o = idesc_f16_f32(kTile, D);
+            auto scores = [&](int i, int j) {             // S_i = Q_i K_j^T
+                const uint32_t qa = smem_u32(sq + i * F::Q_BYTES), kb = smem_u32(sk + (j & 1) * F::K_BYTES);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_bf16_ss(tmem + i * kTile, smem_desc_k128(qa + (k >> 2) * (kTile * 128)) + 2u * (k & 3),
+                                smem_desc_k128(kb + (k >> 2) * (kTile * 128)) + 2u * (k & 3), id_s, k == 0 ? 0u : 1u);
+                mma_commit(&s_full[i]);
+            };
+            bool ok = steps == 0 || mbar_wait_bounded(q_full, 0u, abort_flag);
+            if (ok && steps > 0) {
+                ok = mbar_wait_bounded(&k_full[0], 0u, abort_flag);
+                tc_fence_after();
+                if (ok) {
+                    for (int i = 0; i < tiles; ++i) scores(i, 0);
+                    mma_commit(&k_empty[0]);
+                }
+            }
+            for (int j = 0; ok && j < steps; ++j) {
+                const bool more = j + 1 < steps;
+                ok = mbar_wait_bounded(&v_full[j & 1], (j >> 1) & 1u, abort_flag);
+                for (int i = 0; ok && i < tiles; ++i) {
+                    ok = mbar_wait_bounded(&p_full[i], j & 1u, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t vb = smem_u32(sv_ + (j & 1) * F::V_BYTES);
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k)   // O_i += P_i V_j
+                        mma_f16_ts(tmem + 2 * kTile + i * kTile, tmem + i * kTile + 8 * k,
+                                   smem_desc_k128(vb + (k >> 2) * (D * 128)) + 2u * (k & 3), id_o, (j == 0 && k == 0) ? 0u : 1u);
+                    mma_commit(&pv_done[i]);
+                    if (i + 1 == tiles) mma_commit(&v_empty[j & 1]);
+                    if (more) {
+                        if (i == 0) {
+                            ok = mbar_wait_bounded(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u, abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
+                        scores(i, j + 1);
+                    }
+                }
+                if (!ok) break;
+                if (more) mma_commit(&k_empty[(j + 1) & 1]);
+            }
+            if (!ok) give_up();
+            mma_commit(drain);                            // nothing of this CTA's is in flight when tensor memory is freed
+            mbar_wait_bounded(drain, 0u, nullptr);
+        }
+    } else if (warp >= kTurnWarp) {
+        // ---- Q: two rows a thread, scaled into fp16 by a power of two each ----
+        const int tid = threadIdx.x - kTurnWarp * 32, w4 = warp - kTurnWarp;
+        for (int i = 0; i < tiles && steps > 0; ++i) {
+            const int p = i * kTile + tid;
+            const bool on = p < rows;
+            const unsigned pr = first + (on ? p : 0), qi = pr / static_cast<unsigned>(a.per_kv);
+            const int head = kvh * a.per_kv + static_cast<int>(pr - qi * a.per_kv);
+            float big = 0.0f;
+            for (int c8 = 0; c8 < D / 8; ++c8) {
+                float q[8];
+                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(q[e]));
+            }
+            float down, up;
+            q_powers(big, down, up);
+            row_up[i * kTile + tid] = up;
+            for (int c8 = 0; c8 < D / 8; ++c8) {
+                float q[8];
+                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
+                const float f = on ? down : 0.0f;
+                uint4 v;
+                v.x = pack_f16(q[0] * f, q[1] * f);
+                v.y = pack_f16(q[2] * f, q[3] * f);
+                v.z = pack_f16(q[4] * f, q[5] * f);
+                v.w = pack_f16(q[6] * f, q[7] * f);
+                if (!on) v = make_uint4(0u, 0u, 0u, 0u);
+                *reinterpret_cast<uint4 *>(sq + i * F::Q_BYTES + (c8 >> 3) * (kTile * 128) + tid * 128 + (((c8 & 7) ^ (tid & 7)) << 4)) = v;
+            }
+        }
+        fence_async_smem();
+        mbar_arrive(q_full);
+
+        // ---- codes to operands: a thread's token of K, and its 8 tokens x 4 C channels of V ----
+        const int32_t *table = a.table + blockIdx.z * a.table_ld;
+        const int page_mask = (1 << a.g.page_shift) - 1;
+        const int vr = lane >> 2, vb = lane & 3;          // V: channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
+        const int64_t page_bytes = a.g.kv_heads * a.g.block_bytes;
+        const uint8_t *mine = a.g.data + kvh * a.g.block_bytes;
+        const int64_t v_off = cache_v_off(a.g), kg_off = cache_kg_off(a.g), vg_off = cache_vg_off(a.g);
+        uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;
+        constexpr int PER = (16 * NG + 31) / 32;
+        uint32_t kw[4 * C], vw[4 * C], kg[NG], vg0[PER], vg1[PER];
+        unsigned gone = 0u;                               // bits of the step in kw / vw
+        auto fetch = [&](int j) {
+            // tokens beyond the visible ones take the nearest visible one's address; their grids are dropped below
+            const int t0 = begin + j * kTile + 32 * w4;
+            auto block_of = [&](int tok, bool &out) {
+                const int c = max(lo, min(tok, hi - 1));
+                int page = table[c >> a.g.page_shift];
+                out = static_cast<uint32_t>(page) >= static_cast<uint64_t>(a.g.pages);
+                if (out) page = 0;
+                return mine + page * page_bytes;
+            };
+            bool out;
+            const int tok = t0 + lane;
+            const uint8_t *blk = block_of(tok, out);
+            const unsigned votes = __ballot_sync(0xffffffffu, out);
+            gone = (votes & 1u) | (votes >> 15 & 2u);
+            if (votes && lane == 0) set_error(a.err, ERR_RANGE);
+            const int at = max(lo, min(tok, hi - 1)) & page_mask;
+            const uint4 *pk = reinterpret_cast<const uint4 *>(blk + at * (D / 2));
+#pragma unroll
+            for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&kw[4 * i]) = pk[i];
+            const uint32_t *pg = reinterpret_cast<const uint32_t *>(blk + kg_off) + at * NG;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) kg[g] = out || tok < lo || tok >= hi ? 0u : pg[g];
+            const int b0 = max(lo & ~7, min(t0 + 8 * vb, (hi - 1) & ~7));
+            blk = block_of(b0, out);
+            const uint4 *pv = reinterpret_cast<const uint4 *>(blk + v_off + (b0 & page_mask) * (D / 2) + vr * 16 * C);
+#pragma unroll
+            for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int q = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
+                const int t2 = t0 + 2 * (q / NG);
+                const uint8_t *b = block_of(t2, out);
+                const uint32_t *p = reinterpret_cast<const uint32_t *>(b + vg_off) + q % NG;
+                const bool on0 = !out && t2 >= lo && t2 < hi, on1 = !out && t2 + 1 >= lo && t2 + 1 < hi;
+                vg0[i] = on0 ? p[(t2 & page_mask) * NG] : 0u;
+                vg1[i] = on1 ? p[((t2 + 1) & page_mask) * NG] : 0u;
+            }
+        };
+        // a power of two that brings the largest of the warp's scales to [1, 2); NaN and -0 (bad tokens) apart
+        auto exponent = [&](int big) {
+            big = __reduce_max_sync(0xffffffffu, big);
+            int e = static_cast<int>(static_cast<uint32_t>(big) >> 23) - 127;
+            return big == 0 ? 0 : e < -100 ? -100 : e;
+        };
+        bool ok = true;
+        if (steps > 0) fetch(0);
+        for (int j = 0; j < steps; ++j) {
+            const int s = j & 1;
+            const unsigned ph = ((j >> 1) & 1u) ^ 1u;
+            // keys
+            int big = 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) big = max(big, kg[g] < 0x7F800000u ? static_cast<int>(kg[g]) : 0);
+            const int kf = exponent(big);
+            big = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) big = max(big, max(static_cast<int>(vg0[i]), static_cast<int>(vg1[i])));
+            const int ve = exponent(big);
+            if (!wait_warp(&k_empty[s], ph)) {
+                ok = false;
+                break;
+            }
+            {
+                const float down = __uint_as_float(static_cast<uint32_t>(127 - kf) << 23);
+                uint8_t *row = sk + s * F::K_BYTES + tid * 128;
+                // the token's words stand as [t][w]: channels 32 w + 8 t .. + 7, one 16-byte chunk each
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float sc = __uint_as_float(kg[g] & 0xFFFF0000u) * down, z = __uint_as_float(kg[g] << 16);
+                    const __half2 s2 = __float2half2_rn(sc), z2 = __float2half2_rn(z + 1024.0f), y2 = __float2half2_rn(-64.0f - z);
+                    const __half2 sixteenth = __float2half2_rn(0.0625f);
+#pragma unroll
+                    for (int w = g * GC; w < (g + 1) * GC; ++w)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const uint32_t x = kw[t * C + w], y = x >> 8;
+                            uint32_t h[4] = {(x & 0x000f000fu) | 0x64006400u, (x & 0x00f000f0u) | 0x64006400u,
+                                             (y & 0x000f000fu) | 0x64006400u, (y & 0x00f000f0u) | 0x64006400u};
+                            __half2 *v = reinterpret_cast<__half2 *>(h);
+                            v[0] = __hmul2(__hsub2(v[0], z2), s2);
+                            v[1] = __hmul2(__hfma2(v[1], sixteenth, y2), s2);
+                            v[2] = __hmul2(__hsub2(v[2], z2), s2);
+                            v[3] = __hmul2(__hfma2(v[3], sixteenth, y2), s2);
+                            const int ch = 4 * w + t;
+                            *reinterpret_cast<uint4 *>(row + (ch >> 3) * (kTile * 128) + (((ch & 7) ^ (tid & 7)) << 4)) =
+                                make_uint4(h[0], h[1], h[2], h[3]);
+                        }
+                }
+            }
+            if (lane == 0) {
+                info[j % kInfos].key_up[w4] = __uint_as_float(static_cast<uint32_t>(127 + kf) << 23);
+                info[j % kInfos].val_exp[w4] = static_cast<float>(ve);
+                info[j % kInfos].val_down[w4] = __uint_as_float(static_cast<uint32_t>(127 - ve) << 23);
+                info[j % kInfos].gone[w4] = static_cast<uint8_t>(gone);
+            }
+            fence_async_smem();
+            mbar_arrive(&k_full[s]);
+            // values: scales and zero points of pairs of tokens, turned once by the warp
+            {
+                const float down = __uint_as_float(static_cast<uint32_t>(127 - ve) << 23);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * down, __uint_as_float(vg1[i] & 0xFFFF0000u) * down);
+                    const __half2 z2 = __floats2half2_rn(__uint_as_float(vg0[i] << 16) + 1024.0f, __uint_as_float(vg1[i] << 16) + 1024.0f);
+                    if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG)
+                        pairs[lane + 32 * i] = make_uint2(*reinterpret_cast<const uint32_t *>(&s2), *reinterpret_cast<const uint32_t *>(&z2));
+                }
+                __syncwarp();
+            }
+            if (!wait_warp(&v_empty[s], ph)) {
+                ok = false;
+                break;
+            }
+            {
+                uint8_t *base = sv_ + s * F::V_BYTES + (w4 >> 1) * (D * 128);
+                const int ch = 4 * (w4 & 1) + vb;
+                const __half2 sixteenth = __float2half2_rn(0.0625f), m960 = __float2half2_rn(960.0f);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    __half2 s2[4], z2[4], y2[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint2 q = pairs[(4 * vb + t) * NG + g];
+                        s2[t] = *reinterpret_cast<const __half2 *>(&q.x);
+                        z2[t] = *reinterpret_cast<const __half2 *>(&q.y);
+                        y2[t] = __hsub2(m960, z2[t]);     // -(64 + z)
+                    }
+#pragma unroll
+                    for (int w = g * GC; w < (g + 1) * GC; ++w) {
+                        uint32_t h[4][4];                 // [channel][pair of tokens]
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const uint32_t x = vw[t * C + w], y = x >> 8;
+                            h[0][t] = (x & 0x000f000fu) | 0x64006400u;
+                            h[1][t] = (x & 0x00f000f0u) | 0x64006400u;
+                            h[2][t] = (y & 0x000f000fu) | 0x64006400u;
+                            h[3][t] = (y & 0x00f000f0u) | 0x64006400u;
+                            __half2 *v0 = reinterpret_cast<__half2 *>(&h[0][t]), *v1 = reinterpret_cast<__half2 *>(&h[1][t]);
+                            __half2 *v2 = reinterpret_cast<__half2 *>(&h[2][t]), *v3 = reinterpret_cast<__half2 *>(&h[3][t]);
+                            *v0 = __hmul2(__hsub2(*v0, z2[t]), s2[t]);
+                            *v1 = __hmul2(__hfma2(*v1, sixteenth, y2[t]), s2[t]);
+                            *v2 = __hmul2(__hsub2(*v2, z2[t]), s2[t]);
+                            *v3 = __hmul2(__hfma2(*v3, sixteenth, y2[t]), s2[t]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int d = 32 * w + 4 * vr + i;
+                            *reinterpret_cast<uint4 *>(base + d * 128 + ((ch ^ (d & 7)) << 4)) = make_uint4(h[i][0], h[i][1], h[i][2], h[i][3]);
+                        }
+                    }
+                }
+            }
+            fence_async_smem();
+            mbar_arrive(&v_full[s]);
+            if (j + 1 < steps) fetch(j + 1);
+            __syncwarp();                                 // the pairs are read before the next step's are written
+        }
+        if (!ok && lane == 0) give_up();
+    } else {
+        // ---- softmax: a thread a row ----
+        const int i = warp >> 2, quad = warp & 3, tid = threadIdx.x & (kTile - 1);
+        const int p = i * kTile + tid;
+        const bool on = p < rows;
+        const unsigned pr = first + (on ? p : 0), qi = pr / static_cast<unsigned>(a.per_kv);
+        const int head = kvh * a.per_kv + static_cast<int>(pr - qi * a.per_kv);
+        int see_lo, see_hi;
+        visible(a, sv, qi, qi, see_lo, see_hi);
+        const int all_lo = __reduce_max_sync(0xffffffffu, see_lo), all_hi = __reduce_min_sync(0xffffffffu, see_hi);
+        const uint32_t ts = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = ts + 2 * kTile;
+        float m = kFloor, l = 0.0f;
+        bool ok = i < tiles;
+        float mult = 0.0f;
+        for (int j = 0; ok && j < steps; ++j) {
+            if (!wait_warp(&s_full[i], j & 1u)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            // (the products of this step have read Q and K, so what came with them is there)
+            if (j == 0) mult = row_up[p] * a.scale2;
+            const StepInfo &in = info[j % kInfos];
+            const int j0 = begin + j * kTile;
+            const unsigned gone = in.gone_bits();
+            const bool edge = gone != 0u || j0 < all_lo || j0 + kTile > all_hi;
+            float top = kFloor;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                float v[32];
+                tmem_ld_32x32b_x32(ts + 32 * c, v);
+                if (edge) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int t = j0 + 32 * c + e;
+                        if (t < see_lo || t >= see_hi || ((gone >> (2 * c + (e >> 4))) & 1u)) v[e] = -CUDART_INF_F;
+                    }
+                }
+                float x0 = fmaxf(v[0], v[1]), x1 = fmaxf(v[2], v[3]);
+#pragma unroll
+                for (int e = 4; e < 32; e += 4) {
+                    x0 = fmaxf(x0, fmaxf(v[e], v[e + 1]));
+                    x1 = fmaxf(x1, fmaxf(v[e + 2], v[e + 3]));
+                }
+                top = fmaxf(top, fmaf(fmaxf(x0, x1), mult * in.key_up[c], in.val_exp[c]));
+            }
+            if (__any_sync(0xffffffffu, top > m + kRaise)) {
+                const float u = fmaxf(m, top), f = ex2(m - u);
+                m = u;
+                l *= f;
+                if (j > 0) {
+                    if (!wait_warp(&pv_done[i], (j - 1) & 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        float v[32];
+                        tmem_ld_32x32b_x32(to + 32 * c, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] *= f;
+                        tmem_st_x32(to + 32 * c, v);
+                    }
+                    tmem_wait_st();
+                }
+            }
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                float v[32];
+                tmem_ld_32x32b_x32(ts + 32 * c, v);
+                const float k = mult * in.key_up[c], b = in.val_exp[c] - m;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = fmaf(v[e], k, b);
+                if (edge) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int t = j0 + 32 * c + e;
+                        if (t < see_lo || t >= see_hi || ((gone >> (2 * c + (e >> 4))) & 1u)) v[e] = -CUDART_INF_F;
+                    }
+                }
+                float s0 = 0.0f, s1 = 0.0f;
+                uint32_t h[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    v[e] = ex2(v[e]);
+                    v[e + 1] = ex2(v[e + 1]);
+                    s0 += v[e];
+                    s1 += v[e + 1];
+                    h[e >> 1] = pack_f16(v[e], v[e + 1]);
+                }
+                l = fmaf(s0 + s1, in.val_down[c], l);
+                tmem_st_x16(ts + 16 * c, h);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(&p_full[i]);
+        }
+        if (ok && steps > 0) {
+            ok = wait_warp(&pv_done[i], (steps - 1) & 1u);
+            tc_fence_after();
+        }
+        if (i < tiles && !ok && lane == 0) give_up();
+        if (ok) {
+            float *slot = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * (2 * kTile * (D + 2)) +
+                          static_cast<int64_t>(blockIdx.y) * (2 * kTile * (D + 2));
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                float v[32];
+                if (steps > 0) {
+                    tmem_ld_32x32b_x32(to + 32 * c, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0.0f;
+                }
+                if (!on) continue;
+                if (pieces > 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4 *>(slot + p * D + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        if (32 * c + e < a.g.dim) finish(a, sv.row0 + qi, head, 32 * c + e, make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), m, l);
+                }
+            }
+            if (on && pieces > 1) {
+                slot[2 * kTile * D + p] = m;
+                slot[2 * kTile * (D + 1) + p] = l;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+// Joins the pieces of an item: the block of item x and sequence y, 8 rows a pass.
+__global__ void __launch_bounds__(256) k_attend_join_tiles(const AttendArgs a) {
+    const int chunks = static_cast<int>(gridDim.x / static_cast<unsigned>(a.g.kv_heads));
+    const int chunk = chunks - 1 - static_cast<int>(blockIdx.x / static_cast<unsigned>(a.g.kv_heads));
+    const int kvh = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.g.kv_heads));
+    const SeqView sv = seq_view(a, blockIdx.z, false);
+    const int all = sv.n * a.per_kv, first = chunk * 2 * kTile;
+    int pieces = 0, rows = 0;
+    if (first < all) {
+        rows = all - first < 2 * kTile ? all - first : 2 * kTile;
+        int lo, hi;
+        visible(a, sv, first / a.per_kv, (first + rows - 1) / a.per_kv, lo, hi);
+        const int steps = hi > lo ? (hi - (lo & ~(kTile - 1)) + kTile - 1) / kTile : 0;
+        const int per = max((steps + a.splits - 1) / a.splits, a.min_units);
+        pieces = (steps + per - 1) / per;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (pieces <= 1) return;
+    const int D = a.g.D, quads = D / 4;
+    const int64_t size = 2 * kTile * (D + 2);
+    const float *base = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * size;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < rows * quads; i += gridDim.y * 256) {
+        const int row = i / quads, d = 4 * (i % quads);
+        if (d >= a.g.dim) continue;
+        float big = kFloor, sum = 0.0f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < pieces; ++s) big = fmaxf(big, base[s * size + 2 * kTile * D + row]);
+        for (int s = 0; s < pieces; ++s) {
+            const float *p = base + s * size;
+            const float f = ex2(p[2 * kTile * D + row] - big);
+            const float4 u = *reinterpret_cast<const float4 *>(p + row * D + d);
+            sum = fmaf(f, p[2 * kTile * (D + 1) + row], sum);
+            v = make_float4(fmaf(f, u.x, v.x), fmaf(f, u.y, v.y), fmaf(f, u.z, v.z), fmaf(f, u.w, v.w));
+        }
+        const unsigned pr = first + row, q = pr / static_cast<unsigned>(a.per_kv);
+        finish(a, sv.row0 + q, kvh * a.per_kv + static_cast<int>(pr - q * a.per_kv), d, v, big, sum);
+    }
+}
+
+template <int C, int GC>
+cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) {
+    using F = TcCfg<C, GC>;
+    static const cudaError_t once =
+        cudaFuncSetAttribute(k_attend_tiles<C, GC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM_ASKED);
+    if (once != cudaSuccess) return once;
+    k_attend_tiles<C, GC><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tiles(const AttendArgs &a, cudaStream_t s) {
+    const int C = a.g.D / 32, GC = C / a.g.groups;
+    const unsigned items = static_cast<unsigned>(ceil_div(a.max_q * a.per_kv, 2 * kTile) * a.g.kv_heads);
+    const dim3 grid(items, static_cast<unsigned>(a.splits), static_cast<unsigned>(a.seqs));
+    cudaError_t e;
+    if (C == 2) e = GC == 1 ? launch_tiles<2, 1>(a, grid, s) : launch_tiles<2, 2>(a, grid, s);
+    else if (C == 3) e = launch_tiles<3, 1>(a, grid, s);
+    else if (GC == 1) e = launch_tiles<4, 1>(a, grid, s);
+    else if (GC == 2) e = launch_tiles<4, 2>(a, grid, s);
+    else e = launch_tiles<4, 4>(a, grid, s);
+    if (e != cudaSuccess || a.splits == 1) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(items, 8, static_cast<unsigned>(a.seqs));
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_attend_join_tiles, a);
+}
+
+}  // namespace qe

@@ -402,6 +402,16 @@ def test_workspace_streams_and_graphs():
     assert qe.qe_sync_status() == qe.QE_OK
 
 
+@pytest.mark.parametrize("q_len,window,page", [(1, 40, 16), (3, 17, 16), (100, 30, 16), (100, 200, 32)])
+def test_pages_that_left_the_window_are_not_looked_up(q_len, window, page):
+    n = 900
+    b = Batch([q_len, q_len], [n, n - 37], 4, 2, 64, 32, page, torch.bfloat16, seed=30)
+    want = b.run(window=window)
+    for i, m in enumerate(b.kv_len):
+        b.table[i, :(m - q_len - window + 1) // page] = -1        # freed: the oldest row's window starts later
+    assert torch.equal(b.run(window=window), want) and qe.qe_sync_status() == qe.QE_OK
+
+
 def test_device_side_bounds():
     """Page ids out of range, lengths past the table, more rows than announced: reported, nothing read outside."""
     b = Batch([1, 1, 1], [200, 100, 50], 4, 4, 64, 32, 16, torch.bfloat16, seed=21)
