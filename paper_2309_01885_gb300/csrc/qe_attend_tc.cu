@@ -10,8 +10,9 @@
 //   warps 0-3, 4-7   softmax of row tile 0 and 1, a thread a row: scores from
 //                    tensor memory twice (maximum, then exponentials), P back in
 //                    place of the scores as the A operand of the second product;
-//   warps 8-11       codes to fp16 operands in shared memory (128-byte swizzle):
-//                    K as [token][channel], V as [channel][token];
+//   warps 8-11       codes to fp16 operands in shared memory (128-byte swizzle), keys
+//                    as [token][channel], values as [channel][token]; the next step's
+//                    codes are loaded while the products run;
 //   warp 12          one lane issues the products.  While one row tile is in
 //                    softmax the other one's products run.
 // Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16,
@@ -63,6 +64,33 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const float (&v)[32]
         : "memory");
 }
 
+// (x, y) * k + b and sums, two at a time
+__device__ __forceinline__ void fma2(float &x, float &y, uint64_t k, uint64_t b) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(v) : "l"(k), "l"(b));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ uint64_t twice(float x) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(v) : "f"(x));
+    return v;
+}
+__device__ __forceinline__ void add2(uint64_t &s, float x, float y) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s) : "l"(v));
+}
+
+__device__ __forceinline__ float total(const uint64_t (&s)[4]) {
+    uint64_t v;
+    asm("{\n\t.reg .b64 t;\n\tadd.rn.f32x2 t, %1, %2;\n\tadd.rn.f32x2 %0, %3, %4;\n\tadd.rn.f32x2 %0, %0, t;\n\t}"
+        : "=&l"(v) : "l"(s[0]), "l"(s[1]), "l"(s[2]), "l"(s[3]));
+    float x, y;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+    return x + y;
+}
+
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -85,7 +113,7 @@ struct TcCfg {
     static constexpr int V_BYTES = D * kTile * 2;
     static constexpr int VPAIRS = 4 * 16 * NG * 8;        // (s, s'), (z, z') of the step's pairs of tokens
     static constexpr int BAR_OFF = 2 * Q_BYTES + 2 * K_BYTES + 2 * V_BYTES + VPAIRS;
-    static constexpr int SMEM = 1024 + BAR_OFF + kInfos * static_cast<int>(sizeof(StepInfo)) + 2 * kTile * 4 + 256;
+    static constexpr int SMEM = 1024 + BAR_OFF + kInfos * static_cast<int>(sizeof(StepInfo)) + 256;
     // one CTA an SM: it takes all of tensor memory
     static constexpr int SMEM_ASKED = SMEM > 120 * 1024 ? SMEM : 120 * 1024;
 };
@@ -104,7 +132,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 16);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     StepInfo *info = reinterpret_cast<StepInfo *>(bars + 18);
-    float *row_up = reinterpret_cast<float *>(info + kInfos);  // [2][kTile]
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -132,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     }
 
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 128);
+        mbar_init(q_full, 256);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&k_full[s], 128);
             mbar_init(&k_empty[s], 1);
@@ -211,122 +238,113 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             mbar_wait_bounded(drain, 0u, nullptr);
         }
     } else if (warp >= kTurnWarp) {
-        // ---- Q: two rows a thread, scaled into fp16 by a power of two each ----
-        const int tid = threadIdx.x - kTurnWarp * 32, w4 = warp - kTurnWarp;
-        for (int i = 0; i < tiles && steps > 0; ++i) {
-            const int p = i * kTile + tid;
-            const bool on = p < rows;
-            const unsigned pr = first + (on ? p : 0), qi = pr / static_cast<unsigned>(a.per_kv);
-            const int head = kvh * a.per_kv + static_cast<int>(pr - qi * a.per_kv);
-            float big = 0.0f;
-            for (int c8 = 0; c8 < D / 8; ++c8) {
-                float q[8];
-                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(q[e]));
-            }
-            float down, up;
-            q_powers(big, down, up);
-            row_up[i * kTile + tid] = up;
-            for (int c8 = 0; c8 < D / 8; ++c8) {
-                float q[8];
-                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
-                const float f = on ? down : 0.0f;
-                uint4 v;
-                v.x = pack_f16(q[0] * f, q[1] * f);
-                v.y = pack_f16(q[2] * f, q[3] * f);
-                v.z = pack_f16(q[4] * f, q[5] * f);
-                v.w = pack_f16(q[6] * f, q[7] * f);
-                if (!on) v = make_uint4(0u, 0u, 0u, 0u);
-                *reinterpret_cast<uint4 *>(sq + i * F::Q_BYTES + (c8 >> 3) * (kTile * 128) + tid * 128 + (((c8 & 7) ^ (tid & 7)) << 4)) = v;
-            }
-        }
-        fence_async_smem();
-        mbar_arrive(q_full);
-
-        // ---- codes to operands: a thread's token of K, and its 8 tokens x 4 C channels of V ----
+        const int tid = threadIdx.x & (kTile - 1), w4 = warp & 3;
+        // ---- codes to operands ----
         const int32_t *table = a.table + blockIdx.z * a.table_ld;
         const int page_mask = (1 << a.g.page_shift) - 1;
-        const int vr = lane >> 2, vb = lane & 3;          // V: channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
         const int64_t page_bytes = a.g.kv_heads * a.g.block_bytes;
         const uint8_t *mine = a.g.data + kvh * a.g.block_bytes;
         const int64_t v_off = cache_v_off(a.g), kg_off = cache_kg_off(a.g), vg_off = cache_vg_off(a.g);
-        uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;
-        constexpr int PER = (16 * NG + 31) / 32;
-        uint32_t kw[4 * C], vw[4 * C], kg[NG], vg0[PER], vg1[PER];
-        unsigned gone = 0u;                               // bits of the step in kw / vw
-        auto fetch = [&](int j) {
-            // tokens beyond the visible ones take the nearest visible one's address; their grids are dropped below
-            const int t0 = begin + j * kTile + 32 * w4;
-            auto block_of = [&](int tok, bool &out) {
-                const int c = max(lo, min(tok, hi - 1));
-                int page = table[c >> a.g.page_shift];
-                out = static_cast<uint32_t>(page) >= static_cast<uint64_t>(a.g.pages);
-                if (out) page = 0;
-                return mine + page * page_bytes;
-            };
-            bool out;
-            const int tok = t0 + lane;
-            const uint8_t *blk = block_of(tok, out);
-            const unsigned votes = __ballot_sync(0xffffffffu, out);
-            gone = (votes & 1u) | (votes >> 15 & 2u);
-            if (votes && lane == 0) set_error(a.err, ERR_RANGE);
-            const int at = max(lo, min(tok, hi - 1)) & page_mask;
-            const uint4 *pk = reinterpret_cast<const uint4 *>(blk + at * (D / 2));
+        // tokens beyond the visible ones take the nearest visible one's place in memory; their grids are dropped
+        auto near = [&](int tok) { return max(lo, min(tok, hi - 1)); };
+        auto block_of = [&](int page, bool &out) {
+            out = static_cast<uint32_t>(page) >= static_cast<uint64_t>(a.g.pages);
+            return mine + (out ? 0 : page) * page_bytes;
+        };
+        // a power of two that brings the largest of the warp's scales to [1, 2); NaN and -0 (bad tokens) apart
+        auto exponent = [&](int big) {
+            big = __reduce_max_sync(0xffffffffu, big);
+            const int e = static_cast<int>(static_cast<uint32_t>(big) >> 23) - 127;
+            return big == 0 ? 0 : e < -100 ? -100 : e;
+        };
+        auto power = [](int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); };
+        constexpr int PER = (16 * NG + 31) / 32;          // (pair of tokens, group)s of a lane
+        auto pair_of = [&](int i) { return lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1; };
+        uint32_t vg0[PER], vg1[PER];
+        int vpage[PER];
+        auto value_pages = [&](int j) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&kw[4 * i]) = pk[i];
-            const uint32_t *pg = reinterpret_cast<const uint32_t *>(blk + kg_off) + at * NG;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) kg[g] = out || tok < lo || tok >= hi ? 0u : pg[g];
-            const int b0 = max(lo & ~7, min(t0 + 8 * vb, (hi - 1) & ~7));
-            blk = block_of(b0, out);
-            const uint4 *pv = reinterpret_cast<const uint4 *>(blk + v_off + (b0 & page_mask) * (D / 2) + vr * 16 * C);
-#pragma unroll
-            for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
+            for (int i = 0; i < PER; ++i) vpage[i] = table[near(begin + j * kTile + 32 * w4 + 2 * (pair_of(i) / NG)) >> a.g.page_shift];
+        };
+        auto value_grids = [&](int j) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int q = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
-                const int t2 = t0 + 2 * (q / NG);
-                const uint8_t *b = block_of(t2, out);
-                const uint32_t *p = reinterpret_cast<const uint32_t *>(b + vg_off) + q % NG;
+                const int q = pair_of(i), t2 = begin + j * kTile + 32 * w4 + 2 * (q / NG);
+                bool out;
+                const uint32_t *p = reinterpret_cast<const uint32_t *>(block_of(vpage[i], out) + vg_off) + q % NG;
                 const bool on0 = !out && t2 >= lo && t2 < hi, on1 = !out && t2 + 1 >= lo && t2 + 1 < hi;
                 vg0[i] = on0 ? p[(t2 & page_mask) * NG] : 0u;
                 vg1[i] = on1 ? p[((t2 + 1) & page_mask) * NG] : 0u;
             }
         };
-        // a power of two that brings the largest of the warp's scales to [1, 2); NaN and -0 (bad tokens) apart
-        auto exponent = [&](int big) {
-            big = __reduce_max_sync(0xffffffffu, big);
-            int e = static_cast<int>(static_cast<uint32_t>(big) >> 23) - 127;
-            return big == 0 ? 0 : e < -100 ? -100 : e;
-        };
-        bool ok = true;
-        if (steps > 0) fetch(0);
-        for (int j = 0; j < steps; ++j) {
-            const int s = j & 1;
-            const unsigned ph = ((j >> 1) & 1u) ^ 1u;
-            // keys
+        auto value_exponent = [&]() {
             int big = 0;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) big = max(big, kg[g] < 0x7F800000u ? static_cast<int>(kg[g]) : 0);
-            const int kf = exponent(big);
-            big = 0;
-#pragma unroll
             for (int i = 0; i < PER; ++i) big = max(big, max(static_cast<int>(vg0[i]), static_cast<int>(vg1[i])));
-            const int ve = exponent(big);
-            if (!wait_warp(&k_empty[s], ph)) {
-                ok = false;
-                break;
+            return exponent(big);
+        };
+        const __half2 sixteenth = __float2half2_rn(0.0625f);
+        bool ok = true;
+        if (steps > 0) {
+            uint32_t kw[4 * C], kg[NG];
+            unsigned gone = 0u;                           // bits of the step in kw
+            int page = 0;
+            auto key_page = [&](int j) { page = table[near(begin + j * kTile + tid) >> a.g.page_shift]; };
+            auto key_codes = [&](int j) {
+                const int tok = begin + j * kTile + tid, at = near(tok) & page_mask;
+                bool out;
+                const uint8_t *blk = block_of(page, out);
+                const unsigned votes = __ballot_sync(0xffffffffu, out);
+                gone = (votes & 1u) | (votes >> 15 & 2u);
+                if (votes && lane == 0) set_error(a.err, ERR_RANGE);
+                const uint4 *pk = reinterpret_cast<const uint4 *>(blk + at * (D / 2));
+#pragma unroll
+                for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&kw[4 * i]) = pk[i];
+                const uint32_t *pg = reinterpret_cast<const uint32_t *>(blk + kg_off) + at * NG;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) kg[g] = out || tok < lo || tok >= hi ? 0u : pg[g];
+            };
+            const int vr = lane >> 2, vb = lane & 3;      // channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
+            uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;   // [group][pair]
+            uint32_t vw[4 * C];
+            int cpage = 0;
+            auto block_at = [&](int j) { return max(lo & ~7, min(begin + j * kTile + 32 * w4 + 8 * vb, (hi - 1) & ~7)); };
+            auto code_page = [&](int j) { cpage = table[block_at(j) >> a.g.page_shift]; };
+            auto codes = [&](int j) {
+                bool out;
+                const uint4 *pv = reinterpret_cast<const uint4 *>(block_of(cpage, out) + v_off + (block_at(j) & page_mask) * (D / 2) + vr * 16 * C);
+#pragma unroll
+                for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
+            };
+            const __half2 m960 = __float2half2_rn(960.0f);
+            key_page(0);
+            code_page(0);
+            value_pages(0);
+            key_codes(0);
+            codes(0);
+            value_grids(0);
+            if (steps > 1) {
+                key_page(1);
+                code_page(1);
+                value_pages(1);
             }
-            {
-                const float down = __uint_as_float(static_cast<uint32_t>(127 - kf) << 23);
+            for (int j = 0; j < steps; ++j) {
+                const int s = j & 1;
+                int big = 0;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) big = max(big, kg[g] < 0x7F800000u ? static_cast<int>(kg[g]) : 0);
+                const int kf = exponent(big), ve = value_exponent();
+                if (!wait_warp(&k_empty[s], ((j >> 1) & 1u) ^ 1u)) {
+                    ok = false;
+                    break;
+                }
+                const float down = power(-kf);
                 uint8_t *row = sk + s * F::K_BYTES + tid * 128;
                 // the token's words stand as [t][w]: channels 32 w + 8 t .. + 7, one 16-byte chunk each
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
                     const float sc = __uint_as_float(kg[g] & 0xFFFF0000u) * down, z = __uint_as_float(kg[g] << 16);
                     const __half2 s2 = __float2half2_rn(sc), z2 = __float2half2_rn(z + 1024.0f), y2 = __float2half2_rn(-64.0f - z);
-                    const __half2 sixteenth = __float2half2_rn(0.0625f);
 #pragma unroll
                     for (int w = g * GC; w < (g + 1) * GC; ++w)
 #pragma unroll
@@ -344,45 +362,56 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                                 make_uint4(h[0], h[1], h[2], h[3]);
                         }
                 }
-            }
-            if (lane == 0) {
-                info[j % kInfos].key_up[w4] = __uint_as_float(static_cast<uint32_t>(127 + kf) << 23);
-                info[j % kInfos].val_exp[w4] = static_cast<float>(ve);
-                info[j % kInfos].val_down[w4] = __uint_as_float(static_cast<uint32_t>(127 - ve) << 23);
-                info[j % kInfos].gone[w4] = static_cast<uint8_t>(gone);
-            }
-            fence_async_smem();
-            mbar_arrive(&k_full[s]);
-            // values: scales and zero points of pairs of tokens, turned once by the warp
-            {
-                const float down = __uint_as_float(static_cast<uint32_t>(127 - ve) << 23);
+                if (lane == 0) {
+                    StepInfo &in = info[j % kInfos];
+                    in.key_up[w4] = power(kf);
+                    in.val_exp[w4] = static_cast<float>(ve);
+                    in.val_down[w4] = power(-ve);
+                    in.gone[w4] = static_cast<uint8_t>(gone);
+                }
+                fence_async_smem();
+                mbar_arrive(&k_full[s]);
+                if (j + 1 < steps) {
+                    key_codes(j + 1);
+                    if (j + 2 < steps) key_page(j + 2);
+                }
+                // scales and zero points of pairs of tokens, turned once by the warp
+                const float vdown = power(-ve);
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * down, __uint_as_float(vg1[i] & 0xFFFF0000u) * down);
+                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * vdown, __uint_as_float(vg1[i] & 0xFFFF0000u) * vdown);
                     const __half2 z2 = __floats2half2_rn(__uint_as_float(vg0[i] << 16) + 1024.0f, __uint_as_float(vg1[i] << 16) + 1024.0f);
+                    const int q = pair_of(i);
                     if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG)
-                        pairs[lane + 32 * i] = make_uint2(*reinterpret_cast<const uint32_t *>(&s2), *reinterpret_cast<const uint32_t *>(&z2));
+                        pairs[(q % NG) * 16 + q / NG] = make_uint2(*reinterpret_cast<const uint32_t *>(&s2), *reinterpret_cast<const uint32_t *>(&z2));
                 }
                 __syncwarp();
-            }
-            if (!wait_warp(&v_empty[s], ph)) {
-                ok = false;
-                break;
-            }
-            {
+                if (j + 1 < steps) {
+                    value_grids(j + 1);
+                    if (j + 2 < steps) value_pages(j + 2);
+                }
+                if (!wait_warp(&v_empty[s], ((j >> 1) & 1u) ^ 1u)) {
+                    ok = false;
+                    break;
+                }
                 uint8_t *base = sv_ + s * F::V_BYTES + (w4 >> 1) * (D * 128);
                 const int ch = 4 * (w4 & 1) + vb;
-                const __half2 sixteenth = __float2half2_rn(0.0625f), m960 = __float2half2_rn(960.0f);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
                     __half2 s2[4], z2[4], y2[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const uint2 q = pairs[(4 * vb + t) * NG + g];
-                        s2[t] = *reinterpret_cast<const __half2 *>(&q.x);
-                        z2[t] = *reinterpret_cast<const __half2 *>(&q.y);
-                        y2[t] = __hsub2(m960, z2[t]);     // -(64 + z)
+                    {
+                        const uint4 q0 = *reinterpret_cast<const uint4 *>(&pairs[g * 16 + 4 * vb]), q1 = *reinterpret_cast<const uint4 *>(&pairs[g * 16 + 4 * vb + 2]);
+                        s2[0] = *reinterpret_cast<const __half2 *>(&q0.x);
+                        z2[0] = *reinterpret_cast<const __half2 *>(&q0.y);
+                        s2[1] = *reinterpret_cast<const __half2 *>(&q0.z);
+                        z2[1] = *reinterpret_cast<const __half2 *>(&q0.w);
+                        s2[2] = *reinterpret_cast<const __half2 *>(&q1.x);
+                        z2[2] = *reinterpret_cast<const __half2 *>(&q1.y);
+                        s2[3] = *reinterpret_cast<const __half2 *>(&q1.z);
+                        z2[3] = *reinterpret_cast<const __half2 *>(&q1.w);
                     }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) y2[t] = __hsub2(m960, z2[t]);     // -(64 + z)
 #pragma unroll
                     for (int w = g * GC; w < (g + 1) * GC; ++w) {
                         uint32_t h[4][4];                 // [channel][pair of tokens]
@@ -407,11 +436,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                         }
                     }
                 }
+                fence_async_smem();
+                mbar_arrive(&v_full[s]);
+                if (j + 1 < steps) {
+                    codes(j + 1);
+                    if (j + 2 < steps) code_page(j + 2);
+                }
+                __syncwarp();                             // the pairs are read before the next step's are written
             }
-            fence_async_smem();
-            mbar_arrive(&v_full[s]);
-            if (j + 1 < steps) fetch(j + 1);
-            __syncwarp();                                 // the pairs are read before the next step's are written
         }
         if (!ok && lane == 0) give_up();
     } else {
@@ -425,50 +457,83 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         visible(a, sv, qi, qi, see_lo, see_hi);
         const int all_lo = __reduce_max_sync(0xffffffffu, see_lo), all_hi = __reduce_min_sync(0xffffffffu, see_hi);
         const uint32_t ts = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = ts + 2 * kTile;
-        float m = kFloor, l = 0.0f;
-        bool ok = i < tiles;
+        // Q: scaled into fp16 by a power of two of the row
         float mult = 0.0f;
-        for (int j = 0; ok && j < steps; ++j) {
-            if (!wait_warp(&s_full[i], j & 1u)) {
-                ok = false;
-                break;
+        if (i < tiles && steps > 0) {
+            float big = 0.0f;
+#pragma unroll 4
+            for (int c8 = 0; c8 < D / 8; ++c8) {
+                float q[8];
+                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(q[e]));
             }
+            float down, up;
+            q_powers(big, down, up);
+            mult = up * a.scale2;
+            uint8_t *row = sq + i * F::Q_BYTES + tid * 128;
+#pragma unroll 4
+            for (int c8 = 0; c8 < D / 8; ++c8) {
+                float q[8];
+                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (on) {
+                    v.x = pack_f16(q[0] * down, q[1] * down);
+                    v.y = pack_f16(q[2] * down, q[3] * down);
+                    v.z = pack_f16(q[4] * down, q[5] * down);
+                    v.w = pack_f16(q[6] * down, q[7] * down);
+                }
+                *reinterpret_cast<uint4 *>(row + (c8 >> 3) * (kTile * 128) + (((c8 & 7) ^ (tid & 7)) << 4)) = v;
+            }
+            fence_async_smem();
+        }
+        mbar_arrive(q_full);
+        float m = kFloor, l = 0.0f;
+        bool ok = true;                                   // once false the remaining waits return at once
+        for (int j = 0; i < tiles && j < steps; ++j) {
+            ok = wait_warp(&s_full[i], j & 1u) && ok;
             tc_fence_after();
-            // (the products of this step have read Q and K, so what came with them is there)
-            if (j == 0) mult = row_up[p] * a.scale2;
+            // (the products of this step have read K, so what came with it is there)
             const StepInfo &in = info[j % kInfos];
             const int j0 = begin + j * kTile;
             const unsigned gone = in.gone_bits();
             const bool edge = gone != 0u || j0 < all_lo || j0 + kTile > all_hi;
+            // bit e: the row sees token e of the 32 from 32 c on
+            auto seen = [&](int c) {
+                const int t0 = j0 + 32 * c, from = max(see_lo - t0, 0), upto = min(see_hi - t0, 32);
+                unsigned bits = from < 32 ? 0xffffffffu << from : 0u;
+                bits &= upto > 0 ? 0xffffffffu >> (32 - upto) : 0u;
+                if ((gone >> (2 * c)) & 1u) bits &= 0xffff0000u;
+                if ((gone >> (2 * c)) & 2u) bits &= 0x0000ffffu;
+                return bits;
+            };
+            auto hide = [](float (&v)[32], unsigned bits) {
+                asm volatile("" ::: "memory");            // a branch around this, not selects on every step
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (!((bits >> e) & 1u)) v[e] = -CUDART_INF_F;
+            };
             float top = kFloor;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 float v[32];
                 tmem_ld_32x32b_x32(ts + 32 * c, v);
-                if (edge) {
+                if (edge) hide(v, seen(c));
+                float x[4];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int t = j0 + 32 * c + e;
-                        if (t < see_lo || t >= see_hi || ((gone >> (2 * c + (e >> 4))) & 1u)) v[e] = -CUDART_INF_F;
-                    }
-                }
-                float x0 = fmaxf(v[0], v[1]), x1 = fmaxf(v[2], v[3]);
+                for (int q = 0; q < 4; ++q) x[q] = fmaxf(v[q], v[q + 4]);
 #pragma unroll
-                for (int e = 4; e < 32; e += 4) {
-                    x0 = fmaxf(x0, fmaxf(v[e], v[e + 1]));
-                    x1 = fmaxf(x1, fmaxf(v[e + 2], v[e + 3]));
-                }
-                top = fmaxf(top, fmaf(fmaxf(x0, x1), mult * in.key_up[c], in.val_exp[c]));
+                for (int e = 8; e < 32; e += 8)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[e + q], v[e + q + 4]));
+                top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c], in.val_exp[c]));
             }
             if (__any_sync(0xffffffffu, top > m + kRaise)) {
                 const float u = fmaxf(m, top), f = ex2(m - u);
                 m = u;
                 l *= f;
                 if (j > 0) {
-                    if (!wait_warp(&pv_done[i], (j - 1) & 1u)) {
-                        ok = false;
-                        break;
-                    }
+                    ok = wait_warp(&pv_done[i], (j - 1) & 1u) && ok;
                     tc_fence_after();
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
@@ -478,46 +543,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                         for (int e = 0; e < 32; ++e) v[e] *= f;
                         tmem_st_x32(to + 32 * c, v);
                     }
-                    tmem_wait_st();
                 }
             }
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 float v[32];
                 tmem_ld_32x32b_x32(ts + 32 * c, v);
-                const float k = mult * in.key_up[c], b = in.val_exp[c] - m;
+                const uint64_t k = twice(mult * in.key_up[c]), b = twice(in.val_exp[c] - m);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = fmaf(v[e], k, b);
-                if (edge) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int t = j0 + 32 * c + e;
-                        if (t < see_lo || t >= see_hi || ((gone >> (2 * c + (e >> 4))) & 1u)) v[e] = -CUDART_INF_F;
-                    }
-                }
-                float s0 = 0.0f, s1 = 0.0f;
+                for (int e = 0; e < 32; e += 2) fma2(v[e], v[e + 1], k, b);
+                if (edge) hide(v, seen(c));
+                uint64_t sum[4] = {0, 0, 0, 0};
                 uint32_t h[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
                     v[e] = ex2(v[e]);
                     v[e + 1] = ex2(v[e + 1]);
-                    s0 += v[e];
-                    s1 += v[e + 1];
+                    add2(sum[(e >> 1) & 3], v[e], v[e + 1]);
                     h[e >> 1] = pack_f16(v[e], v[e + 1]);
                 }
-                l = fmaf(s0 + s1, in.val_down[c], l);
-                tmem_st_x16(ts + 16 * c, h);
+                l = fmaf(total(sum), in.val_down[c], l);
+                tmem_st_x16(ts + 16 * c, h);              // columns whose scores this thread has read
             }
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&p_full[i]);
         }
-        if (ok && steps > 0) {
-            ok = wait_warp(&pv_done[i], (steps - 1) & 1u);
+        if (i < tiles && steps > 0) {
+            ok = wait_warp(&pv_done[i], (steps - 1) & 1u) && ok;
             tc_fence_after();
+            if (!ok && lane == 0) give_up();
         }
-        if (i < tiles && !ok && lane == 0) give_up();
-        if (ok) {
+        if (i < tiles) {
             float *slot = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * (2 * kTile * (D + 2)) +
                           static_cast<int64_t>(blockIdx.y) * (2 * kTile * (D + 2));
 #pragma unroll 1
