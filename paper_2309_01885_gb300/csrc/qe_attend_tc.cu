@@ -7,14 +7,17 @@
 // cores' 4 x 128^2 x D products a step and, nearly as much, by issuing what
 // softmax (256 x 128 exponentials) and the turning of 2 x 128 x D codes cost; two
 // row tiles share each turned step.  Roles:
-//   warps 0-3, 4-7   softmax of row tile 0 and 1, a thread a row: scores from
-//                    tensor memory twice (maximum, then exponentials), P back in
-//                    place of the scores as the A operand of the second product;
-//   warps 8-11       codes to fp16 operands in shared memory (128-byte swizzle), keys
-//                    as [token][channel], values as [channel][token]; the next step's
-//                    codes are loaded while the products run;
-//   warp 12          one lane issues the products.  While one row tile is in
-//                    softmax the other one's products run.
+//   warps 0-3, 4-7   softmax of row tile 0 and 1, a thread a row, 64 tokens a round:
+//                    scores from tensor memory into registers, P back in place of
+//                    the scores as the A operand of the second product;
+//   warps 8-11       key codes to fp16 operands [token][channel] in shared memory
+//                    (128-byte swizzle), warps 12-15 value codes to [channel][token];
+//                    the next step's codes are loaded while the products run;
+//   warp 16          one lane issues the products.  Two score buffers of 64 tokens a
+//                    row tile: the products of one round run while softmax is at the
+//                    next.  (A thread of the softmax warps that issued them itself was
+//                    held 1600 cycles a round by the filled tensor queue.)
+// Registers are dealt out anew at the start: softmax keeps a round's scores in them.
 // Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16,
 // with powers of two for each 32 tokens that bring the largest scale to [1, 2); Q's
 // rows likewise.  2^F and the row's power of two go into the score's multiplier, E
@@ -32,35 +35,74 @@ namespace qe {
 namespace {
 
 constexpr int kTile = 128;                // rows of a tile, tokens of a step
-constexpr int kThreads = 416;
-constexpr int kTurnWarp = 8, kMmaWarp = 12;
+constexpr int kHalf = 64;                 // tokens of a softmax round
+constexpr int kThreads = 640;             // the last three warps only lend their registers
+constexpr int kKeyWarp = 8, kValWarp = 12, kMmaWarp = 16;
+// registers a thread: at launch, then softmax, turning and the rest (256 x 128 + 256 x 80 + 128 x 64 = 640 x 96)
+constexpr int kLaunchRegs = 96, kSoftRegs = 128, kTurnRegs = 80, kRestRegs = 64;
+static_assert(256 * kSoftRegs + 256 * kTurnRegs + 128 * kRestRegs <= kThreads * kLaunchRegs, "more registers asked for than launched with");
 constexpr int kInfos = 4;                // the turning warps are at most two steps ahead of softmax
 
-__device__ __forceinline__ void mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// Issued by one elected lane of a warp that goes along together, so that addresses stay in
+// uniform registers.
+__device__ __forceinline__ void mma_ts_one(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
         "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void mma_ss_one(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const float (&v)[32]) {
+__device__ __forceinline__ void commit_one(uint32_t bar) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-        "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]),
-        "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]),
-        "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+// 64 columns of the thread's row.
+__device__ __forceinline__ void tmem_ld_x64(uint32_t taddr, float (&v)[64]) {
+    asm volatile(
+        "{\n\ttcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t}"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+        : "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, float (&v)[16]) {
+    asm volatile(
+        "{\n\ttcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t}"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const float (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
         : "memory");
 }
 
@@ -105,6 +147,11 @@ struct StepInfo {
     }
 };
 
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 template <int C, int GC>
 struct TcCfg {
     static constexpr int D = 32 * C, NG = C / GC, DQ = D <= 64 ? 64 : 128;   // DQ: channels in whole swizzle atoms of 64
@@ -127,11 +174,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     uint8_t *smem = smem_raw + pad;
     uint8_t *sq = smem, *sk = sq + 2 * F::Q_BYTES, *sv_ = sk + 2 * F::K_BYTES, *spairs = sv_ + 2 * F::V_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + F::BAR_OFF);
-    uint64_t *q_full = bars, *k_full = bars + 1, *k_empty = bars + 3, *v_full = bars + 5, *v_empty = bars + 7;
-    uint64_t *s_full = bars + 9, *p_full = bars + 11, *pv_done = bars + 13, *drain = bars + 15;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 16);
+    uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
+    uint64_t *s_full = bars + 8, *pv_done = bars + 12, *p_full = bars + 16;   // [row tile][round & 1]
+    uint64_t *q_full = bars + 20, *drain = bars + 21;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 22);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    StepInfo *info = reinterpret_cast<StepInfo *>(bars + 18);
+    StepInfo *info = reinterpret_cast<StepInfo *>(bars + 24);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -159,16 +207,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     }
 
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 256);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&k_full[s], 128);
             mbar_init(&k_empty[s], 1);
             mbar_init(&v_full[s], 128);
             mbar_init(&v_empty[s], 1);
             mbar_init(&s_full[s], 1);
-            mbar_init(&p_full[s], 128);
+            mbar_init(&s_full[2 + s], 1);
             mbar_init(&pv_done[s], 1);
+            mbar_init(&pv_done[2 + s], 1);
+            mbar_init(&p_full[s], 128);
+            mbar_init(&p_full[2 + s], 128);
         }
+        mbar_init(q_full, 256);
         mbar_init(drain, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -187,57 +238,69 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         set_error(a.err, ERR_TIMEOUT);
     };
 
-    if (warp == kMmaWarp) {
-        if (lane == 0) {
-            constexpr uint32_t id_s = idesc_f16_f32(kTile, kTile), id_o = idesc_f16_f32(kTile, D);
-            auto scores = [&](int i, int j) {             // S_i = Q_i K_j^T
-                const uint32_t qa = smem_u32(sq + i * F::Q_BYTES), kb = smem_u32(sk + (j & 1) * F::K_BYTES);
+    const int halves = hi > begin ? min(2 * steps, (hi - begin + kHalf - 1) / kHalf) : 0;   // rounds
+
+    if (warp >= kMmaWarp) {
+        regs_down<kRestRegs>();
+        if (warp == kMmaWarp && halves > 0) {
+            const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
+            const int rounds = __shfl_sync(0xffffffffu, halves, 0), row_tiles = __shfl_sync(0xffffffffu, tiles, 0);
+            const uint32_t bar0 = smem_u32(bars);         // barriers as above, 8 bytes each
+            const uint64_t q0 = smem_desc_k128(smem_u32(sq)), k0 = smem_desc_k128(smem_u32(sk)), v0 = smem_desc_k128(smem_u32(sv_));
+            // S_i = Q_i K^T of round u into buffer u & 1 (descriptors count 16-byte units)
+            auto scores = [&](int i, int u) {
+                constexpr uint32_t id = idesc_f16_f32(kTile, kHalf);
+                const uint64_t qa = q0 + i * (F::Q_BYTES / 16), kb = k0 + ((u >> 1) & 1) * (F::K_BYTES / 16) + (u & 1) * (kHalf * 8);
+                const uint32_t d = t0 + i * kTile + (u & 1) * kHalf;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    mma_bf16_ss(tmem + i * kTile, smem_desc_k128(qa + (k >> 2) * (kTile * 128)) + 2u * (k & 3),
-                                smem_desc_k128(kb + (k >> 2) * (kTile * 128)) + 2u * (k & 3), id_s, k == 0 ? 0u : 1u);
-                mma_commit(&s_full[i]);
+                    mma_ss_one(d, qa + (k >> 2) * (kTile * 8) + 2 * (k & 3), kb + (k >> 2) * (kTile * 8) + 2 * (k & 3), id, k == 0 ? 0u : 1u);
+                commit_one(bar0 + 8 * (8 + 2 * i + (u & 1)));
             };
-            bool ok = steps == 0 || mbar_wait_bounded(q_full, 0u, abort_flag);
-            if (ok && steps > 0) {
-                ok = mbar_wait_bounded(&k_full[0], 0u, abort_flag);
-                tc_fence_after();
-                if (ok) {
-                    for (int i = 0; i < tiles; ++i) scores(i, 0);
-                    mma_commit(&k_empty[0]);
-                }
-            }
-            for (int j = 0; ok && j < steps; ++j) {
-                const bool more = j + 1 < steps;
-                ok = mbar_wait_bounded(&v_full[j & 1], (j >> 1) & 1u, abort_flag);
-                for (int i = 0; ok && i < tiles; ++i) {
-                    ok = mbar_wait_bounded(&p_full[i], j & 1u, abort_flag);
+            // O_i += P_i V of round u
+            auto values = [&](int i, int u) {
+                constexpr uint32_t id = idesc_f16_f32(kTile, D);
+                const uint64_t vb = v0 + ((u >> 1) & 1) * (F::V_BYTES / 16) + (u & 1) * (D * 8);
+                const uint32_t pa = t0 + i * kTile + (u & 1) * kHalf, d = t0 + 2 * kTile + i * kTile;
+                const uint32_t more = u > 0 ? 1u : 0u;
+#pragma unroll
+                for (int k = 0; k < kHalf / 16; ++k) mma_ts_one(d, pa + 8 * k, vb + 2 * k, id, k == 0 ? more : 1u);
+                commit_one(bar0 + 8 * (12 + 2 * i + (u & 1)));
+            };
+            bool ok = wait_warp(q_full, 0u) && wait_warp(&k_full[0], 0u);
+            tc_fence_after();
+            for (int u = 0; ok && u < 2 && u < rounds; ++u)
+                for (int i = 0; i < row_tiles; ++i) scores(i, u);
+            if (ok) commit_one(smem_u32(&k_empty[0]));
+            for (int u = 0; ok && u < rounds; ++u) {
+                const int j = u >> 1;
+                if (!(u & 1)) ok = wait_warp(&v_full[j & 1], (j >> 1) & 1u);
+                for (int i = 0; ok && i < row_tiles; ++i) {
+                    ok = wait_warp(&p_full[2 * i + (u & 1)], j & 1u);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t vb = smem_u32(sv_ + (j & 1) * F::V_BYTES);
-#pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)   // O_i += P_i V_j
-                        mma_f16_ts(tmem + 2 * kTile + i * kTile, tmem + i * kTile + 8 * k,
-                                   smem_desc_k128(vb + (k >> 2) * (D * 128)) + 2u * (k & 3), id_o, (j == 0 && k == 0) ? 0u : 1u);
-                    mma_commit(&pv_done[i]);
-                    if (i + 1 == tiles) mma_commit(&v_empty[j & 1]);
-                    if (more) {
-                        if (i == 0) {
-                            ok = mbar_wait_bounded(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u, abort_flag);
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        scores(i, j + 1);
+                    values(i, u);
+                    if (u + 2 >= rounds) continue;
+                    if (i == 0 && !(u & 1)) {
+                        ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
                     }
+                    scores(i, u + 2);
                 }
-                if (!ok) break;
-                if (more) mma_commit(&k_empty[(j + 1) & 1]);
+                if (ok && (u & 1)) {                      // both halves of step j's V, of step j + 1's K have been multiplied
+                    commit_one(smem_u32(&v_empty[j & 1]));
+                    commit_one(smem_u32(&k_empty[(j + 1) & 1]));
+                }
             }
-            if (!ok) give_up();
-            mma_commit(drain);                            // nothing of this CTA's is in flight when tensor memory is freed
+            if (!ok && lane == 0) give_up();
+            __syncwarp();
+            commit_one(smem_u32(drain));                  // nothing of this CTA's is in flight when tensor memory is freed
             mbar_wait_bounded(drain, 0u, nullptr);
         }
-    } else if (warp >= kTurnWarp) {
+    } else if (warp >= kKeyWarp) {
+        regs_down<kTurnRegs>();
+        const bool keys = warp < kValWarp;
         const int tid = threadIdx.x & (kTile - 1), w4 = warp & 3;
         // ---- codes to operands ----
         const int32_t *table = a.table + blockIdx.z * a.table_ld;
@@ -285,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         };
         const __half2 sixteenth = __float2half2_rn(0.0625f);
         bool ok = true;
-        if (steps > 0) {
+        if (keys && steps > 0) {
             uint32_t kw[4 * C], kg[NG];
             unsigned gone = 0u;                           // bits of the step in kw
             int page = 0;
@@ -304,28 +367,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 #pragma unroll
                 for (int g = 0; g < NG; ++g) kg[g] = out || tok < lo || tok >= hi ? 0u : pg[g];
             };
-            const int vr = lane >> 2, vb = lane & 3;      // channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
-            uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;   // [group][pair]
-            uint32_t vw[4 * C];
-            int cpage = 0;
-            auto block_at = [&](int j) { return max(lo & ~7, min(begin + j * kTile + 32 * w4 + 8 * vb, (hi - 1) & ~7)); };
-            auto code_page = [&](int j) { cpage = table[block_at(j) >> a.g.page_shift]; };
-            auto codes = [&](int j) {
-                bool out;
-                const uint4 *pv = reinterpret_cast<const uint4 *>(block_of(cpage, out) + v_off + (block_at(j) & page_mask) * (D / 2) + vr * 16 * C);
-#pragma unroll
-                for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
-            };
-            const __half2 m960 = __float2half2_rn(960.0f);
             key_page(0);
-            code_page(0);
             value_pages(0);
             key_codes(0);
-            codes(0);
             value_grids(0);
             if (steps > 1) {
                 key_page(1);
-                code_page(1);
                 value_pages(1);
             }
             for (int j = 0; j < steps; ++j) {
@@ -373,13 +420,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 mbar_arrive(&k_full[s]);
                 if (j + 1 < steps) {
                     key_codes(j + 1);
-                    if (j + 2 < steps) key_page(j + 2);
+                    value_grids(j + 1);
+                    if (j + 2 < steps) {
+                        key_page(j + 2);
+                        value_pages(j + 2);
+                    }
                 }
+            }
+        } else if (steps > 0) {
+            const int vr = lane >> 2, vb = lane & 3;      // channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
+            uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;   // [group][pair]
+            uint32_t vw[4 * C];
+            int page = 0;
+            auto block_at = [&](int j) { return max(lo & ~7, min(begin + j * kTile + 32 * w4 + 8 * vb, (hi - 1) & ~7)); };
+            auto code_page = [&](int j) { page = table[block_at(j) >> a.g.page_shift]; };
+            auto codes = [&](int j) {
+                bool out;
+                const uint4 *pv = reinterpret_cast<const uint4 *>(block_of(page, out) + v_off + (block_at(j) & page_mask) * (D / 2) + vr * 16 * C);
+#pragma unroll
+                for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
+            };
+            code_page(0);
+            value_pages(0);
+            codes(0);
+            value_grids(0);
+            if (steps > 1) {
+                code_page(1);
+                value_pages(1);
+            }
+            const __half2 m960 = __float2half2_rn(960.0f);
+            for (int j = 0; j < steps; ++j) {
+                const int s = j & 1;
                 // scales and zero points of pairs of tokens, turned once by the warp
-                const float vdown = power(-ve);
+                const float down = power(-value_exponent());
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * vdown, __uint_as_float(vg1[i] & 0xFFFF0000u) * vdown);
+                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * down, __uint_as_float(vg1[i] & 0xFFFF0000u) * down);
                     const __half2 z2 = __floats2half2_rn(__uint_as_float(vg0[i] << 16) + 1024.0f, __uint_as_float(vg1[i] << 16) + 1024.0f);
                     const int q = pair_of(i);
                     if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG)
@@ -447,6 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         }
         if (!ok && lane == 0) give_up();
     } else {
+        regs_up<kSoftRegs>();
         // ---- softmax: a thread a row ----
         const int i = warp >> 2, quad = warp & 3, tid = threadIdx.x & (kTile - 1);
         const int p = i * kTile + tid;
@@ -456,121 +533,135 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         int see_lo, see_hi;
         visible(a, sv, qi, qi, see_lo, see_hi);
         const int all_lo = __reduce_max_sync(0xffffffffu, see_lo), all_hi = __reduce_min_sync(0xffffffffu, see_hi);
-        const uint32_t ts = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = ts + 2 * kTile;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = lanes + 2 * kTile;
+        bool ok = true;                                   // once false the remaining waits return at once
         // Q: scaled into fp16 by a power of two of the row
         float mult = 0.0f;
-        if (i < tiles && steps > 0) {
-            float big = 0.0f;
-#pragma unroll 4
-            for (int c8 = 0; c8 < D / 8; ++c8) {
-                float q[8];
-                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
+        if (i < tiles && halves > 0) {
+            uint4 raw[D / 8];
+            const uint16_t *from = reinterpret_cast<const uint16_t *>(a.Q) + (sv.row0 + qi) * a.q_row + head * a.q_head;
+            if (a.q_vec) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(q[e]));
+                for (int c = 0; c < D / 8; ++c)
+                    raw[c] = 8 * c < a.g.dim ? *reinterpret_cast<const uint4 *>(from + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+            } else {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    uint16_t e[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) e[k] = 8 * c < a.g.dim ? from[8 * c + k] : static_cast<uint16_t>(0);
+                    raw[c] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                }
             }
+            // the largest magnitude: 16-bit floats without their signs are ordered as integers
+            uint32_t big = 0u;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                big = __vmaxu2(big, __vmaxu2(raw[c].x & 0x7fff7fffu, raw[c].y & 0x7fff7fffu));
+                big = __vmaxu2(big, __vmaxu2(raw[c].z & 0x7fff7fffu, raw[c].w & 0x7fff7fffu));
+            }
+            const uint32_t most = max(big & 0xffffu, big >> 16);
             float down, up;
-            q_powers(big, down, up);
+            q_powers(a.half ? __half2float(__ushort_as_half(static_cast<unsigned short>(most))) : __uint_as_float(most << 16), down, up);
             mult = up * a.scale2;
             uint8_t *row = sq + i * F::Q_BYTES + tid * 128;
-#pragma unroll 4
-            for (int c8 = 0; c8 < D / 8; ++c8) {
-                float q[8];
-                load_q8(a, sv.row0 + qi, head, 8 * c8, q);
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (on) {
-                    v.x = pack_f16(q[0] * down, q[1] * down);
-                    v.y = pack_f16(q[2] * down, q[3] * down);
-                    v.z = pack_f16(q[4] * down, q[5] * down);
-                    v.w = pack_f16(q[6] * down, q[7] * down);
+            auto scaled = [&](uint32_t w) {
+                float x, y;
+                if (a.half) {
+                    const __half2 h = *reinterpret_cast<const __half2 *>(&w);
+                    x = __low2float(h);
+                    y = __high2float(h);
+                } else {
+                    x = __uint_as_float(w << 16);
+                    y = __uint_as_float(w & 0xffff0000u);
                 }
-                *reinterpret_cast<uint4 *>(row + (c8 >> 3) * (kTile * 128) + (((c8 & 7) ^ (tid & 7)) << 4)) = v;
-            }
+                return on ? pack_f16(x * down, y * down) : 0u;
+            };
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c)
+                *reinterpret_cast<uint4 *>(row + (c >> 3) * (kTile * 128) + (((c & 7) ^ (tid & 7)) << 4)) =
+                    make_uint4(scaled(raw[c].x), scaled(raw[c].y), scaled(raw[c].z), scaled(raw[c].w));
             fence_async_smem();
         }
         mbar_arrive(q_full);
         float m = kFloor, l = 0.0f;
-        bool ok = true;                                   // once false the remaining waits return at once
-        for (int j = 0; i < tiles && j < steps; ++j) {
-            ok = wait_warp(&s_full[i], j & 1u) && ok;
+        for (int u = 0; i < tiles && u < halves; ++u) {
+            const int j = u >> 1;
+            ok = wait_warp(&s_full[2 * i + (u & 1)], j & 1u) && ok;
             tc_fence_after();
-            // (the products of this step have read K, so what came with it is there)
+            // (the products of this round have read K, so what came with it is there)
             const StepInfo &in = info[j % kInfos];
-            const int j0 = begin + j * kTile;
-            const unsigned gone = in.gone_bits();
-            const bool edge = gone != 0u || j0 < all_lo || j0 + kTile > all_hi;
-            // bit e: the row sees token e of the 32 from 32 c on
-            auto seen = [&](int c) {
-                const int t0 = j0 + 32 * c, from = max(see_lo - t0, 0), upto = min(see_hi - t0, 32);
-                unsigned bits = from < 32 ? 0xffffffffu << from : 0u;
-                bits &= upto > 0 ? 0xffffffffu >> (32 - upto) : 0u;
-                if ((gone >> (2 * c)) & 1u) bits &= 0xffff0000u;
-                if ((gone >> (2 * c)) & 2u) bits &= 0x0000ffffu;
-                return bits;
-            };
-            auto hide = [](float (&v)[32], unsigned bits) {
-                asm volatile("" ::: "memory");            // a branch around this, not selects on every step
+            const int j0 = begin + u * kHalf, c0 = 2 * (u & 1);
+            const unsigned gone = (in.gone_bits() >> (2 * c0)) & 15u;
+            const uint32_t ts = lanes + (u & 1) * kHalf;
+            float v[64];
+            tmem_ld_x64(ts, v);
+            if (gone != 0u || j0 < all_lo || j0 + kHalf > all_hi) {
+                asm volatile("" ::: "memory");            // a branch around this, not selects on every round
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    if (!((bits >> e) & 1u)) v[e] = -CUDART_INF_F;
-            };
+                for (int c = 0; c < 2; ++c) {
+                    // bit e: the row sees token e of the 32 from 32 c on
+                    const int t0 = j0 + 32 * c, from = max(see_lo - t0, 0), upto = min(see_hi - t0, 32);
+                    unsigned bits = from < 32 ? 0xffffffffu << from : 0u;
+                    bits &= upto > 0 ? 0xffffffffu >> (32 - upto) : 0u;
+                    if ((gone >> (2 * c)) & 1u) bits &= 0xffff0000u;
+                    if ((gone >> (2 * c)) & 2u) bits &= 0x0000ffffu;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!((bits >> e) & 1u)) v[32 * c + e] = -CUDART_INF_F;
+                }
+            }
             float top = kFloor;
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                float v[32];
-                tmem_ld_32x32b_x32(ts + 32 * c, v);
-                if (edge) hide(v, seen(c));
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
                 float x[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] = fmaxf(v[q], v[q + 4]);
+                for (int q = 0; q < 4; ++q) x[q] = fmaxf(v[32 * c + q], v[32 * c + q + 4]);
 #pragma unroll
                 for (int e = 8; e < 32; e += 8)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[e + q], v[e + q + 4]));
-                top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c], in.val_exp[c]));
+                    for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[32 * c + e + q], v[32 * c + e + q + 4]));
+                top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c0 + c], in.val_exp[c0 + c]));
             }
             if (__any_sync(0xffffffffu, top > m + kRaise)) {
-                const float u = fmaxf(m, top), f = ex2(m - u);
-                m = u;
+                const float w = fmaxf(m, top), f = ex2(m - w);
+                m = w;
                 l *= f;
-                if (j > 0) {
-                    ok = wait_warp(&pv_done[i], (j - 1) & 1u) && ok;
+                if (u > 0) {
+                    ok = wait_warp(&pv_done[2 * i + ((u - 1) & 1)], ((u - 1) >> 1) & 1u) && ok;
                     tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        float v[32];
-                        tmem_ld_32x32b_x32(to + 32 * c, v);
+                    for (int c = 0; c < D / 16; ++c) {
+                        float o[16];
+                        tmem_ld_x16(to + 16 * c, o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] *= f;
-                        tmem_st_x32(to + 32 * c, v);
+                        for (int e = 0; e < 16; ++e) o[e] *= f;
+                        tmem_st_x16(to + 16 * c, o);
                     }
                 }
             }
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                float v[32];
-                tmem_ld_32x32b_x32(ts + 32 * c, v);
-                const uint64_t k = twice(mult * in.key_up[c]), b = twice(in.val_exp[c] - m);
+            uint32_t h[32];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) fma2(v[e], v[e + 1], k, b);
-                if (edge) hide(v, seen(c));
+            for (int c = 0; c < 2; ++c) {
+                const uint64_t k = twice(mult * in.key_up[c0 + c]), b = twice(in.val_exp[c0 + c] - m);
                 uint64_t sum[4] = {0, 0, 0, 0};
-                uint32_t h[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
+                for (int e = 32 * c; e < 32 * c + 32; e += 2) {
+                    fma2(v[e], v[e + 1], k, b);
                     v[e] = ex2(v[e]);
                     v[e + 1] = ex2(v[e + 1]);
                     add2(sum[(e >> 1) & 3], v[e], v[e + 1]);
                     h[e >> 1] = pack_f16(v[e], v[e + 1]);
                 }
-                l = fmaf(total(sum), in.val_down[c], l);
-                tmem_st_x16(ts + 16 * c, h);              // columns whose scores this thread has read
+                l = fmaf(total(sum), in.val_down[c0 + c], l);
             }
+            tmem_st_x32(ts, h);
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&p_full[i]);
+            mbar_arrive(&p_full[2 * i + (u & 1)]);
         }
-        if (i < tiles && steps > 0) {
-            ok = wait_warp(&pv_done[i], (steps - 1) & 1u) && ok;
+        if (i < tiles && halves > 0) {
+            ok = wait_warp(&pv_done[2 * i + ((halves - 1) & 1)], ((halves - 1) >> 1) & 1u) && ok;
             tc_fence_after();
             if (!ok && lane == 0) give_up();
         }
@@ -580,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 float v[32];
-                if (steps > 0) {
+                if (halves > 0) {
                     tmem_ld_32x32b_x32(to + 32 * c, v);
                 } else {
 #pragma unroll
@@ -653,6 +744,12 @@ cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) 
     static const cudaError_t once =
         cudaFuncSetAttribute(k_attend_tiles<C, GC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM_ASKED);
     if (once != cudaSuccess) return once;
+    // the warps' shares of the registers add up only if the kernel was given what it counts on
+    static const bool enough = [] {
+        cudaFuncAttributes at{};
+        return cudaFuncGetAttributes(&at, k_attend_tiles<C, GC>) == cudaSuccess && at.numRegs >= kLaunchRegs;
+    }();
+    if (!enough) return cudaErrorLaunchOutOfResources;
     k_attend_tiles<C, GC><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
     return cudaGetLastError();
 }
