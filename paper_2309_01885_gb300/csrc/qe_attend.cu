@@ -849,7 +849,7 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
     a.o_head = o_head;
     a.half = dtype == QE_F16;
     a.q_vec = (reinterpret_cast<uintptr_t>(Q) & 15u) == 0 && q_row % 8 == 0 && q_head % 8 == 0;
-    a.o_vec = (reinterpret_cast<uintptr_t>(out) & 7u) == 0 && o_row % 4 == 0 && o_head % 4 == 0;
+    a.o_vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && o_row % 8 == 0 && o_head % 8 == 0;
     a.lse = lse;
     a.err = device_error_word();
     if (!a.err) return QE_ERR_CUDA;

@@ -20,7 +20,7 @@ struct AttendArgs {
     void *out;
     int64_t q_row, q_head, o_row, o_head;   // strides in elements
     int half;                 // 1 = fp16, 0 = bf16
-    int q_vec, o_vec;         // 16-byte loads of Q, 8-byte stores of out are aligned
+    int q_vec, o_vec;         // 16-byte loads of Q, stores of out are aligned
     float *lse;               // [rows][q_heads], natural log, or NULL
     int rows_cap;             // (query row, head) pairs that an item of work holds
     int ctas;                 // workers among which the units are dealt out

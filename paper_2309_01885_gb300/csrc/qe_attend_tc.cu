@@ -535,52 +535,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         const int all_lo = __reduce_max_sync(0xffffffffu, see_lo), all_hi = __reduce_min_sync(0xffffffffu, see_hi);
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = lanes + 2 * kTile;
         bool ok = true;                                   // once false the remaining waits return at once
-        // Q: scaled into fp16 by a power of two of the row
+        // Q: the warp's 32 rows, LR lanes to a row, scaled into fp16 by a power of two of the row
+        constexpr int LR = D <= 64 ? 8 : 16, RI = 32 / LR;
+        const int64_t q_at = (sv.row0 + qi) * a.q_row + head * a.q_head;
         float mult = 0.0f;
         if (i < tiles && halves > 0) {
-            uint4 raw[D / 8];
-            const uint16_t *from = reinterpret_cast<const uint16_t *>(a.Q) + (sv.row0 + qi) * a.q_row + head * a.q_head;
-            if (a.q_vec) {
+            const int sub = lane / LR, c = lane % LR;     // row of the RI at once, 16-byte chunk of the row
+            uint4 raw[LR];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c)
-                    raw[c] = 8 * c < a.g.dim ? *reinterpret_cast<const uint4 *>(from + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
-            } else {
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    uint16_t e[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) e[k] = 8 * c < a.g.dim ? from[8 * c + k] : static_cast<uint16_t>(0);
-                    raw[c] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-                }
+            for (int r = 0; r < LR; ++r) {
+                const int64_t at = __shfl_sync(0xffffffffu, q_at, r * RI + sub);
+                const bool mine = i * kTile + quad * 32 + r * RI + sub < rows && 8 * c < a.g.dim;
+                const uint16_t *from = reinterpret_cast<const uint16_t *>(a.Q) + at + 8 * c;
+                raw[r] = make_uint4(0u, 0u, 0u, 0u);
+                if (mine && a.q_vec) raw[r] = *reinterpret_cast<const uint4 *>(from);
+                else if (mine)
+                    raw[r] = make_uint4(from[0] | from[1] << 16, from[2] | from[3] << 16, from[4] | from[5] << 16, from[6] | from[7] << 16);
             }
-            // the largest magnitude: 16-bit floats without their signs are ordered as integers
-            uint32_t big = 0u;
+            uint8_t *tile = sq + i * F::Q_BYTES + (c >> 3) * (kTile * 128);
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                big = __vmaxu2(big, __vmaxu2(raw[c].x & 0x7fff7fffu, raw[c].y & 0x7fff7fffu));
-                big = __vmaxu2(big, __vmaxu2(raw[c].z & 0x7fff7fffu, raw[c].w & 0x7fff7fffu));
+            for (int r = 0; r < LR; ++r) {
+                const int row = quad * 32 + r * RI + sub;
+                // the largest magnitude: 16-bit floats without their signs are ordered as integers
+                uint32_t big = __vmaxu2(__vmaxu2(raw[r].x & 0x7fff7fffu, raw[r].y & 0x7fff7fffu), __vmaxu2(raw[r].z & 0x7fff7fffu, raw[r].w & 0x7fff7fffu));
+#pragma unroll
+                for (int o = 1; o < LR; o <<= 1) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, o));
+                const uint32_t most = max(big & 0xffffu, big >> 16);
+                float down, up;
+                q_powers(a.half ? __half2float(__ushort_as_half(static_cast<unsigned short>(most))) : __uint_as_float(most << 16), down, up);
+                const float back = __shfl_sync(0xffffffffu, up, (lane % RI) * LR);   // the row that this lane owns, if among these
+                if (lane / RI == r) mult = back * a.scale2;
+                auto scaled = [&](uint32_t w) {
+                    float x, y;
+                    if (a.half) {
+                        const __half2 h = *reinterpret_cast<const __half2 *>(&w);
+                        x = __low2float(h);
+                        y = __high2float(h);
+                    } else {
+                        x = __uint_as_float(w << 16);
+                        y = __uint_as_float(w & 0xffff0000u);
+                    }
+                    return pack_f16(x * down, y * down);
+                };
+                if (8 * c < F::DQ)
+                    *reinterpret_cast<uint4 *>(tile + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+                        make_uint4(scaled(raw[r].x), scaled(raw[r].y), scaled(raw[r].z), scaled(raw[r].w));
             }
-            const uint32_t most = max(big & 0xffffu, big >> 16);
-            float down, up;
-            q_powers(a.half ? __half2float(__ushort_as_half(static_cast<unsigned short>(most))) : __uint_as_float(most << 16), down, up);
-            mult = up * a.scale2;
-            uint8_t *row = sq + i * F::Q_BYTES + tid * 128;
-            auto scaled = [&](uint32_t w) {
-                float x, y;
-                if (a.half) {
-                    const __half2 h = *reinterpret_cast<const __half2 *>(&w);
-                    x = __low2float(h);
-                    y = __high2float(h);
-                } else {
-                    x = __uint_as_float(w << 16);
-                    y = __uint_as_float(w & 0xffff0000u);
-                }
-                return on ? pack_f16(x * down, y * down) : 0u;
-            };
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-                *reinterpret_cast<uint4 *>(row + (c >> 3) * (kTile * 128) + (((c & 7) ^ (tid & 7)) << 4)) =
-                    make_uint4(scaled(raw[c].x), scaled(raw[c].y), scaled(raw[c].z), scaled(raw[c].w));
             fence_async_smem();
         }
         mbar_arrive(q_full);
@@ -668,6 +668,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         if (i < tiles) {
             float *slot = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * (2 * kTile * (D + 2)) +
                           static_cast<int64_t>(blockIdx.y) * (2 * kTile * (D + 2));
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees nothing is zero; NaN stays
+            // whole rows go through shared memory (every product has been taken, Q's place is free) and out
+            // LR lanes to a row: a thread's own row would be 8 to 16 bytes a line in each store
+            uint8_t *stage = sq + i * F::Q_BYTES + quad * 32 * (F::DQ * 2);
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 float v[32];
@@ -677,15 +681,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0.0f;
                 }
-                if (!on) continue;
                 if (pieces > 1) {
+                    if (on)
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4 *>(slot + p * D + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<float4 *>(slot + p * D + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        if (32 * c + e < a.g.dim) finish(a, sv.row0 + qi, head, 32 * c + e, make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), m, l);
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float x = v[e + 2 * k] * inv, y = v[e + 2 * k + 1] * inv;
+                            w[k] = a.half ? pack_f16(x, y) : pack_bf16(x, y);
+                        }
+                        *reinterpret_cast<uint4 *>(stage + lane * (F::DQ * 2) + (((4 * c + e / 8) ^ (lane & (LR - 1))) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+            if (pieces == 1) {
+                if (on && a.lse)
+                    a.lse[(sv.row0 + qi) * a.q_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945309f;
+                __syncwarp();
+                const int64_t o_at = (sv.row0 + qi) * a.o_row + head * a.o_head;
+                const int sub = lane / LR, c = lane % LR;
+#pragma unroll 4
+                for (int r = 0; r < LR; ++r) {
+                    const int row = r * RI + sub;
+                    const int64_t at = __shfl_sync(0xffffffffu, o_at, row);
+                    if (i * kTile + quad * 32 + row >= rows || 8 * c >= a.g.dim) continue;
+                    const uint4 w = *reinterpret_cast<const uint4 *>(stage + row * (F::DQ * 2) + ((c ^ (row & (LR - 1))) << 4));
+                    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + at + 8 * c;
+                    if (a.o_vec) {
+                        *reinterpret_cast<uint4 *>(dst) = w;
+                    } else {
+                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[k] = static_cast<uint16_t>(u[k >> 1] >> (16 * (k & 1)));
+                    }
                 }
             }
             if (on && pieces > 1) {
