@@ -372,7 +372,8 @@ qe_status qe_hard_threshold(const float *T, int64_t N, int64_t s, int64_t *idx, 
  *   page_size   a power of two, 16 .. 65536.
  *   head_dim    a multiple of 8 up to 128 (held as 64, 96 or 128 channels).
  *   group_size  32, 64 or 128, a divisor of the channels held.
- * Other values of these three are QE_ERR_UNSUPPORTED.
+ * Other values of these three, and pages of 2 GiB or more (all heads together),
+ * are QE_ERR_UNSUPPORTED.
  */
 typedef struct {
     void *data;
@@ -388,7 +389,7 @@ qe_status qe_cache_size(int64_t pages, int page_size, int kv_heads, int head_dim
  * Quantizes the keys and values of `tokens` tokens into the cache.
  *   K, V     device, token i's head h at K + i * k_token + h * k_head (elements;
  *            channels are contiguous), fp32, bf16 or fp16.  Any strides; where
- *            pointer and strides are multiples of 4 channels the loads are wide.
+ *            pointer and strides are multiples of 16 bytes the loads are wide.
  *   slots    device, int64 per token: where it goes.  A negative slot is skipped
  *            (padding); one past the cache is skipped and latches
  *            QE_ERR_INVALID_ARG.  No two tokens of a call share a slot.

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kWarps * 32, rows_blocks(C, NT)) k_attend_rows
 
     // lanes 0 .. 7 copy a step: keys, values and their grids of its two halves of 16 tokens
     const int part_of = lane & 3, half_of = (lane >> 2) & 1;
-    const int64_t part_off = part_of == 0 ? 0 : part_of == 1 ? cache_v_off(a.g) : part_of == 2 ? cache_kg_off(a.g) : cache_vg_off(a.g);
+    const uint32_t part_off = part_of == 0 ? 0u : part_of == 1 ? a.g.v_off : part_of == 2 ? a.g.kg_off : a.g.vg_off;
     const int tok_bytes = part_of < 2 ? D / 2 : 4 * NG;
     const int part_dst = part_of == 0 ? half_of * F::CODE_BYTES : part_of == 1 ? (2 + half_of) * F::CODE_BYTES
                          : 4 * F::CODE_BYTES + (part_of == 2 ? half_of : 2 + half_of) * F::GRID_BYTES;
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kWarps * 32, rows_blocks(C, NT)) k_attend_rows
         const int my_steps = hi > lo && take > warp ? (take - warp + kWarps - 1) / kWarps : 0;
         const int32_t *table = a.table + at.seq * a.table_ld;
         const uint8_t *mine = a.g.data + kvh * a.g.block_bytes + part_off;
-        const int64_t page_bytes = a.g.kv_heads * a.g.block_bytes;
+        const int64_t page_bytes = a.g.page_bytes;
 
         unsigned gone = 0u;                               // 2 bits a stage: halves whose page id is out of range
         auto page_of = [&](int k) {                       // (halves without a visible token take the nearest one's page)

@@ -305,9 +305,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         // ---- codes to operands ----
         const int32_t *table = a.table + blockIdx.z * a.table_ld;
         const int page_mask = (1 << a.g.page_shift) - 1;
-        const int64_t page_bytes = a.g.kv_heads * a.g.block_bytes;
+        const int64_t page_bytes = a.g.page_bytes;
         const uint8_t *mine = a.g.data + kvh * a.g.block_bytes;
-        const int64_t v_off = cache_v_off(a.g), kg_off = cache_kg_off(a.g), vg_off = cache_vg_off(a.g);
+        const uint32_t v_off = a.g.v_off, kg_off = a.g.kg_off, vg_off = a.g.vg_off;
         // tokens beyond the visible ones take the nearest visible one's place in memory; their grids are dropped
         auto near = [&](int tok) { return max(lo, min(tok, hi - 1)); };
         auto block_of = [&](int page, bool &out) {

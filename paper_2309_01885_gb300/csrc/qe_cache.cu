@@ -1,10 +1,14 @@
 // Writing the 4-bit key/value cache and reading it back (layout: qe_cache.cuh).
 //
-// Both kernels give four channels of a token's head to a lane: a group of G
-// channels is G / 4 neighbouring lanes, whose minimum and maximum meet in
-// shuffles, and a lane's four value codes are one 16-bit half of the layout.
-// They move 2 + 0.5 + 4 / G bytes per 16-bit channel and are bound by HBM.
+// Both kernels give eight channels of a token's head to a lane: 16 bytes of a 16-bit
+// type, one word of key codes, two halves of value codes.  A block takes 16 or 32
+// tokens of the call's list for one head, so that the value words that neighbouring
+// tokens share meet in L1, and two tokens whose slots make a pair exchange halves and
+// move whole words.  A group's minimum and maximum meet in shuffles.  Bound by HBM: 2 +
+// 0.5 + 4 / G bytes for each 16-bit channel.
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "qe_cache.cuh"
 #include "qe_internal.h"
@@ -25,204 +29,355 @@ qe_status cache_geom(const qe_cache *c, CacheGeom *g) {
     g->D = cache_padded(c->head_dim);
     g->group_shift = 31 - __builtin_clz(static_cast<unsigned>(c->group_size));
     g->groups = g->D / c->group_size;
-    g->block_bytes = static_cast<int64_t>(g->D + 8 * g->groups) * c->page_size;
+    g->block_bytes = static_cast<uint32_t>(g->D + 8 * g->groups) * static_cast<uint32_t>(c->page_size);
+    g->page_bytes = g->block_bytes * static_cast<uint32_t>(c->kv_heads);
+    g->v_off = static_cast<uint32_t>(g->D / 2) << g->page_shift;
+    g->kg_off = static_cast<uint32_t>(g->D) << g->page_shift;
+    g->vg_off = static_cast<uint32_t>(g->D + 4 * g->groups) << g->page_shift;
     return QE_OK;
 }
 
 namespace {
 
 template <typename T>
-__device__ __forceinline__ float to_f32(T v) { return static_cast<float>(v); }
-
-// Four neighbouring channels; `vec`: the address is aligned to them.
-template <typename T>
-__device__ __forceinline__ void load4(const T *p, bool vec, int n, float (&v)[4]) {
-    if (vec && n >= 4) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 t = *reinterpret_cast<const float4 *>(p);
-            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-        } else {
-            union { uint2 u; T e[4]; } t;
-            t.u = *reinterpret_cast<const uint2 *>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = to_f32(t.e[i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
-    }
-}
-
-template <typename T>
 __device__ __forceinline__ T from_f32(float v);
 template <>
 __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
+// Eight neighbouring channels and their extremes with 0; `vec`: 16-byte accesses are aligned.
 template <typename T>
-__device__ __forceinline__ void store4(T *p, bool vec, int n, const float (&v)[4]) {
-    if (vec && n >= 4) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-            union { uint2 u; T e[4]; } t;
+__device__ __forceinline__ void load8(const T *p, bool vec, float (&v)[8], float &lo, float &hi) {
+    union { uint4 u[sizeof(T) / 2]; T e[8]; } t;
+    if (vec) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t.e[i] = from_f32<T>(v[i]);
-            *reinterpret_cast<uint2 *>(p) = t.u;
-        }
+        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) t.u[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = from_f32<T>(v[i]);
+        for (int i = 0; i < 8; ++i) t.e[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(t.e[i]);
+    if constexpr (sizeof(T) == 2) {                       // two at a time
+        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const T2 *e = reinterpret_cast<const T2 *>(t.e);
+        const T2 a = __hmin2(__hmin2(e[0], e[1]), __hmin2(e[2], e[3])), b = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
+        lo = fminf(0.0f, fminf(static_cast<float>(a.x), static_cast<float>(a.y)));
+        hi = fmaxf(0.0f, fmaxf(static_cast<float>(b.x), static_cast<float>(b.y)));
+    } else {
+        lo = hi = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            lo = fminf(lo, v[i]);
+            hi = fmaxf(hi, v[i]);
+        }
     }
 }
 
-// The grid of a group whose channels lie in 2^steps neighbouring lanes (four each).
-__device__ __forceinline__ void group_grid(const float (&x)[4], int lanes, float &s, float &z) {
-    float lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
-    float hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+template <typename T>
+__device__ __forceinline__ void store8(T *p, bool vec, const T (&v)[8]) {
+    union { uint4 u[sizeof(T) / 2]; T e[8]; } t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.e[i] = v[i];
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = t.u[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = t.e[i];
+    }
+}
+
+// round(x / s), ties to even, left in the low bits of a sum with 1.5 2^23 (whose addition rounds so).
+//
+// x / s is taken as q = x (1 / s), at most 3 units in the last place off, which only matters next to a midpoint h
+// between two integers.  With 16-bit x, x and s h are both multiples of 2^-13 of their size (11 bits of x; 8 of s
+// times 5 of 2 h): x / s is h itself or at least 2^-14 away, and rounding q to multiples of 2^-16 first (as the sum
+// with 192 does) puts it on h in the one case and leaves it on its side in the other.  Binary32 x are divided
+// where q lies next to a midpoint.
+constexpr float kRound = 12582912.0f;
+template <typename T, int N>
+__device__ __forceinline__ void rounded(const float (&x)[N], float s, float (&t)[N]) {
+    const float inv = __frcp_rn(s);                       // s >= 2^-126: at most 2^126
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = __fadd_rn(__fmaf_rn(x[i], inv, 192.0f), kRound - 192.0f);
+    } else {
+        float off = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float q = x[i] * inv;
+            t[i] = __fadd_rn(q, kRound);
+            off = fmaxf(off, fabsf(q - __fsub_rn(t[i], kRound)));
+        }
+        if (off > 0.49999f)
+#pragma unroll
+            for (int i = 0; i < N; ++i) t[i] = __fadd_rn(__fdiv_rn(x[i], s), kRound);
+    }
+}
+
+// clamp(round(x / s) + z, 0, 15) for eight channels, code i at bit shift(i).  No code falls below 0: z is
+// round(-lo / s), and rounding keeps order and sign.
+template <typename T, typename Shift>
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float z, Shift shift) {
+    float t[8];
+    rounded<T>(x, s, t);
+    uint32_t w = 0u, base = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w += __float_as_uint(fminf(__fadd_rn(t[i], z), kRound + 15.0f)) << shift(i);
+        base += 0x4B400000u << shift(i);
+    }
+    return w - base;
+}
+
+// The grid of a group whose channels lie in `lanes` neighbouring lanes (eight each), from the lane's own extremes.
+template <typename T>
+__device__ __forceinline__ void group_grid(float lo, float hi, int lanes, float &s, float &z) {
     for (int o = 1; o < lanes; o <<= 1) {
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    lo = fminf(lo, 0.0f);
-    hi = fmaxf(hi, 0.0f);
     const float r = __fdiv_rn(__fsub_rn(hi, lo), 15.0f);
     s = fmaxf(__bfloat162float(__float2bfloat16_rn(r)), 1.17549435e-38f);
-    z = rintf(__fdiv_rn(fabsf(lo), s));
+    const float x[1] = {-lo};
+    float t[1];
+    rounded<T>(x, s, t);
+    z = __fsub_rn(t[0], kRound);
 }
 
-__device__ __forceinline__ uint32_t nearest_code(float x, float s, float z) {
-    const float c = rintf(__fdiv_rn(x, s)) + z;
-    return static_cast<uint32_t>(fminf(fmaxf(c, 0.0f), 15.0f));
+// Eight channels' s (c - z), rounded once to T, from pairs of codes at bits 0 and 16 of p[0 .. 3]; c - z is exact.
+template <typename T>
+__device__ __forceinline__ void values8(const uint32_t (&p)[4], uint32_t grid, T (&out)[8]) {
+    const float s = __uint_as_float(grid & 0xFFFF0000u), z = __uint_as_float(grid << 16);
+    if constexpr (sizeof(T) == 2 && !std::is_same<T, __half>::value) {
+        // the scale is a bf16 number: one product in bf16 rounds as the definition does
+        const __nv_bfloat162 s2 = __float2bfloat162_rn(s), z2 = __float2bfloat162_rn(z + 128.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = p[i] | 0x43004300u;        // 128 + c
+            const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&w), z2), s2);
+            out[2 * i] = v.x;
+            out[2 * i + 1] = v.y;
+        }
+    } else {
+        const __half2 z2 = __float2half2_rn(z + 1024.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = p[i] | 0x64006400u;        // 1024 + c
+            const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&w), z2);
+            out[2 * i] = from_f32<T>(s * __low2float(d));
+            out[2 * i + 1] = from_f32<T>(s * __high2float(d));
+        }
+    }
 }
 
 struct CacheIo {
     CacheGeom g;
     const int64_t *slots;
-    int64_t tokens;
+    uint32_t tokens;
     int64_t k_token, k_head, v_token, v_head;   // strides in elements
     int k_vec, v_vec;
     unsigned *err;
 };
 
-// One item = one token's kv head; D / 4 lanes of a warp (half a warp for D = 64).
-template <typename T>
-__global__ void __launch_bounds__(256) k_cache_append(const CacheIo a, const T *K, const T *V) {
-    const CacheGeom &g = a.g;
-    const int lane = threadIdx.x & 31;
-    const int per = g.D == 64 ? 2 : 1;                       // items of a warp
-    const int sub = per == 2 ? lane >> 4 : 0;
-    const int l = per == 2 ? lane & 15 : lane;               // quad of channels 4 l .. 4 l + 3
-    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
-    const int64_t items = a.tokens * g.kv_heads;
-    const int64_t item = warp * per + sub;
-    if (warp * per >= items) return;                         // uniform in the warp
-    const int64_t tok = item / g.kv_heads;
-    const int head = static_cast<int>(item - tok * g.kv_heads);
-    bool live = item < items && 4 * l < g.D;
-    const int64_t slot = item < items ? a.slots[tok] : -1;
-    const int64_t page = slot >> g.page_shift;
-    if (slot < 0) live = false;
-    else if (page >= g.pages) {
-        live = false;
-        if (l == 0) set_error(a.err, ERR_RANGE);
-    }
-    float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (live && 4 * l < g.dim) {
-        load4(K + tok * a.k_token + head * a.k_head + 4 * l, a.k_vec != 0, g.dim - 4 * l, k);
-        load4(V + tok * a.v_token + head * a.v_head + 4 * l, a.v_vec != 0, g.dim - 4 * l, v);
-    }
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        bad = bad || !(fabsf(k[i]) <= kCacheMaxAbs) || !(fabsf(v[i]) <= kCacheMaxAbs);
-    const unsigned votes = __ballot_sync(0xffffffffu, bad);
-    bad = ((per == 2 ? (votes >> (16 * sub)) & 0xffffu : votes) != 0u);
-    if (bad) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) k[i] = v[i] = 0.0f;
-        if (l == 0 && live) set_error(a.err, ERR_NUMERIC);
-    }
-    const int lanes = 1 << (g.group_shift - 2);              // lanes of a group
-    float ks, kz, vs, vz;
-    group_grid(k, lanes, ks, kz);
-    group_grid(v, lanes, vs, vz);
-    uint32_t kw = 0u, vw = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        kw |= nearest_code(k[i], ks, kz) << (4 * ((i >> 1) + 2 * (l & 1)) + 16 * (i & 1));
-        vw |= nearest_code(v[i], vs, vz) << (4 * i);
-    }
-    kw |= __shfl_xor_sync(0xffffffffu, kw, 1);
-    if (!live) return;
-    const int C = g.D >> 5, w = l >> 3;
-    const int64_t at = slot & ((static_cast<int64_t>(1) << g.page_shift) - 1);
-    uint8_t *blk = g.data + (page * g.kv_heads + head) * g.block_bytes;
-    const int64_t b8 = (at >> 3) * (4 * g.D);                // bytes of the 8-token blocks before
-    const int j = static_cast<int>(at & 7);
-    if ((l & 1) == 0)
-        *reinterpret_cast<uint32_t *>(blk + b8 + 4 * ((4 * j + ((l & 7) >> 1)) * C + w)) = kw;
-    *reinterpret_cast<uint16_t *>(blk + cache_v_off(g) + b8 + 4 * ((4 * (l & 7) + (j >> 1)) * C + w) + 2 * (j & 1)) =
-        static_cast<uint16_t>(vw);
-    if ((l & (lanes - 1)) == 0) {
-        const int64_t word = at * g.groups + (l >> (g.group_shift - 2));
-        reinterpret_cast<uint32_t *>(blk + cache_kg_off(g))[word] =
-            bad ? kBadKeyGrid : __float_as_uint(ks) | (__float_as_uint(kz) >> 16);
-        reinterpret_cast<uint32_t *>(blk + cache_vg_off(g))[word] =
-            bad ? kBadValueGrid : __float_as_uint(vs) | (__float_as_uint(vz) >> 16);
-    }
+// Lanes of a token's head, and tokens of a block of 256 threads.
+template <int D>
+struct IoCfg {
+    static constexpr int LANES = D <= 64 ? 8 : 16, TOKENS = 256 / LANES;
+};
+
+// A block's head and a lane's eight channels of it; the block takes PER tokens a lane.
+struct Lane {
+    uint32_t head, c8, tok;   // tok: the first
+    uint8_t *base;            // this head's block of page 0
+};
+
+template <int D, int PER>
+__device__ __forceinline__ Lane io_lane(const CacheIo &a) {
+    using F = IoCfg<D>;
+    Lane l;
+    const unsigned heads = static_cast<unsigned>(a.g.kv_heads), tile = blockIdx.x / heads;
+    l.head = blockIdx.x - tile * heads;
+    l.c8 = threadIdx.x % F::LANES;
+    l.tok = tile * (F::TOKENS * PER) + threadIdx.x / F::LANES;
+    l.base = a.g.data + l.head * a.g.block_bytes;
+    return l;
 }
 
-__device__ __forceinline__ float grid_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ __forceinline__ float grid_zero(uint32_t w) { return __uint_as_float(w << 16); }
+// Where a token's head lies.
+struct Cell {
+    int64_t slot;
+    bool live;                // a token of the list, with a slot in the cache
+    uint8_t *blk;             // its page's block of this head
+    uint32_t at;              // position in the page
+};
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_cache_read(const CacheIo a, T *K, T *V) {
+__device__ __forceinline__ Cell io_cell(const CacheIo &a, const Lane &l, uint32_t tok) {
+    Cell c;
+    c.slot = tok < a.tokens ? a.slots[tok] : -1;
+    const int64_t page = c.slot >> a.g.page_shift;
+    c.live = c.slot >= 0 && page < a.g.pages;
+    if (c.slot >= 0 && !c.live && l.c8 == 0) set_error(a.err, ERR_RANGE);
+    c.blk = l.base + (c.live ? static_cast<uint64_t>(static_cast<uint32_t>(page)) * a.g.page_bytes : 0);
+    c.at = static_cast<uint32_t>(c.slot) & ((1u << a.g.page_shift) - 1u);
+    return c;
+}
+
+// Whether the token and the one LANES lanes away make a pair of neighbouring slots (even, odd): both lanes agree.
+template <int LANES>
+__device__ __forceinline__ bool paired(const Cell &c) {
+    const int64_t other = __shfl_xor_sync(0xffffffffu, c.live ? c.slot : -1, LANES);
+    return c.live && other >= 0 && other == (c.slot ^ 1) && ((threadIdx.x & LANES) != 0) == ((c.slot & 1) != 0);
+}
+
+template <int D, int PER, typename T>
+__global__ void __launch_bounds__(256) k_cache_append(const CacheIo a, const T *K, const T *V) {
+    constexpr int LANES = IoCfg<D>::LANES, TOKENS = IoCfg<D>::TOKENS, C = D / 32;
     const CacheGeom &g = a.g;
-    const int lane = threadIdx.x & 31;
-    const int per = g.D == 64 ? 2 : 1;
-    const int l = per == 2 ? lane & 15 : lane;
-    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
-    const int64_t item = warp * per + (per == 2 ? lane >> 4 : 0);
-    if (item >= a.tokens * g.kv_heads || 4 * l >= g.dim) return;
-    const int64_t tok = item / g.kv_heads;
-    const int head = static_cast<int>(item - tok * g.kv_heads);
-    const int64_t slot = a.slots[tok];
-    const int64_t page = slot >> g.page_shift;
-    float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0 && page >= g.pages) {
-        if (l == 0) set_error(a.err, ERR_RANGE);
-    } else if (slot >= 0) {
-        const int C = g.D >> 5, w = l >> 3;
-        const int64_t at = slot & ((static_cast<int64_t>(1) << g.page_shift) - 1);
-        const uint8_t *blk = g.data + (page * g.kv_heads + head) * g.block_bytes;
-        const int64_t b8 = (at >> 3) * (4 * g.D);
-        const int j = static_cast<int>(at & 7);
-        const uint32_t kw =
-            *reinterpret_cast<const uint32_t *>(blk + b8 + 4 * ((4 * j + ((l & 7) >> 1)) * C + w)) >> (8 * (l & 1));
-        const uint32_t vw = *reinterpret_cast<const uint16_t *>(blk + cache_v_off(g) + b8 +
-                                                                4 * ((4 * (l & 7) + (j >> 1)) * C + w) + 2 * (j & 1));
-        const int64_t word = at * g.groups + (l >> (g.group_shift - 2));
-        const uint32_t kg = reinterpret_cast<const uint32_t *>(blk + cache_kg_off(g))[word];
-        uint32_t vg = reinterpret_cast<const uint32_t *>(blk + cache_vg_off(g))[word];
-        if (vg & 0x80000000u) vg = kBadKeyGrid;
-        const float ks = grid_scale(kg), kz = grid_zero(kg), vs = grid_scale(vg), vz = grid_zero(vg);
+    const Lane l = io_lane<D, PER>(a);
+    const bool inside = 8 * l.c8 < D, loads = 8 * l.c8 < static_cast<uint32_t>(g.dim);
+    const T *kp = K + l.tok * a.k_token + l.head * a.k_head + 8 * l.c8, *vp = V + l.tok * a.v_token + l.head * a.v_head + 8 * l.c8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            k[i] = ks * (static_cast<float>((kw >> (4 * (i >> 1) + 16 * (i & 1))) & 15u) - kz);
-            v[i] = vs * (static_cast<float>((vw >> (4 * i)) & 15u) - vz);
+    for (int n = 0; n < PER; ++n, kp += TOKENS * a.k_token, vp += TOKENS * a.v_token) {
+        const Cell c = io_cell(a, l, l.tok + n * TOKENS);
+        float k[8], v[8], k_lo = 0.0f, k_hi = 0.0f, v_lo = 0.0f, v_hi = 0.0f, odd_one = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = v[i] = 0.0f;
+        if (c.live && loads) {
+            load8(kp, a.k_vec != 0, k, k_lo, k_hi);
+            load8(vp, a.v_vec != 0, v, v_lo, v_hi);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd_one = fmaf(k[i], 0.0f, fmaf(v[i], 0.0f, odd_one));   // NaN from a NaN or an infinity on
+        bool bad = !(odd_one == 0.0f) || fmaxf(fmaxf(k_hi, -k_lo), fmaxf(v_hi, -v_lo)) > kCacheMaxAbs;
+        const unsigned votes = __ballot_sync(0xffffffffu, bad) >> (threadIdx.x & 31 & ~(LANES - 1));
+        bad = (votes & ((1u << LANES) - 1u)) != 0u;           // of the token's head
+        if (bad) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k[i] = v[i] = 0.0f;
+            k_lo = k_hi = v_lo = v_hi = 0.0f;
+            if (l.c8 == 0 && c.live) set_error(a.err, ERR_NUMERIC);
+        }
+        const int lanes = 1 << (g.group_shift - 3);           // of a group
+        float ks, kz, vs, vz;
+        group_grid<T>(k_lo, k_hi, lanes, ks, kz);
+        group_grid<T>(v_lo, v_hi, lanes, vs, vz);
+        // channels 8 c8 .. + 7 are word t = c8 % 4 of chunk w = c8 / 4; for values r = 2 t and 2 t + 1
+        const uint32_t kw = codes8<T>(k, ks, kz, [](int i) { return 4 * (i >> 1) + 16 * (i & 1); });
+        const uint32_t vw = codes8<T>(v, vs, vz, [](int i) { return 4 * i; });
+        const bool pair = paired<LANES>(c);
+        // of a pair the even token's lane writes the words of r = 2 t, the odd one's those of 2 t + 1
+        const bool odd = (threadIdx.x & LANES) != 0;
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, odd ? vw & 0xffffu : vw >> 16, LANES);
+        if (!c.live || !inside) continue;
+        const uint32_t w = l.c8 >> 2, t = l.c8 & 3, j = c.at & 7;
+        uint8_t *b8 = c.blk + (c.at >> 3) * (4 * D);          // the 8-token block's key codes
+        *reinterpret_cast<uint32_t *>(b8 + 4 * ((4 * j + t) * C + w)) = kw;
+        uint8_t *vb = b8 + g.v_off;
+        if (pair) {
+            const uint32_t word = odd ? theirs | (vw & 0xffff0000u) : (vw & 0xffffu) | theirs << 16;
+            *reinterpret_cast<uint32_t *>(vb + 4 * ((4 * (2 * t + odd) + (j >> 1)) * C + w)) = word;
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<uint16_t *>(vb + 4 * ((4 * (2 * t + h) + (j >> 1)) * C + w) + 2 * (j & 1)) =
+                    static_cast<uint16_t>(vw >> (16 * h));
+        }
+        if ((l.c8 & (lanes - 1)) == 0) {
+            const uint32_t word = c.at * g.groups + (l.c8 >> (g.group_shift - 3));
+            reinterpret_cast<uint32_t *>(c.blk + g.kg_off)[word] =
+                bad ? kBadKeyGrid : __float_as_uint(ks) | (__float_as_uint(kz) >> 16);
+            reinterpret_cast<uint32_t *>(c.blk + g.vg_off)[word] =
+                bad ? kBadValueGrid : __float_as_uint(vs) | (__float_as_uint(vz) >> 16);
         }
     }
-    if (K) store4(K + tok * a.k_token + head * a.k_head + 4 * l, a.k_vec != 0, g.dim - 4 * l, k);
-    if (V) store4(V + tok * a.v_token + head * a.v_head + 4 * l, a.v_vec != 0, g.dim - 4 * l, v);
 }
 
-bool quads_aligned(const void *p, int64_t s0, int64_t s1, int size) {
-    return (reinterpret_cast<uintptr_t>(p) % (4 * size)) == 0 && s0 % 4 == 0 && s1 % 4 == 0;
+template <int D, int PER, typename T>
+__global__ void __launch_bounds__(256) k_cache_read(const CacheIo a, T *K, T *V) {
+    constexpr int LANES = IoCfg<D>::LANES, TOKENS = IoCfg<D>::TOKENS, C = D / 32;
+    const CacheGeom &g = a.g;
+    const Lane l = io_lane<D, PER>(a);
+    const bool inside = 8 * l.c8 < D;
+    T *kto = K + l.tok * a.k_token + l.head * a.k_head + 8 * l.c8, *vto = V + l.tok * a.v_token + l.head * a.v_head + 8 * l.c8;
+#pragma unroll
+    for (int n = 0; n < PER; ++n, kto += TOKENS * a.k_token, vto += TOKENS * a.v_token) {
+        const Cell c = io_cell(a, l, l.tok + n * TOKENS);
+        const bool pair = paired<LANES>(c), odd = (threadIdx.x & LANES) != 0;
+        const uint32_t w = l.c8 >> 2, t = l.c8 & 3, j = c.at & 7;
+        uint32_t kw = 0u, vw = 0u, kg = 0u, vg = 0u;
+        if (c.live && inside) {
+            const uint8_t *b8 = c.blk + (c.at >> 3) * (4 * D);
+            kw = *reinterpret_cast<const uint32_t *>(b8 + 4 * ((4 * j + t) * C + w));
+            const uint8_t *vb = b8 + g.v_off;
+            if (pair) {
+                vw = *reinterpret_cast<const uint32_t *>(vb + 4 * ((4 * (2 * t + odd) + (j >> 1)) * C + w));
+            } else {
+                vw = *reinterpret_cast<const uint16_t *>(vb + 4 * (8 * t + (j >> 1)) * C + 4 * w + 2 * (j & 1));
+                vw |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(vb + 4 * (8 * t + 4 + (j >> 1)) * C + 4 * w + 2 * (j & 1))) << 16;
+            }
+            const uint32_t word = c.at * g.groups + (l.c8 >> (g.group_shift - 3));
+            kg = reinterpret_cast<const uint32_t *>(c.blk + g.kg_off)[word];
+            vg = reinterpret_cast<const uint32_t *>(c.blk + g.vg_off)[word];
+        }
+        // of a pair the even token's lane read r = 2 t of both, the odd one's 2 t + 1: each hands over the other token's half
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, odd ? vw & 0xffffu : vw >> 16, LANES);
+        if (pair) vw = odd ? theirs | (vw & 0xffff0000u) : (vw & 0xffffu) | theirs << 16;
+        if (l.tok + n * TOKENS >= a.tokens || 8 * l.c8 >= static_cast<uint32_t>(g.dim)) continue;
+        if (vg & 0x80000000u) vg = kBadKeyGrid;
+        uint32_t kp[4], vp[4], vh[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            kp[i] = (kw >> (4 * i)) & 0x000f000fu;            // channels 2 i, 2 i + 1
+            vh[i] = (vw >> (4 * i)) & 0x000f000fu;            // channels i, i + 4
+        }
+        vp[0] = __byte_perm(vh[0], vh[1], 0x5410);
+        vp[1] = __byte_perm(vh[2], vh[3], 0x5410);
+        vp[2] = __byte_perm(vh[0], vh[1], 0x7632);
+        vp[3] = __byte_perm(vh[2], vh[3], 0x7632);
+        T k[8], v[8];
+        values8(kp, kg, k);
+        values8(vp, vg, v);
+        if (K) store8(kto, a.k_vec != 0, k);
+        if (V) store8(vto, a.v_vec != 0, v);
+    }
+}
+
+template <int D, int PER, typename T, bool APPEND>
+void launch_one(const CacheIo &io, void *K, void *V, cudaStream_t s) {
+    const unsigned blocks = static_cast<unsigned>(ceil_div(io.tokens, IoCfg<D>::TOKENS * PER) * io.g.kv_heads);
+    if constexpr (APPEND) k_cache_append<D, PER, T><<<blocks, 256, 0, s>>>(io, static_cast<const T *>(K), static_cast<const T *>(V));
+    else k_cache_read<D, PER, T><<<blocks, 256, 0, s>>>(io, static_cast<T *>(K), static_cast<T *>(V));
+}
+
+template <int D, typename T, bool APPEND>
+void launch_per(const CacheIo &io, void *K, void *V, cudaStream_t s) {
+    // four tokens a lane where that still leaves the GPU full (its 1216 blocks of 256): what a lane works out once
+    // is half of what a token costs it
+    if (static_cast<int64_t>(io.tokens) * io.g.kv_heads >= int64_t{4} * 1216 * IoCfg<D>::TOKENS) launch_one<D, 4, T, APPEND>(io, K, V, s);
+    else launch_one<D, 1, T, APPEND>(io, K, V, s);
+}
+
+template <typename T, bool APPEND>
+cudaError_t launch_io(const CacheIo &io, void *K, void *V, cudaStream_t s) {
+    if (io.g.D == 64) launch_per<64, T, APPEND>(io, K, V, s);
+    else if (io.g.D == 96) launch_per<96, T, APPEND>(io, K, V, s);
+    else launch_per<128, T, APPEND>(io, K, V, s);
+    return cudaGetLastError();
+}
+
+template <bool APPEND>
+qe_status launch_dtype(const CacheIo &io, void *K, void *V, qe_dtype dtype, cudaStream_t s) {
+    const cudaError_t e = dtype == QE_F32 ? launch_io<float, APPEND>(io, K, V, s)
+                          : dtype == QE_BF16 ? launch_io<__nv_bfloat16, APPEND>(io, K, V, s)
+                                             : launch_io<__half, APPEND>(io, K, V, s);
+    return e == cudaSuccess ? QE_OK : QE_ERR_CUDA;
+}
+
+bool wide_aligned(const void *p, int64_t s0, int64_t s1, int size) {
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && s0 % (16 / size) == 0 && s1 % (16 / size) == 0;
 }
 
 // Checks that the two calls share; `io` is filled but for the error word.
@@ -233,29 +388,23 @@ qe_status cache_io(const qe_cache *cache, const void *K, int64_t k_token, int64_
     const qe_status st = cache_geom(cache, &io->g);
     if (st != QE_OK) return st;
     if (tokens == 0) return QE_OK;
-    if (tokens > (int64_t{1} << 33) / io->g.kv_heads) return QE_ERR_INVALID_ARG;   // a grid's blocks
+    if (tokens > 0x7fffffff || tokens > (int64_t{1} << 33) / io->g.kv_heads) return QE_ERR_INVALID_ARG;   // a grid's blocks
     const uintptr_t esize = dtype == QE_F32 ? 4 : 2;
     if (!slots || (reinterpret_cast<uintptr_t>(slots) & 7u) != 0 || reinterpret_cast<uintptr_t>(K) % esize != 0 ||
         reinterpret_cast<uintptr_t>(V) % esize != 0)
         return QE_ERR_INVALID_ARG;
     const int size = dtype == QE_F32 ? 4 : 2;
     io->slots = slots;
-    io->tokens = tokens;
+    io->tokens = static_cast<uint32_t>(tokens);
     io->k_token = k_token;
     io->k_head = k_head;
     io->v_token = v_token;
     io->v_head = v_head;
-    io->k_vec = quads_aligned(K, k_token, k_head, size);
-    io->v_vec = quads_aligned(V, v_token, v_head, size);
+    io->k_vec = wide_aligned(K, k_token, k_head, size);
+    io->v_vec = wide_aligned(V, v_token, v_head, size);
     io->err = device_error_word();
     if (!io->err) return QE_ERR_CUDA;
     return QE_OK;
-}
-
-// Blocks of 8 warps over the items.
-unsigned item_blocks(const CacheIo &io) {
-    const int64_t warps = ceil_div(io.tokens * io.g.kv_heads, io.g.D == 64 ? 2 : 1);
-    return static_cast<unsigned>(ceil_div(warps, 8));
 }
 
 }  // namespace
@@ -273,7 +422,7 @@ qe_status qe_cache_size(int64_t pages, int page_size, int kv_heads, int head_dim
     if ((group_size != 32 && group_size != 64 && group_size != 128) || D % group_size != 0) return QE_ERR_UNSUPPORTED;
     if (kv_heads > 65535 || pages > 0x7fffffff) return QE_ERR_INVALID_ARG;
     const uint64_t block = static_cast<uint64_t>(D + 8 * (D / group_size)) * static_cast<uint64_t>(page_size);
-    if (static_cast<uint64_t>(pages) > (static_cast<uint64_t>(1) << 62) / (block * kv_heads)) return QE_ERR_INVALID_ARG;
+    if (block * kv_heads >= (static_cast<uint64_t>(1) << 31)) return QE_ERR_UNSUPPORTED;
     *bytes = static_cast<size_t>(static_cast<uint64_t>(pages) * kv_heads * block);
     return QE_OK;
 }
@@ -285,16 +434,7 @@ qe_status qe_cache_append(const qe_cache *cache, const void *K, int64_t k_token,
     if (tokens > 0 && (!K || !V)) return QE_ERR_INVALID_ARG;
     const qe_status st = cache_io(cache, K, k_token, k_head, V, v_token, v_head, dtype, slots, tokens, &io);
     if (st != QE_OK || tokens == 0) return st;
-    const unsigned blocks = item_blocks(io);
-    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == QE_F32)
-        k_cache_append<float><<<blocks, 256, 0, s>>>(io, static_cast<const float *>(K), static_cast<const float *>(V));
-    else if (dtype == QE_BF16)
-        k_cache_append<__nv_bfloat16><<<blocks, 256, 0, s>>>(io, static_cast<const __nv_bfloat16 *>(K),
-                                                             static_cast<const __nv_bfloat16 *>(V));
-    else
-        k_cache_append<__half><<<blocks, 256, 0, s>>>(io, static_cast<const __half *>(K), static_cast<const __half *>(V));
-    return cudaGetLastError() == cudaSuccess ? QE_OK : QE_ERR_CUDA;
+    return launch_dtype<true>(io, const_cast<void *>(K), const_cast<void *>(V), dtype, reinterpret_cast<cudaStream_t>(stream));
 }
 
 qe_status qe_cache_read(const qe_cache *cache, const int64_t *slots, int64_t tokens, void *K, int64_t k_token,
@@ -303,16 +443,7 @@ qe_status qe_cache_read(const qe_cache *cache, const int64_t *slots, int64_t tok
     if (tokens > 0 && !K && !V) return QE_ERR_INVALID_ARG;
     const qe_status st = cache_io(cache, K, k_token, k_head, V, v_token, v_head, dtype, slots, tokens, &io);
     if (st != QE_OK || tokens == 0) return st;
-    const unsigned blocks = item_blocks(io);
-    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (dtype == QE_F32)
-        k_cache_read<float><<<blocks, 256, 0, s>>>(io, static_cast<float *>(K), static_cast<float *>(V));
-    else if (dtype == QE_BF16)
-        k_cache_read<__nv_bfloat16><<<blocks, 256, 0, s>>>(io, static_cast<__nv_bfloat16 *>(K),
-                                                           static_cast<__nv_bfloat16 *>(V));
-    else
-        k_cache_read<__half><<<blocks, 256, 0, s>>>(io, static_cast<__half *>(K), static_cast<__half *>(V));
-    return cudaGetLastError() == cudaSuccess ? QE_OK : QE_ERR_CUDA;
+    return launch_dtype<false>(io, K, V, dtype, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

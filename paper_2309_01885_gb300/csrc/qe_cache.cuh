@@ -32,7 +32,9 @@ constexpr float kCacheMaxAbs = 8.5070592e37f;     // 2^126: larger magnitudes co
 struct CacheGeom {
     uint8_t *data;
     int64_t pages;
-    int64_t block_bytes;      // one page of one kv head
+    uint32_t block_bytes;     // one page of one kv head
+    uint32_t page_bytes;      // one page: offsets inside it fit in 32 bits
+    uint32_t v_off, kg_off, vg_off;   // parts of a block: value codes, key grids, value grids
     int page_shift;           // log2(page_size)
     int kv_heads;
     int dim;                  // channels of a head
@@ -42,17 +44,6 @@ struct CacheGeom {
 };
 
 __host__ __device__ inline int cache_padded(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
-
-// Byte offsets inside a block.
-__host__ __device__ __forceinline__ int64_t cache_v_off(const CacheGeom &g) {
-    return static_cast<int64_t>(g.D / 2) << g.page_shift;
-}
-__host__ __device__ __forceinline__ int64_t cache_kg_off(const CacheGeom &g) {
-    return static_cast<int64_t>(g.D) << g.page_shift;
-}
-__host__ __device__ __forceinline__ int64_t cache_vg_off(const CacheGeom &g) {
-    return static_cast<int64_t>(g.D + 4 * g.groups) << g.page_shift;
-}
 
 // Checks a qe_cache and fills the geometry; QE_ERR_INVALID_ARG / QE_ERR_UNSUPPORTED otherwise.
 qe_status cache_geom(const qe_cache *cache, CacheGeom *g);
