@@ -26,7 +26,8 @@ LIB = os.path.join(OUT_DIR, "libqe.so")
 SOURCES = ["qe_sweep_seq256.cu", "qe_sweep_chg256.cu", "qe_sweep_rows256.cu", "qe_sweep_seq256r.cu",
            "qe_sweep_chg.cu", "qe_sweep_rows.cu", "qe_sweep_seq.cu", "qe_gemm.cu", "qe_api.cu", "qe_cd.cu",
            "qe_outlier.cu", "qe_noalloc.cu", "qe_stream.cu", "qe_pack.cu", "qe_select.cu",
-           "qe_cache.cu", "qe_attend.cu", "qe_attend_tc.cu"]
+           "qe_cache.cu", "qe_attend.cu", "qe_attend_whole8.cu", "qe_attend_whole4.cu",
+           "qe_attend_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
               f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}"]

@@ -163,6 +163,9 @@ __device__ __forceinline__ int64_t worker_units(const AttendArgs &a, int64_t tot
 
 // few query rows per kv head: `tiles` x 8 pairs an item; then the items that workers share are joined
 cudaError_t launch_attend_rows(const AttendArgs &a, int tiles, cudaStream_t s);
+// the same with a CTA (of 8 or 4 warps) for each item
+cudaError_t launch_attend_whole8(const AttendArgs &a, int tiles, cudaStream_t s);
+cudaError_t launch_attend_whole4(const AttendArgs &a, int tiles, cudaStream_t s);
 constexpr int kRowsUnit = 32;
 
 // many query rows per kv head: tiles of 128 rows on the tensor cores

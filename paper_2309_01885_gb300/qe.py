@@ -401,6 +401,8 @@ def qe_quantize_layer_outlier(W: torch.Tensor, Sigma: torch.Tensor, bits: int, i
 
 # ---- the key/value cache in 4 bits ------------------------------------------------------------
 
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _CACHE_DTYPES = {torch.float32: QE_F32, torch.bfloat16: QE_BF16, torch.float16: QE_F16}
 
 
@@ -425,21 +427,22 @@ class KVCache:
         self.pages, self.page_size, self.kv_heads = pages, page_size, kv_heads
         self.head_dim, self.group_size, self.data, self.device = head_dim, group_size, data, data.device
         self._c = QECache(data.data_ptr(), data.numel(), pages, page_size, kv_heads, head_dim, group_size)
-        self._ref = ctypes.addressof(self._c)
+        self._ref, self._index = ctypes.addressof(self._c), data.get_device()
 
 
 def _cache_heads(cache: KVCache, t: torch.Tensor, heads: int, what: str):
     """Strides (row, head) of a rows x heads x head_dim tensor on the cache's device."""
     shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim or (stride[2] != 1 and shape[2] != 1):
+    if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim or stride[2] != 1:
         raise ValueError(f"{what}: expected rows x {heads} x {cache.head_dim} with contiguous channels")
-    if t.device != cache.device:
+    if t.get_device() != cache._index:
         raise ValueError(f"{what}: not on the cache's device")
     return stride[0], stride[1]
 
 
-def _cache_index(cache: KVCache, t: torch.Tensor, dtype: torch.dtype, dims: int, what: str):
-    if t.dtype != dtype or t.dim() != dims or t.device != cache.device or t.stride(-1) != 1:
+def _cache_index(cache: KVCache, t: torch.Tensor, dtype: torch.dtype, dims: int, what: str) -> int:
+    """Address of an index tensor, contiguous along its last axis."""
+    if t.dtype is not dtype or t.get_device() != cache._index or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{what}: expected a {dims}-dimensional {dtype} tensor on the cache's device, contiguous along its last axis")
     return t.data_ptr()
 
@@ -451,19 +454,16 @@ def _cache_dtype(t) -> int:
     return d
 
 
-def _raw_stream(device, stream) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
-
-
 def qe_cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """Quantize keys and values (tokens x kv_heads x head_dim, any row and head strides) into the
     cache's `slots` (int64 per token: page * page_size + position in the page; negative = skip)."""
-    ks, vs = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
-    n = slots.shape[0]
-    if k.shape[0] != n or v.shape[0] != n or k.dtype != v.dtype:
+    at = _cache_index(cache, slots, torch.int64, 1, "slots")
+    (k0, k1), (v0, v1) = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
+    n, dtype = slots.shape[0], k.dtype
+    if k.shape[0] != n or v.shape[0] != n or v.dtype is not dtype:
         raise ValueError("k, v and slots hold the same tokens, k and v the same dtype")
-    st = load().qe_cache_append(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _cache_dtype(k.dtype),
-                                _cache_index(cache, slots, torch.int64, 1, "slots"), n, _raw_stream(cache.device, stream))
+    st = (_lib or load()).qe_cache_append(cache._ref, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, _cache_dtype(dtype), at, n,
+                                          _raw_stream(cache._index) if stream is None else stream.cuda_stream)
     if st != QE_OK:
         raise QEError(st, "qe_cache_append")
 
@@ -472,24 +472,32 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
                   v: torch.Tensor | None = None, stream=None) -> tuple:
     """(keys, values) of the cache's `slots`, tokens x kv_heads x head_dim, rounded once to `dtype`;
     written into `k` and `v` where given (any row and head strides)."""
-    n = slots.shape[0]
+    at = _cache_index(cache, slots, torch.int64, 1, "slots")
+    n, heads, dim = slots.shape[0], cache.kv_heads, cache.head_dim
+    k0, k1, v0, v1 = heads * dim, dim, heads * dim, dim
     if k is None:
-        k = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device)
+        k = torch.empty((n, heads, dim), dtype=dtype, device=cache.device)
+    else:
+        k0, k1 = _cache_heads(cache, k, heads, "k")
+        if k.shape[0] != n or k.dtype is not dtype:
+            raise ValueError("k holds the tokens of slots, in dtype")
     if v is None:
-        v = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device)
-    ks, vs = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
-    if k.shape[0] != n or v.shape[0] != n or k.dtype != dtype or v.dtype != dtype:
-        raise ValueError("k and v hold the tokens of slots, in dtype")
-    st = load().qe_cache_read(cache._ref, _cache_index(cache, slots, torch.int64, 1, "slots"), n, k.data_ptr(), ks[0],
-                              ks[1], v.data_ptr(), vs[0], vs[1], _cache_dtype(dtype), _raw_stream(cache.device, stream))
+        v = torch.empty((n, heads, dim), dtype=dtype, device=cache.device)
+    else:
+        v0, v1 = _cache_heads(cache, v, heads, "v")
+        if v.shape[0] != n or v.dtype is not dtype:
+            raise ValueError("v holds the tokens of slots, in dtype")
+    st = (_lib or load()).qe_cache_read(cache._ref, at, n, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, _cache_dtype(dtype),
+                                        _raw_stream(cache._index) if stream is None else stream.cuda_stream)
     if st != QE_OK:
         raise QEError(st, "qe_cache_read")
     return k, v
 
 
-def qe_cache_attention_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int) -> int:
-    """Bytes of workspace qe_cache_attention takes for such a batch."""
-    at = QEAttention(seqs=seqs, rows=rows, q_heads=q_heads, causal=1, max_q=max_q, max_kv=max_kv)
+def qe_cache_attention_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int, *,
+                                 causal: bool = True, window: int = 0) -> int:
+    """Bytes of workspace qe_cache_attention takes for such a batch (a call without the window never takes less)."""
+    at = QEAttention(seqs=seqs, rows=rows, q_heads=q_heads, causal=causal, window=window, max_q=max_q, max_kv=max_kv)
     n = ctypes.c_size_t(0)
     _check(load().qe_cache_attention_workspace(cache._ref, ctypes.addressof(at), ctypes.byref(n)),
            "qe_cache_attention_workspace")
@@ -506,26 +514,33 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
     max_q rows; max_kv is about the longest kv_len.  causal / window (0 = none) / scale (0 = 1 /
     sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x q_heads, written.  workspace: optional
     uint8 tensor of qe_cache_attention_workspace() bytes."""
-    rows, heads = q.shape[0], q.shape[1]
-    qs = _cache_heads(cache, q, heads, "q")
-    if out is None:
-        out = torch.empty(rows, heads, cache.head_dim, dtype=q.dtype, device=cache.device)
-    os_ = _cache_heads(cache, out, heads, "out")
-    if out.dtype != q.dtype or out.shape[0] != rows:
-        raise ValueError("out has q's shape and dtype")
-    seqs = kv_len.shape[0]
+    rows, heads, dim = q.shape
+    q0, q1 = _cache_heads(cache, q, heads, "q")
+    seqs, dtype = kv_len.shape[0], q.dtype
     if q_start.shape[0] != seqs + 1 or page_table.shape[0] != seqs:
         raise ValueError("q_start holds seqs + 1 values, page_table seqs rows")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()):
-        raise ValueError("lse: expected a contiguous fp32 tensor, rows x q_heads")
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=dtype, device=cache.device)
+        o0, o1 = heads * dim, dim
+    else:
+        o0, o1 = _cache_heads(cache, out, heads, "out")
+        if out.dtype is not dtype or out.shape[0] != rows:
+            raise ValueError("out has q's shape and dtype")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()
+                            or lse.get_device() != cache._index):
+        raise ValueError("lse: expected a contiguous fp32 tensor on the cache's device, rows x q_heads")
     at = QEAttention(seqs, rows, heads, causal, window, scale, max_q, max_kv,
                      _cache_index(cache, q_start, torch.int32, 1, "q_start"),
                      _cache_index(cache, kv_len, torch.int32, 1, "kv_len"),
                      _cache_index(cache, page_table, torch.int32, 2, "page_table"), page_table.stride(0))
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    st = load().qe_cache_attention(cache._ref, ctypes.addressof(at), q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0],
-                                   os_[1], _cache_dtype(q.dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
-                                   _raw_stream(cache.device, stream))
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.get_device() != cache._index or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the cache's device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = (_lib or load()).qe_cache_attention(cache._ref, ctypes.addressof(at), q.data_ptr(), q0, q1, out.data_ptr(), o0, o1,
+                                             _cache_dtype(dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
+                                             _raw_stream(cache._index) if stream is None else stream.cuda_stream)
     if st != QE_OK:
         raise QEError(st, "qe_cache_attention")
     return out
