@@ -15,6 +15,9 @@
 //          are scaled by a power of two into fp16's range (exact but for values
 //          2^-39 below the row's largest).
 //   values O^T[channel][row] = V^T P^T with c - z, exact in the same subnormals, and
+//          P^T's fragment times the scale in fp16, 2^-12 relative: P is rounded before and
+//          the product again, which bf16 results do not show; for fp16 ones P's rounding
+//          is carried along, so that one is left.
 //          P^T's fragment times the scale in fp16 (twice rounded, 2^-12 relative each).
 // Grids are turned into what the fragments want once per step by the whole warp and
 // read back from shared memory: four lanes of a quad would each do it otherwise.
@@ -66,6 +69,11 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+    const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&c));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
     const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&v);
@@ -112,8 +120,9 @@ struct RowsCfg {
     static constexpr int SMEM = kWarps * WARP_BYTES + kWarps * STAGES * 8 + (kWarps * 32 + 1) * 8;
 };
 
+// HALF: fp16 queries and results, bf16 otherwise.
 // WHOLE: block x takes item x whole (items numbered by the longest sequence), nothing is dealt out or joined.
-template <int C, int GC, int NT, int kWarps, bool WHOLE>
+template <int C, int GC, int NT, int kWarps, bool WHOLE, bool HALF>
 __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k_attend_rows(const AttendArgs a) {
     using F = RowsCfg<C, GC, NT, kWarps>;
     constexpr int D = F::D, NG = F::NG, STAGES = F::STAGES;
@@ -432,7 +441,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                         }
                     }
                 }
-                uint32_t pf[NT][2];
+                uint32_t pf[NT][2], pl[NT][2];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -440,8 +449,15 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                         x[n][e] = ex2(x[n][e] - m[n][e & 1]);
                         l[n][e & 1] += x[n][e];
                     }
-                    pf[n][0] = movmatrix_trans(pack_f16(x[n][0], x[n][1]));
-                    pf[n][1] = movmatrix_trans(pack_f16(x[n][2], x[n][3]));
+                    pf[n][0] = pack_f16(x[n][0], x[n][1]);
+                    pf[n][1] = pack_f16(x[n][2], x[n][3]);
+                    if constexpr (HALF) {                 // what the rounding left out
+                        const __half2 h0 = *reinterpret_cast<const __half2 *>(&pf[n][0]), h1 = *reinterpret_cast<const __half2 *>(&pf[n][1]);
+                        pl[n][0] = movmatrix_trans(pack_f16(x[n][0] - __low2float(h0), x[n][1] - __high2float(h0)));
+                        pl[n][1] = movmatrix_trans(pack_f16(x[n][2] - __low2float(h1), x[n][3] - __high2float(h1)));
+                    }
+                    pf[n][0] = movmatrix_trans(pf[n][0]);
+                    pf[n][1] = movmatrix_trans(pf[n][1]);
                 }
                 // ---- O^T[channel][row] += (c - z)^T (P s)^T over tokens 2 t, 2 t + 1 and the same 8 further ----
                 uint32_t w0[C], w1[C], g0[2 * NG], g1[2 * NG];
@@ -456,8 +472,13 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                     uint32_t ps[NT][2];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        ps[n][0] = mul_f16x2(pf[n][0], g0[2 * g]);
-                        ps[n][1] = mul_f16x2(pf[n][1], g1[2 * g]);
+                        if constexpr (HALF) {
+                            ps[n][0] = fma_f16x2(pf[n][0], g0[2 * g], mul_f16x2(pl[n][0], g0[2 * g]));
+                            ps[n][1] = fma_f16x2(pf[n][1], g1[2 * g], mul_f16x2(pl[n][1], g1[2 * g]));
+                        } else {
+                            ps[n][0] = mul_f16x2(pf[n][0], g0[2 * g]);
+                            ps[n][1] = mul_f16x2(pf[n][1], g1[2 * g]);
+                        }
                     }
                     const uint32_t z0 = g0[2 * g + 1], z1 = g1[2 * g + 1];
                     const uint32_t y0 = mul_f16x2(z0, 0x4C004C00u), y1 = mul_f16x2(z1, 0x4C004C00u);   // 16 z
@@ -556,14 +577,19 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
     }
 }
 
-template <int C, int GC, int NT, int W, bool WHOLE>
-cudaError_t launch_rows(const AttendArgs &a, cudaStream_t s) {
+template <int C, int GC, int NT, int W, bool WHOLE, bool HALF>
+cudaError_t launch_rows_as(const AttendArgs &a, cudaStream_t s) {
     using F = RowsCfg<C, GC, NT, W>;
     static const cudaError_t once =
-        cudaFuncSetAttribute(k_attend_rows<C, GC, NT, W, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM);
+        cudaFuncSetAttribute(k_attend_rows<C, GC, NT, W, WHOLE, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM);
     if (once != cudaSuccess) return once;
-    k_attend_rows<C, GC, NT, W, WHOLE><<<static_cast<unsigned>(WHOLE ? a.items : a.ctas), W * 32, F::SMEM, s>>>(a);
+    k_attend_rows<C, GC, NT, W, WHOLE, HALF><<<static_cast<unsigned>(WHOLE ? a.items : a.ctas), W * 32, F::SMEM, s>>>(a);
     return cudaGetLastError();
+}
+
+template <int C, int GC, int NT, int W, bool WHOLE>
+cudaError_t launch_rows(const AttendArgs &a, cudaStream_t s) {
+    return a.half ? launch_rows_as<C, GC, NT, W, WHOLE, true>(a, s) : launch_rows_as<C, GC, NT, W, WHOLE, false>(a, s);
 }
 
 template <int C, int GC, int W, bool WHOLE>
