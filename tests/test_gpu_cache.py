@@ -460,3 +460,17 @@ def test_long_context_in_pieces():
     """A context long enough for many pieces, in one page as a cache without paging has it."""
     b = Batch([1, 2], [65535, 40000], 4, 2, 64, 64, 65536, torch.float16, seed=24)
     check(b, torch.float16)
+
+
+def test_example_runs_end_to_end():
+    """The example layer: quantized projections, prompts, then single tokens.  With 8-bit weights what is left is
+    mostly the 4-bit keys and values: half a step of a sixteenth of the range each, some 5 per cent of their size."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "quantized_attention.py")
+    spec = importlib.util.spec_from_file_location("quantized_attention", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    coarse, fine = mod.run(bits=3), mod.run(bits=8)
+    assert fine["prompt"] < 0.2 and fine["step"] < 0.2
+    assert fine["prompt"] < coarse["prompt"] and fine["step"] < coarse["step"]
