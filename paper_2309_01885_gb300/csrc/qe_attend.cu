@@ -183,23 +183,28 @@ int sm_count() {
     return n;
 }
 
-constexpr int64_t kFewPairs = 32;         // (query row, head) pairs of a kv head up to which the row kernel takes a call
+// (query row, head) pairs of a kv head up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles):
+// 64 channels, 29 pairs 63 / 92; 128 channels, 20 pairs 82 / 97, 32 pairs 64 / 57.
+constexpr int64_t few_pairs(int D) { return D <= 64 ? 32 : 24; }
 
 AttendPlan attend_plan(const CacheGeom &g, const qe_attention &at) {
     const int64_t seqs = at.seqs, max_q = at.max_q, max_kv = at.max_kv, window = at.causal ? at.window : 0;
     const int q_heads = at.q_heads;
     AttendPlan p;
     const int64_t pairs = max_q * (q_heads / g.kv_heads);
+    const int64_t span = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;   // most that a row sees
     p.splits = 1;
     p.warps = 0;
-    if (pairs > kFewPairs) {
+    if (pairs > few_pairs(g.D)) {
         p.tiles = 0;
         p.rows_cap = 256;
         p.items = seqs * ceil_div(pairs, 256) * g.kv_heads;
         p.ctas = 0;
         p.min_units = 4;
-        const int64_t steps = ceil_div(max_kv, 128), want = sm_count() / p.items;
-        const int64_t most = steps / p.min_units;
+        // pieces of an item, each a CTA, while all of them fit one wave: 4 items of 53000 tokens 36 us.  Cutting for a
+        // second wave as well does not pay where lengths differ: 160 items of 1000 .. 8000 tokens 150 us whole, 169 in
+        // two pieces (of 8000 each: 295 and 267)
+        const int64_t want = sm_count() / p.items, most = ceil_div(span, 128) / p.min_units;
         p.splits = static_cast<int>(want < most ? want : most);
         if (p.splits < 1) p.splits = 1;
         return p;
@@ -212,7 +217,6 @@ AttendPlan attend_plan(const CacheGeom &g, const qe_attention &at) {
     // short contexts: a CTA for each item saves the dealing out and the joining.  Measured (32 heads of 128, us,
     // dealt out / CTAs of 8 warps / of 4): 32 items of 513 tokens 15.6 / 8.5 / 10.0, 128 of 1000 .. 2000 21.5 /
     // 16.3 / 21.5, 512 of up to 1024 35 / 34 / 23, 2048 of 300 .. 600 59 / 103 / 70
-    const int64_t span = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;
     p.warps = items <= 152 && span <= 2048 ? 8 : items <= 1216 && span <= 1088 ? 4 : 0;
     if (p.warps > 0) {
         p.ctas = 1;
