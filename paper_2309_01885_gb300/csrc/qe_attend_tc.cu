@@ -36,11 +36,8 @@ namespace {
 
 constexpr int kTile = 128;                // rows of a tile, tokens of a step
 constexpr int kHalf = 64;                 // tokens of a softmax round
-constexpr int kThreads = 640;             // the last three warps only lend their registers
-constexpr int kKeyWarp = 8, kValWarp = 12, kMmaWarp = 16;
-// registers a thread: at launch, then softmax, turning and the rest (256 x 128 + 256 x 80 + 128 x 64 = 640 x 96)
-constexpr int kLaunchRegs = 96, kSoftRegs = 128, kTurnRegs = 80, kRestRegs = 64;
-static_assert(256 * kSoftRegs + 256 * kTurnRegs + 128 * kRestRegs <= kThreads * kLaunchRegs, "more registers asked for than launched with");
+constexpr int kThreads = 896;             // the last three warps have no part in it
+constexpr int kKeyWarp = 16, kValWarp = 20, kMmaWarp = 24;
 constexpr int kInfos = 4;                // the turning warps are at most two steps ahead of softmax
 
 // Issued by one elected lane of a warp that goes along together, so that addresses stay in
@@ -70,23 +67,6 @@ __device__ __forceinline__ void commit_one(uint32_t bar) {
         "{\n\t.reg .pred q;\n\t"
         "elect.sync _|q, 0xffffffff;\n\t"
         "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-
-// 64 columns of the thread's row.
-__device__ __forceinline__ void tmem_ld_x64(uint32_t taddr, float (&v)[64]) {
-    asm volatile(
-        "{\n\ttcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
-        "tcgen05.wait::ld.sync.aligned;\n\t}"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
-        : "r"(taddr)
         : "memory");
 }
 
@@ -147,11 +127,6 @@ struct StepInfo {
     }
 };
 
-template <int N>
-__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
 template <int C, int GC>
 struct TcCfg {
     static constexpr int D = 32 * C, NG = C / GC, DQ = D <= 64 ? 64 : 128;   // DQ: channels in whole swizzle atoms of 64
@@ -160,7 +135,8 @@ struct TcCfg {
     static constexpr int V_BYTES = D * kTile * 2;
     static constexpr int VPAIRS = 4 * 16 * NG * 8;        // (s, s'), (z, z') of the step's pairs of tokens
     static constexpr int BAR_OFF = 2 * Q_BYTES + 2 * K_BYTES + 2 * V_BYTES + VPAIRS;
-    static constexpr int SMEM = 1024 + BAR_OFF + kInfos * static_cast<int>(sizeof(StepInfo)) + 256;
+    static constexpr int ROW_OFF = BAR_OFF + 20 * 8 + kInfos * static_cast<int>(sizeof(StepInfo));   // floats of the rows
+    static constexpr int SMEM = 1024 + ROW_OFF + 5 * 2 * kTile * 4;
     // one CTA an SM: it takes all of tensor memory
     static constexpr int SMEM_ASKED = SMEM > 120 * 1024 ? SMEM : 120 * 1024;
 };
@@ -175,11 +151,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     uint8_t *sq = smem, *sk = sq + 2 * F::Q_BYTES, *sv_ = sk + 2 * F::K_BYTES, *spairs = sv_ + 2 * F::V_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + F::BAR_OFF);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
-    uint64_t *s_full = bars + 8, *pv_done = bars + 12, *p_full = bars + 16;   // [row tile][round & 1]
-    uint64_t *q_full = bars + 20, *drain = bars + 21;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 22);
+    uint64_t *s_full = bars + 8, *pv_done = bars + 10, *p_full = bars + 12;   // a row tile each; p_full[row tile][half]
+    uint64_t *q_full = bars + 16, *drain = bars + 17;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 18);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    StepInfo *info = reinterpret_cast<StepInfo *>(bars + 24);
+    StepInfo *info = reinterpret_cast<StepInfo *>(bars + 20);
+    // of each row: its multiplier; for either half of a step the greatest score; in the end the sums
+    float *row_mult = reinterpret_cast<float *>(smem + F::ROW_OFF), *row_max = row_mult + 2 * kTile, *row_sum = row_max + 4 * kTile;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -213,13 +191,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             mbar_init(&v_full[s], 128);
             mbar_init(&v_empty[s], 1);
             mbar_init(&s_full[s], 1);
-            mbar_init(&s_full[2 + s], 1);
             mbar_init(&pv_done[s], 1);
-            mbar_init(&pv_done[2 + s], 1);
             mbar_init(&p_full[s], 128);
             mbar_init(&p_full[2 + s], 128);
         }
-        mbar_init(q_full, 256);
+        mbar_init(q_full, 512);
         mbar_init(drain, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -238,57 +214,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         set_error(a.err, ERR_TIMEOUT);
     };
 
-    const int halves = hi > begin ? min(2 * steps, (hi - begin + kHalf - 1) / kHalf) : 0;   // rounds
-
     if (warp >= kMmaWarp) {
-        regs_down<kRestRegs>();
-        if (warp == kMmaWarp && halves > 0) {
+        if (warp == kMmaWarp && steps > 0) {
             const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
-            const int rounds = __shfl_sync(0xffffffffu, halves, 0), row_tiles = __shfl_sync(0xffffffffu, tiles, 0);
+            const int todo = __shfl_sync(0xffffffffu, steps, 0), row_tiles = __shfl_sync(0xffffffffu, tiles, 0);
             const uint32_t bar0 = smem_u32(bars);         // barriers as above, 8 bytes each
             const uint64_t q0 = smem_desc_k128(smem_u32(sq)), k0 = smem_desc_k128(smem_u32(sk)), v0 = smem_desc_k128(smem_u32(sv_));
-            // S_i = Q_i K^T of round u into buffer u & 1 (descriptors count 16-byte units)
-            auto scores = [&](int i, int u) {
-                constexpr uint32_t id = idesc_f16_f32(kTile, kHalf);
-                const uint64_t qa = q0 + i * (F::Q_BYTES / 16), kb = k0 + ((u >> 1) & 1) * (F::K_BYTES / 16) + (u & 1) * (kHalf * 8);
-                const uint32_t d = t0 + i * kTile + (u & 1) * kHalf;
+            // S_i = Q_i K^T of step j (descriptors count 16-byte units)
+            auto scores = [&](int i, int j) {
+                constexpr uint32_t id = idesc_f16_f32(kTile, kTile);
+                const uint64_t qa = q0 + i * (F::Q_BYTES / 16), kb = k0 + (j & 1) * (F::K_BYTES / 16);
+                const uint32_t d = t0 + i * kTile;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     mma_ss_one(d, qa + (k >> 2) * (kTile * 8) + 2 * (k & 3), kb + (k >> 2) * (kTile * 8) + 2 * (k & 3), id, k == 0 ? 0u : 1u);
-                commit_one(bar0 + 8 * (8 + 2 * i + (u & 1)));
+                commit_one(bar0 + 8 * (8 + i));
             };
-            // O_i += P_i V of round u
-            auto values = [&](int i, int u) {
+            // O_i += P_i V of half h of step j
+            auto values = [&](int i, int j, int h) {
                 constexpr uint32_t id = idesc_f16_f32(kTile, D);
-                const uint64_t vb = v0 + ((u >> 1) & 1) * (F::V_BYTES / 16) + (u & 1) * (D * 8);
-                const uint32_t pa = t0 + i * kTile + (u & 1) * kHalf, d = t0 + 2 * kTile + i * kTile;
-                const uint32_t more = u > 0 ? 1u : 0u;
+                const uint64_t vb = v0 + (j & 1) * (F::V_BYTES / 16) + h * (D * 8);
+                const uint32_t pa = t0 + i * kTile + h * kHalf, d = t0 + 2 * kTile + i * kTile;
+                const uint32_t more = j + h > 0 ? 1u : 0u;
 #pragma unroll
                 for (int k = 0; k < kHalf / 16; ++k) mma_ts_one(d, pa + 8 * k, vb + 2 * k, id, k == 0 ? more : 1u);
-                commit_one(bar0 + 8 * (12 + 2 * i + (u & 1)));
             };
             bool ok = wait_warp(q_full, 0u) && wait_warp(&k_full[0], 0u);
             tc_fence_after();
-            for (int u = 0; ok && u < 2 && u < rounds; ++u)
-                for (int i = 0; i < row_tiles; ++i) scores(i, u);
-            if (ok) commit_one(smem_u32(&k_empty[0]));
-            for (int u = 0; ok && u < rounds; ++u) {
-                const int j = u >> 1;
-                if (!(u & 1)) ok = wait_warp(&v_full[j & 1], (j >> 1) & 1u);
+            if (ok) {
+                for (int i = 0; i < row_tiles; ++i) scores(i, 0);
+                commit_one(smem_u32(&k_empty[0]));
+            }
+            for (int j = 0; ok && j < todo; ++j) {
+                ok = wait_warp(&v_full[j & 1], (j >> 1) & 1u);
                 for (int i = 0; ok && i < row_tiles; ++i) {
-                    ok = wait_warp(&p_full[2 * i + (u & 1)], j & 1u);
+                    for (int h = 0; ok && h < 2; ++h) {
+                        ok = wait_warp(&p_full[2 * i + h], j & 1u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(i, j, h);
+                    }
                     if (!ok) break;
-                    tc_fence_after();
-                    values(i, u);
-                    if (u + 2 >= rounds) continue;
-                    if (i == 0 && !(u & 1)) {
+                    if (j + 1 == todo) {
+                        commit_one(bar0 + 8 * (10 + i));
+                        continue;
+                    }
+                    if (i == 0) {
                         ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
                         if (!ok) break;
                         tc_fence_after();
                     }
-                    scores(i, u + 2);
+                    scores(i, j + 1);
                 }
-                if (ok && (u & 1)) {                      // both halves of step j's V, of step j + 1's K have been multiplied
+                if (ok) {                                 // step j's V and step j + 1's K have been multiplied
                     commit_one(smem_u32(&v_empty[j & 1]));
                     commit_one(smem_u32(&k_empty[(j + 1) & 1]));
                 }
@@ -299,7 +277,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             mbar_wait_bounded(drain, 0u, nullptr);
         }
     } else if (warp >= kKeyWarp) {
-        regs_down<kTurnRegs>();
         const bool keys = warp < kValWarp;
         const int tid = threadIdx.x & (kTile - 1), w4 = warp & 3;
         // ---- codes to operands ----
@@ -523,9 +500,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         }
         if (!ok && lane == 0) give_up();
     } else {
-        regs_up<kSoftRegs>();
-        // ---- softmax: a thread a row ----
-        const int i = warp >> 2, quad = warp & 3, tid = threadIdx.x & (kTile - 1);
+        // ---- softmax: a thread a row and half of the step's tokens ----
+        const int grp = warp >> 3, i = (warp >> 2) & 1, quad = warp & 3, tid = threadIdx.x & (kTile - 1);
         const int p = i * kTile + tid;
         const bool on = p < rows;
         const unsigned pr = first + (on ? p : 0), qi = pr / static_cast<unsigned>(a.per_kv);
@@ -538,33 +514,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         // Q: the warp's 32 rows, LR lanes to a row, scaled into fp16 by a power of two of the row
         constexpr int LR = D <= 64 ? 8 : 16, RI = 32 / LR;
         const int64_t q_at = (sv.row0 + qi) * a.q_row + head * a.q_head;
-        float mult = 0.0f;
-        if (i < tiles && halves > 0) {
+        if (i < tiles && steps > 0) {
             const int sub = lane / LR, c = lane % LR;     // row of the RI at once, 16-byte chunk of the row
-            uint4 raw[LR];
+            constexpr int HR = LR / 2;                    // each group brings half of the rows
+            uint4 raw[HR];
 #pragma unroll
-            for (int r = 0; r < LR; ++r) {
+            for (int k = 0; k < HR; ++k) {
+                const int r = grp * HR + k;
                 const int64_t at = __shfl_sync(0xffffffffu, q_at, r * RI + sub);
                 const bool mine = i * kTile + quad * 32 + r * RI + sub < rows && 8 * c < a.g.dim;
                 const uint16_t *from = reinterpret_cast<const uint16_t *>(a.Q) + at + 8 * c;
-                raw[r] = make_uint4(0u, 0u, 0u, 0u);
-                if (mine && a.q_vec) raw[r] = *reinterpret_cast<const uint4 *>(from);
+                raw[k] = make_uint4(0u, 0u, 0u, 0u);
+                if (mine && a.q_vec) raw[k] = *reinterpret_cast<const uint4 *>(from);
                 else if (mine)
-                    raw[r] = make_uint4(from[0] | from[1] << 16, from[2] | from[3] << 16, from[4] | from[5] << 16, from[6] | from[7] << 16);
+                    raw[k] = make_uint4(from[0] | from[1] << 16, from[2] | from[3] << 16, from[4] | from[5] << 16, from[6] | from[7] << 16);
             }
             uint8_t *tile = sq + i * F::Q_BYTES + (c >> 3) * (kTile * 128);
 #pragma unroll
-            for (int r = 0; r < LR; ++r) {
-                const int row = quad * 32 + r * RI + sub;
+            for (int k = 0; k < HR; ++k) {
+                const int row = quad * 32 + (grp * HR + k) * RI + sub;
                 // the largest magnitude: 16-bit floats without their signs are ordered as integers
-                uint32_t big = __vmaxu2(__vmaxu2(raw[r].x & 0x7fff7fffu, raw[r].y & 0x7fff7fffu), __vmaxu2(raw[r].z & 0x7fff7fffu, raw[r].w & 0x7fff7fffu));
+                uint32_t big = __vmaxu2(__vmaxu2(raw[k].x & 0x7fff7fffu, raw[k].y & 0x7fff7fffu), __vmaxu2(raw[k].z & 0x7fff7fffu, raw[k].w & 0x7fff7fffu));
 #pragma unroll
                 for (int o = 1; o < LR; o <<= 1) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, o));
                 const uint32_t most = max(big & 0xffffu, big >> 16);
                 float down, up;
                 q_powers(a.half ? __half2float(__ushort_as_half(static_cast<unsigned short>(most))) : __uint_as_float(most << 16), down, up);
-                const float back = __shfl_sync(0xffffffffu, up, (lane % RI) * LR);   // the row that this lane owns, if among these
-                if (lane / RI == r) mult = back * a.scale2;
+                if (c == 0) row_mult[i * kTile + row] = up * a.scale2;
                 auto scaled = [&](uint32_t w) {
                     float x, y;
                     if (a.half) {
@@ -579,28 +555,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 };
                 if (8 * c < F::DQ)
                     *reinterpret_cast<uint4 *>(tile + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-                        make_uint4(scaled(raw[r].x), scaled(raw[r].y), scaled(raw[r].z), scaled(raw[r].w));
+                        make_uint4(scaled(raw[k].x), scaled(raw[k].y), scaled(raw[k].z), scaled(raw[k].w));
             }
             fence_async_smem();
         }
         mbar_arrive(q_full);
-        float m = kFloor, l = 0.0f;
-        for (int u = 0; i < tiles && u < halves; ++u) {
-            const int j = u >> 1;
-            ok = wait_warp(&s_full[2 * i + (u & 1)], j & 1u) && ok;
+        float m = kFloor, l = 0.0f, mult = 0.0f;
+        for (int j = 0; i < tiles && j < steps; ++j) {
+            ok = wait_warp(&s_full[i], j & 1u) && ok;     // and the products of the step before have been taken
             tc_fence_after();
-            // (the products of this round have read K, so what came with it is there)
+            // (these products have read Q and K, so what came with them is there)
+            if (j == 0) mult = row_mult[p];
             const StepInfo &in = info[j % kInfos];
-            const int j0 = begin + u * kHalf, c0 = 2 * (u & 1);
+            const int j0 = begin + j * kTile + grp * kHalf, c0 = 2 * grp;
             const unsigned gone = (in.gone_bits() >> (2 * c0)) & 15u;
-            const uint32_t ts = lanes + (u & 1) * kHalf;
-            float v[64];
-            tmem_ld_x64(ts, v);
-            if (gone != 0u || j0 < all_lo || j0 + kHalf > all_hi) {
-                asm volatile("" ::: "memory");            // a branch around this, not selects on every round
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    // bit e: the row sees token e of the 32 from 32 c on
+            const uint32_t ts = lanes + grp * kHalf;
+            const bool edge = gone != 0u || j0 < all_lo || j0 + kHalf > all_hi;
+            // the scores of the half's tokens 32 c .. + 31
+            auto fetch = [&](int c, float (&v)[32]) {
+                tmem_ld_32x32b_x32(ts + 32 * c, v);
+                if (edge) {
+                    asm volatile("" ::: "memory");        // a branch around this, not selects in every step
+                    // bit e: the row sees token e of the 32
                     const int t0 = j0 + 32 * c, from = max(see_lo - t0, 0), upto = min(see_hi - t0, 32);
                     unsigned bits = from < 32 ? 0xffffffffu << from : 0u;
                     bits &= upto > 0 ? 0xffffffffu >> (32 - upto) : 0u;
@@ -608,62 +584,78 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     if ((gone >> (2 * c)) & 2u) bits &= 0x0000ffffu;
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (!((bits >> e) & 1u)) v[32 * c + e] = -CUDART_INF_F;
+                        if (!((bits >> e) & 1u)) v[e] = -CUDART_INF_F;
                 }
-            }
-            float top = kFloor;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            };
+            auto highest = [&](int c, const float (&v)[32]) {
                 float x[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] = fmaxf(v[32 * c + q], v[32 * c + q + 4]);
+                for (int q = 0; q < 4; ++q) x[q] = fmaxf(v[q], v[q + 4]);
 #pragma unroll
                 for (int e = 8; e < 32; e += 8)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[32 * c + e + q], v[32 * c + e + q + 4]));
-                top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c0 + c], in.val_exp[c0 + c]));
-            }
+                    for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[e + q], v[e + q + 4]));
+                return fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c0 + c], in.val_exp[c0 + c]);
+            };
+            float v[32];
+            fetch(1, v);
+            float top = fmaxf(kFloor, highest(1, v));
+            fetch(0, v);
+            top = fmaxf(top, highest(0, v));
+            // the other half's, from the other group's warp of these rows
+            row_max[grp * 2 * kTile + p] = top;
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * i + quad) : "memory");
+            top = fmaxf(top, row_max[(1 - grp) * 2 * kTile + p]);
             if (__any_sync(0xffffffffu, top > m + kRaise)) {
-                const float w = fmaxf(m, top), f = ex2(m - w);
-                m = w;
+                const float now = fmaxf(m, top), f = ex2(m - now);
+                m = now;
                 l *= f;
-                if (u > 0) {
-                    ok = wait_warp(&pv_done[2 * i + ((u - 1) & 1)], ((u - 1) >> 1) & 1u) && ok;
-                    tc_fence_after();
+                if (j > 0) {                              // either group has half of the channels
 #pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
+                    for (int c = grp * (D / 32); c < (grp + 1) * (D / 32); ++c) {
                         float o[16];
                         tmem_ld_x16(to + 16 * c, o);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[e] *= f;
                         tmem_st_x16(to + 16 * c, o);
                     }
+                    // a product of either half adds to all channels
+                    tmem_wait_st();
+                    tc_fence_before();
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * i + quad) : "memory");
+                    tc_fence_after();
                 }
             }
-            uint32_t h[32];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
+                if (c == 1) fetch(1, v);
                 const uint64_t k = twice(mult * in.key_up[c0 + c]), b = twice(in.val_exp[c0 + c] - m);
                 uint64_t sum[4] = {0, 0, 0, 0};
+                float h[16];
 #pragma unroll
-                for (int e = 32 * c; e < 32 * c + 32; e += 2) {
+                for (int e = 0; e < 32; e += 2) {
                     fma2(v[e], v[e + 1], k, b);
                     v[e] = ex2(v[e]);
                     v[e + 1] = ex2(v[e + 1]);
                     add2(sum[(e >> 1) & 3], v[e], v[e + 1]);
-                    h[e >> 1] = pack_f16(v[e], v[e + 1]);
+                    h[e >> 1] = __uint_as_float(pack_f16(v[e], v[e + 1]));
                 }
                 l = fmaf(total(sum), in.val_down[c0 + c], l);
+                tmem_st_x16(ts + 16 * c, h);              // in place of scores that have been read
             }
-            tmem_st_x32(ts, h);
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&p_full[2 * i + (u & 1)]);
+            mbar_arrive(&p_full[2 * i + grp]);
         }
-        if (i < tiles && halves > 0) {
-            ok = wait_warp(&pv_done[2 * i + ((halves - 1) & 1)], ((halves - 1) >> 1) & 1u) && ok;
-            tc_fence_after();
-            if (!ok && lane == 0) give_up();
+        if (i < tiles) {
+            row_sum[grp * 2 * kTile + p] = l;
+            asm volatile("bar.sync %0, 256;" ::"r"(9 + i) : "memory");
+            l += row_sum[(1 - grp) * 2 * kTile + p];
+            if (steps > 0) {
+                ok = wait_warp(&pv_done[i], 0u) && ok;
+                tc_fence_after();
+                if (!ok && lane == 0) give_up();
+            }
         }
         if (i < tiles) {
             float *slot = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * (2 * kTile * (D + 2)) +
@@ -673,9 +665,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             // LR lanes to a row: a thread's own row would be 8 to 16 bytes a line in each store
             uint8_t *stage = sq + i * F::Q_BYTES + quad * 32 * (F::DQ * 2);
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = grp; c < D / 32; c += 2) {
                 float v[32];
-                if (halves > 0) {
+                if (steps > 0) {
                     tmem_ld_32x32b_x32(to + 32 * c, v);
                 } else {
 #pragma unroll
@@ -701,13 +693,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 }
             }
             if (pieces == 1) {
-                if (on && a.lse)
+                if (on && a.lse && grp == 0)
                     a.lse[(sv.row0 + qi) * a.q_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945309f;
-                __syncwarp();
+                asm volatile("bar.sync %0, 256;" ::"r"(9 + i) : "memory");
                 const int64_t o_at = (sv.row0 + qi) * a.o_row + head * a.o_head;
                 const int sub = lane / LR, c = lane % LR;
 #pragma unroll 4
-                for (int r = 0; r < LR; ++r) {
+                for (int r = grp * (LR / 2); r < (grp + 1) * (LR / 2); ++r) {
                     const int row = r * RI + sub;
                     const int64_t at = __shfl_sync(0xffffffffu, o_at, row);
                     if (i * kTile + quad * 32 + row >= rows || 8 * c >= a.g.dim) continue;
@@ -722,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     }
                 }
             }
-            if (on && pieces > 1) {
+            if (on && pieces > 1 && grp == 0) {
                 slot[2 * kTile * D + p] = m;
                 slot[2 * kTile * (D + 1) + p] = l;
             }
@@ -778,12 +770,6 @@ cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) 
     static const cudaError_t once =
         cudaFuncSetAttribute(k_attend_tiles<C, GC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM_ASKED);
     if (once != cudaSuccess) return once;
-    // the warps' shares of the registers add up only if the kernel was given what it counts on
-    static const bool enough = [] {
-        cudaFuncAttributes at{};
-        return cudaFuncGetAttributes(&at, k_attend_tiles<C, GC>) == cudaSuccess && at.numRegs >= kLaunchRegs;
-    }();
-    if (!enough) return cudaErrorLaunchOutOfResources;
     k_attend_tiles<C, GC><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
     return cudaGetLastError();
 }
