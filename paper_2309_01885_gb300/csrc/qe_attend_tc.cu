@@ -7,23 +7,27 @@
 // cores' 4 x 128^2 x D products a step and, nearly as much, by issuing what
 // softmax (256 x 128 exponentials) and the turning of 2 x 128 x D codes cost; two
 // row tiles share each turned step.  Roles:
-//   warps 0-3, 4-7   softmax of row tile 0 and 1, a thread a row, 64 tokens a round:
-//                    scores from tensor memory into registers, P back in place of
-//                    the scores as the A operand of the second product;
-//   warps 8-11       key codes to fp16 operands [token][channel] in shared memory
-//                    (128-byte swizzle), warps 12-15 value codes to [channel][token];
+//   warps 0-15       softmax, a thread a row and 64 tokens of the step: warps 0-3 and
+//                    8-11 have row tile 0, 4-7 and 12-15 tile 1.  Scores come from tensor
+//                    memory into registers, P goes back in their place as the A operand
+//                    of the second product;
+//   warps 16-19      key codes to fp16 operands [token][channel] in shared memory
+//                    (128-byte swizzle), warps 20-23 value codes to [channel][token];
 //                    the next step's codes are loaded while the products run;
-//   warp 16          one lane issues the products.  Two score buffers of 64 tokens a
-//                    row tile: the products of one round run while softmax is at the
-//                    next.  (A thread of the softmax warps that issued them itself was
-//                    held 1600 cycles a round by the filled tensor queue.)
-// Registers are dealt out anew at the start: softmax keeps a round's scores in them.
+//   warp 24          issues the products, one tile's while softmax is at the other's.  (A
+//                    thread of the softmax warps that issued them itself was held by the
+//                    filled tensor queue.)
+// What was measured on the way, a causal prompt of 8192 tokens, 32 heads of 128 on 8:
+// scores of 64 tokens a product, two buffers a row tile, four softmax warps a tile 568
+// us (a product of 128 x 64 takes as long as one of 128 x 128); whole steps and eight
+// warps a tile 540; exponentials taken at the old maximum before the new scores' is
+// known 512.
 // Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16,
 // with powers of two for each 32 tokens that bring the largest scale to [1, 2); Q's
 // rows likewise.  2^F and the row's power of two go into the score's multiplier, E
 // into the exponent of P and 2^-E into the row sum, so that no magnitude leaves
-// fp16's range.  The running maximum is raised only when it is exceeded by 2^8, so
-// the accumulator in tensor memory is rarely rescaled.  Sums are fp32.
+// fp16's range.  The running maximum is raised only when a score exceeds it by 8 (a
+// factor of 2^8), so the accumulator in tensor memory is rarely rescaled.  Sums are fp32.
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
@@ -79,12 +83,37 @@ __device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, float (&v)[16]) {
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const float (&v)[16]) {
+template <class T>
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const T (&v)[16]) {
+    static_assert(sizeof(T) == 4, "32 bits a column");
+    uint32_t r[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) memcpy(&r[e], &v[e], 4);
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+// Two warps meet at named barrier `id`.
+__device__ __forceinline__ void sync_64(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+// They meet and learn whether any of them says so.
+__device__ __forceinline__ bool any_of_64(int id, bool mine) {
+    int any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.or.pred p, %2, 64, q;\n\tselp.s32 %0, 1, 0, p;\n\t}"
+        : "=r"(any) : "r"(static_cast<int>(mine)), "r"(id) : "memory");
+    return any != 0;
+}
+
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2 *>(&w); }
 
 // (x, y) * k + b and sums, two at a time
 __device__ __forceinline__ void fma2(float &x, float &y, uint64_t k, uint64_t b) {
@@ -151,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     uint8_t *sq = smem, *sk = sq + 2 * F::Q_BYTES, *sv_ = sk + 2 * F::K_BYTES, *spairs = sv_ + 2 * F::V_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + F::BAR_OFF);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
-    uint64_t *s_full = bars + 8, *pv_done = bars + 10, *p_full = bars + 12;   // a row tile each; p_full[row tile][half]
+    uint64_t *s_full = bars + 8, *pv_done = bars + 10, *p_full = bars + 12;   // a row tile each
     uint64_t *q_full = bars + 16, *drain = bars + 17;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 18);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -186,16 +215,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2; ++s) {
-            mbar_init(&k_full[s], 128);
+            mbar_init(&k_full[s], 4);
             mbar_init(&k_empty[s], 1);
-            mbar_init(&v_full[s], 128);
+            mbar_init(&v_full[s], 4);
             mbar_init(&v_empty[s], 1);
             mbar_init(&s_full[s], 1);
             mbar_init(&pv_done[s], 1);
-            mbar_init(&p_full[s], 128);
-            mbar_init(&p_full[2 + s], 128);
+            mbar_init(&p_full[s], 8);
         }
-        mbar_init(q_full, 512);
+        mbar_init(q_full, 16);
         mbar_init(drain, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -207,7 +235,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     const uint32_t tmem = *tmem_slot;
     // the same answer for the whole warp, whose lanes go on together
     auto wait_warp = [&](uint64_t *bar, unsigned parity) {
-        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag)) != 0;
+        bool there = false;                               // (the clock is read only when it takes long)
+        for (int n = 0; n < 16 && !there; ++n) there = mbar_try_wait(bar, parity);
+        return __all_sync(0xffffffffu, there || mbar_wait_bounded(bar, parity, abort_flag)) != 0;
     };
     auto give_up = [&]() {
         *abort_flag = 1;
@@ -230,14 +260,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     mma_ss_one(d, qa + (k >> 2) * (kTile * 8) + 2 * (k & 3), kb + (k >> 2) * (kTile * 8) + 2 * (k & 3), id, k == 0 ? 0u : 1u);
                 commit_one(bar0 + 8 * (8 + i));
             };
-            // O_i += P_i V of half h of step j
-            auto values = [&](int i, int j, int h) {
+            // O_i += P_i V of step j
+            auto values = [&](int i, int j) {
                 constexpr uint32_t id = idesc_f16_f32(kTile, D);
-                const uint64_t vb = v0 + (j & 1) * (F::V_BYTES / 16) + h * (D * 8);
-                const uint32_t pa = t0 + i * kTile + h * kHalf, d = t0 + 2 * kTile + i * kTile;
-                const uint32_t more = j + h > 0 ? 1u : 0u;
+                const uint64_t vb = v0 + (j & 1) * (F::V_BYTES / 16);
+                const uint32_t pa = t0 + i * kTile, d = t0 + 2 * kTile + i * kTile;
+                const uint32_t more = j > 0 ? 1u : 0u;
 #pragma unroll
-                for (int k = 0; k < kHalf / 16; ++k) mma_ts_one(d, pa + 8 * k, vb + 2 * k, id, k == 0 ? more : 1u);
+                for (int k = 0; k < kTile / 16; ++k)      // either half's P stands where its scores began
+                    mma_ts_one(d, pa + (k >> 2) * kHalf + 8 * (k & 3), vb + (k >> 2) * (D * 8) + 2 * (k & 3), id, k == 0 ? more : 1u);
             };
             bool ok = wait_warp(q_full, 0u) && wait_warp(&k_full[0], 0u);
             tc_fence_after();
@@ -247,24 +278,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             }
             for (int j = 0; ok && j < todo; ++j) {
                 ok = wait_warp(&v_full[j & 1], (j >> 1) & 1u);
+                if (ok && j + 1 < todo) ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
                 for (int i = 0; ok && i < row_tiles; ++i) {
-                    for (int h = 0; ok && h < 2; ++h) {
-                        ok = wait_warp(&p_full[2 * i + h], j & 1u);
-                        if (!ok) break;
-                        tc_fence_after();
-                        values(i, j, h);
-                    }
+                    ok = wait_warp(&p_full[i], j & 1u);
                     if (!ok) break;
-                    if (j + 1 == todo) {
-                        commit_one(bar0 + 8 * (10 + i));
-                        continue;
-                    }
-                    if (i == 0) {
-                        ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
-                    scores(i, j + 1);
+                    tc_fence_after();
+                    values(i, j);
+                    if (j + 1 < todo) scores(i, j + 1);
+                    else commit_one(bar0 + 8 * (10 + i));
                 }
                 if (ok) {                                 // step j's V and step j + 1's K have been multiplied
                     commit_one(smem_u32(&v_empty[j & 1]));
@@ -394,7 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     in.gone[w4] = static_cast<uint8_t>(gone);
                 }
                 fence_async_smem();
-                mbar_arrive(&k_full[s]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&k_full[s]);
                 if (j + 1 < steps) {
                     key_codes(j + 1);
                     value_grids(j + 1);
@@ -490,12 +512,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     }
                 }
                 fence_async_smem();
-                mbar_arrive(&v_full[s]);
+                __syncwarp();                             // also: the pairs are read before the next step's are written
+                if (lane == 0) mbar_arrive(&v_full[s]);
                 if (j + 1 < steps) {
                     codes(j + 1);
                     if (j + 2 < steps) code_page(j + 2);
                 }
-                __syncwarp();                             // the pairs are read before the next step's are written
             }
         }
         if (!ok && lane == 0) give_up();
@@ -559,10 +581,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             }
             fence_async_smem();
         }
-        mbar_arrive(q_full);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full);
         float m = kFloor, l = 0.0f, mult = 0.0f;
         for (int j = 0; i < tiles && j < steps; ++j) {
-            ok = wait_warp(&s_full[i], j & 1u) && ok;     // and the products of the step before have been taken
+            ok = ok && wait_warp(&s_full[i], j & 1u);     // and the products of the step before have been taken
             tc_fence_after();
             // (these products have read Q and K, so what came with them is there)
             if (j == 0) mult = row_mult[p];
@@ -597,16 +620,57 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[e + q], v[e + q + 4]));
                 return fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c0 + c], in.val_exp[c0 + c]);
             };
-            float v[32];
-            fetch(1, v);
-            float top = fmaxf(kFloor, highest(1, v));
-            fetch(0, v);
-            top = fmaxf(top, highest(0, v));
-            // the other half's, from the other group's warp of these rows
-            row_max[grp * 2 * kTile + p] = top;
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * i + quad) : "memory");
-            top = fmaxf(top, row_max[(1 - grp) * 2 * kTile + p]);
-            if (__any_sync(0xffffffffu, top > m + kRaise)) {
+            // exponentials at the maximum so far, packed
+            auto powers = [&](int c, float (&v)[32], uint32_t *h) {
+                const uint64_t k = twice(mult * in.key_up[c0 + c]), b = twice(in.val_exp[c0 + c] - m);
+                uint64_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    fma2(v[e], v[e + 1], k, b);
+                    v[e] = ex2(v[e]);
+                    v[e + 1] = ex2(v[e + 1]);
+                    add2(sum[(e >> 1) & 3], v[e], v[e + 1]);
+                    h[e >> 1] = pack_f16(v[e], v[e + 1]);
+                }
+                return total(sum) * in.val_down[c0 + c];
+            };
+            const int pair_bar = 1 + 4 * i + quad;        // this warp and the other group's warp of these rows
+            bool raise = j == 0;
+            if (j > 0) {
+                // taken at the old maximum at once; only where one exceeds 2^kRaise (seldom) it is all done again
+                uint32_t h[32];
+                float v[32];
+                fetch(0, v);
+                float sum = powers(0, v, h);
+                fetch(1, v);
+                sum += powers(1, v, h + 16);
+                __half2 x[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = __hmax2(as_half2(h[q]), as_half2(h[q + 4]));
+#pragma unroll
+                for (int e = 8; e < 32; e += 4)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[q] = __hmax2(x[q], as_half2(h[e + q]));
+                x[0] = __hmax2(__hmax2(x[0], x[1]), __hmax2(x[2], x[3]));
+                raise = any_of_64(pair_bar, __hgt(__hmax(__low2half(x[0]), __high2half(x[0])), __float2half(256.0f)));
+                if (!raise) {
+                    tmem_st_x32(ts, h);
+                    l += sum;
+                }
+            }
+            if (raise) {
+                asm volatile("" ::: "memory");
+                float top = kFloor;
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    float v[32];
+                    fetch(c, v);
+                    top = fmaxf(top, highest(c, v));
+                }
+                // the other half's, from the other group
+                row_max[grp * 2 * kTile + p] = top;
+                sync_64(pair_bar);
+                top = fmaxf(top, row_max[(1 - grp) * 2 * kTile + p]);
                 const float now = fmaxf(m, top), f = ex2(m - now);
                 m = now;
                 l *= f;
@@ -619,40 +683,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                         for (int e = 0; e < 16; ++e) o[e] *= f;
                         tmem_st_x16(to + 16 * c, o);
                     }
-                    // a product of either half adds to all channels
-                    tmem_wait_st();
-                    tc_fence_before();
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * i + quad) : "memory");
-                    tc_fence_after();
                 }
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (c == 1) fetch(1, v);
-                const uint64_t k = twice(mult * in.key_up[c0 + c]), b = twice(in.val_exp[c0 + c] - m);
-                uint64_t sum[4] = {0, 0, 0, 0};
-                float h[16];
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    fma2(v[e], v[e + 1], k, b);
-                    v[e] = ex2(v[e]);
-                    v[e + 1] = ex2(v[e + 1]);
-                    add2(sum[(e >> 1) & 3], v[e], v[e + 1]);
-                    h[e >> 1] = __uint_as_float(pack_f16(v[e], v[e + 1]));
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    float v[32];
+                    uint32_t h[16];
+                    fetch(c, v);
+                    l += powers(c, v, h);
+                    tmem_st_x16(ts + 16 * c, h);          // in place of scores that have been read
                 }
-                l = fmaf(total(sum), in.val_down[c0 + c], l);
-                tmem_st_x16(ts + 16 * c, h);              // in place of scores that have been read
             }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&p_full[2 * i + grp]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[i]);
         }
         if (i < tiles) {
             row_sum[grp * 2 * kTile + p] = l;
             asm volatile("bar.sync %0, 256;" ::"r"(9 + i) : "memory");
             l += row_sum[(1 - grp) * 2 * kTile + p];
             if (steps > 0) {
-                ok = wait_warp(&pv_done[i], 0u) && ok;
+                ok = ok && wait_warp(&pv_done[i], 0u);
                 tc_fence_after();
                 if (!ok && lane == 0) give_up();
             }
