@@ -18,7 +18,6 @@
 //          P^T's fragment times the scale in fp16, 2^-12 relative: P is rounded before and
 //          the product again, which bf16 results do not show; for fp16 ones P's rounding
 //          is carried along, so that one is left.
-//          P^T's fragment times the scale in fp16 (twice rounded, 2^-12 relative each).
 // Grids are turned into what the fragments want once per step by the whole warp and
 // read back from shared memory: four lanes of a quad would each do it otherwise.
 // Value scales are taken relative to a power of two that is raised when one exceeds it
@@ -31,6 +30,10 @@
 // memory at the end.  The steps of the whole batch are dealt out evenly over one
 // wave of CTAs (ragged lengths, few or many sequences alike), and items that
 // fall to several CTAs are joined by a second kernel.
+// Measured (whole calls, 32 heads of 128 on 8 unless said): 64 single tokens over 1000
+// .. 8191 95 us (4.1 TB/s of cache; moving the bytes alone took 66 .. 75), 2 over 128K 72
+// us (4.1 TB/s), 32 over 4K with 232 heads of 64 on 8 68 us: there softmax and operands of
+// 29 rows a kv head bound it, not memory.
 #pragma once
 
 #include "qe_attend.h"
