@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                 qf[n][w][2] = pack_f16(q[w][4], q[w][5]);
                 qf[n][w][3] = pack_f16(q[w][6] * 0.0625f, q[w][7] * 0.0625f);
             }
-            const float m = a.scale2 * 16777216.0f * up;
+            const float m = fminf(a.scale2 * 16777216.0f * up, 1.70141183e38f);   // (finite: scores may be 0)
             int l0, h0;
             visible(a, sv, i, i, l0, h0);
             all_lo = l0 > all_lo ? l0 : all_lo;

@@ -595,6 +595,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             const unsigned gone = (in.gone_bits() >> (2 * c0)) & 15u;
             const uint32_t ts = lanes + grp * kHalf;
             const bool edge = gone != 0u || j0 < all_lo || j0 + kHalf > all_hi;
+            // what scores of 32 tokens are multiplied with: never 0, as masked ones are -inf by then (all-zero rows and
+            // keys, or a tiny caller's scale, come to 2^-229 and less), never infinite, as some may be 0; a score that
+            // 2^-126 instead of less makes differ is below 2^-80 either way
+            auto factor = [&](int c) { return fminf(fmaxf(mult * in.key_up[c0 + c], 1.17549435e-38f), 1.70141183e38f); };
             // the scores of the half's tokens 32 c .. + 31
             auto fetch = [&](int c, float (&v)[32]) {
                 tmem_ld_32x32b_x32(ts + 32 * c, v);
@@ -619,11 +623,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 for (int e = 8; e < 32; e += 8)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) x[q] = fmaxf(x[q], fmaxf(v[e + q], v[e + q + 4]));
-                return fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), mult * in.key_up[c0 + c], in.val_exp[c0 + c]);
+                return fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), factor(c), in.val_exp[c0 + c]);
             };
             // exponentials at the maximum so far, packed
             auto powers = [&](int c, float (&v)[32], uint32_t *h) {
-                const uint64_t k = twice(mult * in.key_up[c0 + c]), b = twice(in.val_exp[c0 + c] - m);
+                const uint64_t k = twice(factor(c)), b = twice(in.val_exp[c0 + c] - m);
                 uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
