@@ -15,15 +15,17 @@
 //          are scaled by a power of two into fp16's range (exact but for values
 //          2^-39 below the row's largest).
 //   values O^T[channel][row] = V^T P^T with c - z, exact in the same subnormals, and
-//          P^T's fragment times the scale in fp16, 2^-12 relative: P is rounded before and
+//          P^T's fragment times the scale in fp16, 2^-11 relative: P is rounded before and
 //          the product again, which bf16 results do not show; for fp16 ones P's rounding
 //          is carried along, so that one is left.
 // Grids are turned into what the fragments want once per step by the whole warp and
 // read back from shared memory: four lanes of a quad would each do it otherwise.
-// Value scales are taken relative to a power of two that is raised when one exceeds it
-// by 2^7, and the running maximum is raised only when a score exceeds it by 2^8, so
-// both stay in fp16's range and accumulators are rarely rescaled; sums and softmax
-// statistics stay in fp32.
+// Value scales are taken relative to powers of two of their channel groups, whose largest
+// P's exponent takes over, and tokens far from the others' size are added by themselves in
+// fp32 (qe_attend_out.cuh); the running maximum is raised only when score + e exceeds it
+// by 2^8, so accumulators are rarely rescaled.  What a token adds keeps its bits down to
+// 2^-21 of the greatest of its row, less up to 2^-7 for its scales within 2^e_g, and
+// vanishes 2^10 further down.  Sums and softmax statistics are fp32.
 // The 16 x 8 score fragment becomes P^T's fragment by an 8 x 8 transpose in the
 // warp.  A warp walks 32-token steps on its own, fed by bulk copies into a ring of
 // its own; the warps of a CTA take an item's steps in turn and meet in shared
@@ -31,9 +33,10 @@
 // wave of CTAs (ragged lengths, few or many sequences alike), and items that
 // fall to several CTAs are joined by a second kernel.
 // Measured (whole calls, 32 heads of 128 on 8 unless said): 64 single tokens over 1000
-// .. 8191 95 us (4.1 TB/s of cache; moving the bytes alone took 66 .. 75), 2 over 128K 72
-// us (4.1 TB/s), 32 over 4K with 232 heads of 64 on 8 68 us: there softmax and operands of
-// 29 rows a kv head bound it, not memory.
+// .. 8191 98 us (3.9 TB/s of cache; moving the bytes alone took 66 .. 75; with one power of
+// two for all groups and no tokens apart it was 95), 2 over 128K 74 us (4.0 TB/s), 32 over
+// 4K with 232 heads of 64 on 8 70 us: there softmax and operands of 29 rows a kv head bound
+// it, not memory.
 #pragma once
 
 #include "qe_attend.h"
@@ -47,7 +50,6 @@ namespace {
 // warps of one CTA meet and turn to their next item the others of the SM compute (four:
 // 64 single tokens over 1K .. 8K 100 us, two: 92); more where a CTA takes a whole item.
 constexpr int kDealtWarps = 2;
-constexpr int kScaleRoom = 7;             // log2 of how far a value scale may exceed the power of two it is taken relative to
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     uint32_t y;
@@ -105,6 +107,9 @@ __device__ __forceinline__ void lds_words(const uint8_t *p, uint32_t (&w)[N]) {
 // CTAs of two warps an SM holds, by registers: 128, 168 and 255 a thread.
 __host__ __device__ constexpr int rows_blocks(int C, int NT) { return NT == 1 ? (C == 2 ? 8 : 6) : 4; }
 
+// CTAs of four warps for whole items: three where 168 registers do (16 sequences of 3 .. 5
+// rows in a window of 1024, 32 heads of 80: two 34.7 us, three 27.9).
+__host__ __device__ constexpr int whole_blocks(int C, int GC, int NT, int warps) { return warps == 4 && NT == 1 && (C < 4 || GC == C) ? 3 : 1; }
 
 // C chunks of 32 channels, GC chunks to a group, NT tiles of 8 query rows.
 template <int C, int GC, int NT, int kWarps>
@@ -118,15 +123,58 @@ struct RowsCfg {
     static constexpr int JOIN = ROWS * (D + 4) * 4 + 2 * ROWS * 4;   // one warp's O, m and l at the end
     static constexpr int KEY_GRIDS = 32 * NG * 8;         // (s, z) of a step's tokens in fp32
     static constexpr int VAL_GRIDS = 16 * NG * 8;         // (s, s'), (z, z') of a step's pairs of tokens in fp16
-    static constexpr int USED = RING + KEY_GRIDS + VAL_GRIDS;
+    static constexpr int APART = 32 * 4 + 32 * ROWS * 4;  // of tokens added by themselves: exponent less e; scores
+    static constexpr int USED = RING + KEY_GRIDS + VAL_GRIDS + APART;
     static constexpr int WARP_BYTES = USED > JOIN ? USED : JOIN;
     static constexpr int SMEM = kWarps * WARP_BYTES + kWarps * STAGES * 8 + (kWarps * 32 + 1) * 8;
 };
 
+// Adds the tokens `apart` of a step (2 b at bit b, 2 b + 1 at bit 16 + b) to the accumulators in fp32; their scales are
+// zero in the fragments.  x: their exponents less e, then all scores with these; the sums have taken P as it is with them.
+template <int C, int GC, int NT>
+__device__ __forceinline__ void add_apart(const float (&m)[NT][2], float (&l)[NT][2], float (&o)[NT][2 * C][4], unsigned apart, const float *x,
+                                          int group_exp, const uint32_t *codes, const uint32_t *grids) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
+    __syncwarp();
+    for (; apart != 0u; apart &= apart - 1u) {
+        const int bit = __ffs(static_cast<int>(apart)) - 1, k = 2 * (bit & 15) + (bit >> 4);
+        const float back = power(127 - static_cast<int>(x[k]));           // 2^(e - own)
+        const uint32_t *words = codes + (k >> 3) * (32 * C) + (4 * r + ((k & 7) >> 1)) * C;
+        float p[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                p[n][c] = ex2(x[32 + k * 8 * NT + 8 * n + 2 * t + c] - m[n][c]);
+                if (r == 0) l[n][c] = fmaf(p[n][c], back - 1.0f, l[n][c]);
+                p[n][c] *= back;
+            }
+#pragma unroll
+        for (int w = 0; w < C; ++w) {
+            const int g = w / GC;
+            const uint32_t grid = grids[k * (C / GC) + g], code = words[w] >> (16 * (k & 1));
+            const float s = __uint_as_float(grid & 0xFFFF0000u), z = __uint_as_float(grid << 16);
+            // the accumulators' units, 2^(24 + e_g - e), of channels 4 r + 1 and 4 r + 3 of the chunk 2^4 less, and 2^-e of P
+            const float unit = __shfl_sync(0xffffffffu, power(127 + 127 - 24 - group_exp), g);
+            auto channel = [&](int i) { return s * (static_cast<float>(code >> (4 * i) & 15u) - z); };
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float pu = p[n][c] * unit, pu4 = pu * 16.0f;
+                    o[n][2 * w][c] = fmaf(pu, channel(0), o[n][2 * w][c]);
+                    o[n][2 * w][c + 2] = fmaf(pu4, channel(1), o[n][2 * w][c + 2]);
+                    o[n][2 * w + 1][c] = fmaf(pu, channel(2), o[n][2 * w + 1][c]);
+                    o[n][2 * w + 1][c + 2] = fmaf(pu4, channel(3), o[n][2 * w + 1][c + 2]);
+                }
+        }
+    }
+}
+
 // HALF: fp16 queries and results, bf16 otherwise.
 // WHOLE: block x takes item x whole (items numbered by the longest sequence), nothing is dealt out or joined.
 template <int C, int GC, int NT, int kWarps, bool WHOLE, bool HALF>
-__global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k_attend_rows(const AttendArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, kWarps) : rows_blocks(C, NT)) k_attend_rows(const AttendArgs a) {
     using F = RowsCfg<C, GC, NT, kWarps>;
     constexpr int D = F::D, NG = F::NG, STAGES = F::STAGES;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -290,7 +338,11 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
         }
         float o[NT][2 * C][4];                            // O^T: channels and rows as the fragments have them
         float m[NT][2], l[NT][2];
-        float unit = 0.0f, room = 0.0f;                   // value scales are taken times `unit`, up to `room`; 0: none seen
+        constexpr int PER = (16 * NG + 31) / 32;          // (pair of tokens, channel group)s of a lane: lane + 32 i
+        int val_exp = kLeastExp;                          // e, and 2^-e_g of these groups
+        float down[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) down[i] = power(254 - kLeastExp);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -312,52 +364,100 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
             // ---- the step's grids, each turned once ----
             float2 *kgrid = reinterpret_cast<float2 *>(ring + F::RING);
             uint2 *vgrid = reinterpret_cast<uint2 *>(ring + F::RING + F::KEY_GRIDS);
+            float *apart_x = reinterpret_cast<float *>(ring + F::RING + F::KEY_GRIDS + F::VAL_GRIDS);
             const uint32_t *kwords = reinterpret_cast<const uint32_t *>(st + 4 * F::CODE_BYTES), *vwords = kwords + 32 * NG;
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
                 const uint32_t w = kwords[lane + 32 * i];
                 kgrid[lane + 32 * i] = make_float2(__uint_as_float(w & 0xFFFF0000u), __uint_as_float(w << 16));
             }
-            constexpr int PER = (16 * NG + 31) / 32;      // (pair, group)s of a lane
-            uint32_t v0[PER], v1[PER];
-            int big = 0;                                  // (a bad token's grid is negative as an integer)
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int at = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
-                const int pair = at / NG, g = at % NG;
-                v0[i] = vwords[2 * pair * NG + g];
-                v1[i] = vwords[(2 * pair + 1) * NG + g];
+            auto grids_of = [&](int pair, int g, uint32_t unseen, uint32_t &v0, uint32_t &v1) {
+                v0 = vwords[2 * pair * NG + g];
+                v1 = vwords[(2 * pair + 1) * NG + g];
                 if (edge) {   // grids of tokens that no row sees may never have been written: nothing of them is used
                     const int j = j0 + 2 * pair;
                     const bool none = (lost >> (pair >> 3)) & 1u;
-                    if (none || j < lo || j >= hi) v0[i] = 0u;
-                    if (none || j + 1 < lo || j + 1 >= hi) v1[i] = 0u;
+                    if (none || j < lo || j >= hi) v0 = unseen;
+                    if (none || j + 1 < lo || j + 1 >= hi) v1 = unseen;
                 }
-                big = max(big, max(static_cast<int>(v0[i]), static_cast<int>(v1[i])));
+            };
+            auto scaled = [&](uint32_t v0, uint32_t v1, float by) {
+                return pack_f16(__uint_as_float(v0 & 0xFFFF0000u) * by, __uint_as_float(v1 & 0xFFFF0000u) * by);
+            };
+            if (k == 0) {                                 // one e for all groups to begin with
+                int most = kLeastExp;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int at = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
+                    uint32_t v0, v1;
+                    grids_of(at / NG, at % NG, 0u, v0, v1);
+                    most = max(most, max(scale_exp(v0), scale_exp(v1)) + kHeadroom);
+                }
+                val_exp = min(__reduce_max_sync(0xffffffffu, most), kMostExp);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) down[i] = power(254 - val_exp);
             }
-            if (__any_sync(0xffffffffu, __int_as_float(big) > room)) {
-                big = __reduce_max_sync(0xffffffffu, big);
-                // the largest scale's power of two becomes 1; a zero point's bits do not reach the exponent
-                int e = static_cast<int>(static_cast<uint32_t>(big) >> 23) - 127;
-                e = e < -119 ? -119 : e;
-                const float to = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-                const float f = unit == 0.0f ? 1.0f : to / unit;
-                unit = to;
-                room = __uint_as_float(static_cast<uint32_t>(e + kScaleRoom < 127 ? 127 + kScaleRoom + e : 254) << 23);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int q = 0; q < 2 * C; ++q)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) o[n][q][c] *= f;
-            }
+            uint32_t s2[PER], z2[PER], off = 0u;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint32_t s2 = pack_f16(__uint_as_float(v0[i] & 0xFFFF0000u) * unit, __uint_as_float(v1[i] & 0xFFFF0000u) * unit);
+                const int at = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
+                uint32_t v0, v1;
+                grids_of(at / NG, at % NG, 0x7F000000u - __float_as_uint(down[i]), v0, v1);   // (a scale that fits, 1)
+                s2[i] = scaled(v0, v1, down[i]);
                 // 128 + z in bf16 ends in z's four bits: the integer, which is z in fp16's units of 2^-24
-                const uint32_t z2 = add_bf16x2(__byte_perm(v0[i], v1[i], 0x5410), 0x43004300u) & 0x000f000fu;
-                if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG) vgrid[lane + 32 * i] = make_uint2(s2, z2);
+                z2[i] = add_bf16x2(__byte_perm(v0, v1, 0x5410), 0x43004300u) & 0x000f000fu;
+                off |= misfits(s2[i]);
             }
+            unsigned apart = 0u;                          // tokens that are added by themselves
+            if (__any_sync(0xffffffffu, off != 0u)) {
+                constexpr int G2 = (NG + 1) / 2;
+                uint32_t w0[G2], w1[G2];
+                int eg[G2], before[NG], t0, t1;
+                const int val_was = val_exp, eg_was = 254 - static_cast<int>(__float_as_uint(down[0]) >> 23);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) before[g] = val_exp - __shfl_sync(0xffffffffu, eg_was, g);
+#pragma unroll
+                for (int i = 0; i < G2; ++i) {
+                    grids_of(lane & 15, group_of<NG>(i), 0u, w0[i], w1[i]);
+                    eg[i] = __shfl_sync(0xffffffffu, eg_was, group_of<NG>(i));
+                }
+                apart = refit(w0, w1, val_exp, eg, t0, t1);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {            // accumulators are in units of 2^(e_g - e)
+                    const int now = __shfl_sync(0xffffffffu, eg[g / 2], 16 * (g & 1));
+                    const float f = power(127 + val_exp - now - before[g]);
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if ((lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1) % NG == g) down[i] = power(254 - now);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int q = 2 * g * GC; q < 2 * (g + 1) * GC; ++q)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) o[n][q][c] *= f;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)              // maxima less e, sums times 2^e
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        m[n][c] -= static_cast<float>(val_exp - val_was);
+                        l[n][c] *= power(127 + val_exp - val_was);
+                    }
+                if (lane < 16) {
+                    apart_x[2 * lane] = static_cast<float>(apart >> lane & 1u ? t0 - val_exp : 0);
+                    apart_x[2 * lane + 1] = static_cast<float>(apart >> lane & 0x10000u ? t1 - val_exp : 0);
+                }
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int at = lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1;
+                    uint32_t v0, v1;
+                    grids_of(at / NG, at % NG, 0u, v0, v1);
+                    s2[i] = scaled(apart >> (at / NG) & 1u ? 0u : v0, apart >> (at / NG) & 0x10000u ? 0u : v1, down[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG) vgrid[lane + 32 * i] = make_uint2(s2[i], z2[i]);
             __syncwarp();
 
 #pragma unroll 1
@@ -410,7 +510,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[n][e] *= mult[n][e & 1];
                 }
-                if (edge) {
+                if (edge || apart) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int j = j0 + 16 * h + r + 8 * (e >> 1);
@@ -418,11 +518,22 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                         for (int n = 0; n < NT; ++n)
                             if (((lost >> h) & 1u) || j < see_lo[n][e & 1] || j >= see_hi[n][e & 1]) x[n][e] = -CUDART_INF_F;
                     }
+                    if (apart) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int k = 16 * h + r + 8 * (e >> 1);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                x[n][e] += apart_x[k];
+                                apart_x[32 + k * F::ROWS + 8 * n + 2 * t + (e & 1)] = x[n][e];
+                            }
+                        }
+                    }
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) above = above || fmaxf(x[n][c], x[n][c + 2]) > m[n][c] + kRaise;
+                    for (int c = 0; c < 2; ++c) above = above || fmaxf(x[n][c], x[n][c + 2]) > m[n][c] + (kAbove + kRaise);
                 if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -432,7 +543,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                             u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, 4));
                             u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, 8));
                             u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, 16));
-                            u = fmaxf(u, m[n][c]);
+                            u = fmaxf(u - kAbove, m[n][c]);
                             const float f = ex2(m[n][c] - u);
                             m[n][c] = u;
                             l[n][c] *= f;
@@ -501,6 +612,9 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                     }
                 }
             }
+            if (apart)
+                add_apart<C, GC, NT>(m, l, o, apart, apart_x, 254 - static_cast<int>(__float_as_uint(down[0]) >> 23),
+                                     reinterpret_cast<const uint32_t *>(st + 2 * F::CODE_BYTES), vwords);
             __syncwarp();                                 // every lane has read the stage: refill it
             const int32_t page = next_page;
             next_page = page_of(k + STAGES + 1);
@@ -510,9 +624,12 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
 
         // ---- the warps meet: O, m and l of each in its own ring ----
         __syncwarp();
+        float unit[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            unit[g] = __shfl_sync(0xffffffffu, power(127 + 24 + 254 - static_cast<int>(__float_as_uint(down[0]) >> 23) - val_exp), g);
         float *ow = reinterpret_cast<float *>(ring);
         float *mw = ow + F::ROWS * (D + 4), *lw = mw + F::ROWS;
-        const float back = unit == 0.0f ? 0.0f : 1.0f / unit;   // a power of two
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -523,14 +640,15 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? 1 : rows_blocks(C, NT)) k
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 const int row = 8 * n + 2 * t + c;
                 if (r == 0) {
-                    mw[row] = m[n][c];
-                    lw[row] = sum;
+                    mw[row] = m[n][c] + static_cast<float>(val_exp - 127);
+                    lw[row] = sum * power(254 - val_exp);
                 }
 #pragma unroll
-                for (int w = 0; w < C; ++w)
+                for (int w = 0; w < C; ++w) {
+                    const float u = unit[w / GC], u4 = u * 0.0625f;
                     *reinterpret_cast<float4 *>(ow + row * (D + 4) + 32 * w + 4 * r) =
-                        make_float4(o[n][2 * w][c] * 16777216.0f * back, o[n][2 * w][c + 2] * 1048576.0f * back,
-                                    o[n][2 * w + 1][c] * 16777216.0f * back, o[n][2 * w + 1][c + 2] * 1048576.0f * back);
+                        make_float4(o[n][2 * w][c] * u, o[n][2 * w][c + 2] * u4, o[n][2 * w + 1][c] * u, o[n][2 * w + 1][c + 2] * u4);
+                }
             }
         }
         __syncthreads();
