@@ -21,14 +21,20 @@
 // scores of 64 tokens a product, two buffers a row tile, four softmax warps a tile 568
 // us (a product of 128 x 64 takes as long as one of 128 x 128); whole steps and eight
 // warps a tile 540; exponentials taken at the old maximum before the new scores' is
-// known 512, which is 1.07 PFLOP/s.  The tensor pipe is then active 46% of the time, issue
-// slots 63%: the rest is the chain scores - softmax - P - products of either row tile.
-// Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16,
-// with powers of two for each 32 tokens that bring the largest scale to [1, 2); Q's
-// rows likewise.  2^F and the row's power of two go into the score's multiplier, E
-// into the exponent of P and 2^-E into the row sum, so that no magnitude leaves
-// fp16's range.  The running maximum is raised only when a score exceeds it by 8 (a
-// factor of 2^8), so the accumulator in tensor memory is rarely rescaled.  Sums are fp32.
+// known 512; tokens that may sit out a step 528, which is 1.04 PFLOP/s (with such tokens
+// added in fp32 by the softmax warps 598, for want of registers).  The tensor pipe is active
+// less than half of the time: the rest is the chain scores - softmax - P - products of
+// either row tile.
+// Numerics: K' = s (c - z) 2^-F and V' = s (c - z) 2^-E are rounded once to fp16, with
+// powers of two for each 32 tokens that bring the largest key scale to 2^10 and a token's
+// largest value scale to 2^-2 .. 2^10, so that scales of other tokens and channel groups keep
+// their bits down to 2^-14; Q's rows likewise.  2^F and the row's power of two go into
+// the score's multiplier, E into the exponent of P and 2^-E into the row sum.  Tokens whose
+// values do not fit the others' power of two sit out, and the step is taken again with
+// them and an E of theirs (seldom).  The running maximum is one of score + E, of what a token
+// adds, and raised only when one exceeds it by 8 (a factor of 2^8), so the accumulator in
+// tensor memory is rarely rescaled; P is taken 2^7 above it, keeps its bits down to 2^-21
+// of the greatest and vanishes 2^10 further down.  Sums are fp32.
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
@@ -43,6 +49,9 @@ constexpr int kTile = 128;                // rows of a tile, tokens of a step
 constexpr int kHalf = 64;                 // tokens of a step that a softmax warp takes
 constexpr int kThreads = 896;             // the last three warps have no part in it
 constexpr int kKeyWarp = 16, kValWarp = 20, kMmaWarp = 24;
+constexpr int kKeyRoom = 10, kValRoom = 10;   // log2 of the power of two that the largest scale is brought to
+constexpr int kTileWindow = 12;           // log2 of how far below it a token's largest value scale may be
+constexpr int kLeastE = 127 - 80;         // E + kValRoom is not below this: with 2^90 the sum of P stays finite
 constexpr int kInfos = 4;                // the turning warps are at most two steps ahead of softmax
 
 // Issued by one elected lane of a warp that goes along together, so that addresses stay in
@@ -143,6 +152,33 @@ __device__ __forceinline__ float total(const uint64_t (&s)[4]) {
     return x + y;
 }
 
+// The warps that turn codes meet and learn whether any of them says so.
+__device__ __forceinline__ bool any_turning(bool mine) {
+    int any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbar.red.or.pred p, 11, 256, q;\n\tselp.s32 %0, 1, 0, p;\n\t}"
+        : "=r"(any) : "r"(static_cast<int>(mine)) : "memory");
+    return any != 0;
+}
+
+// Whether a token whose largest value scale has exponent b (biased; 0, 1: unseen, all zeros or marked bad, no matter) does not fit.
+__device__ __forceinline__ bool misfit(int b, int e) { return b > e || (b > 1 && b < e - kTileWindow && e > kLeastE); }
+
+// Of the tokens `left` of 32, b the exponent of the lane's: a new e that at least a quarter of them fit; those that do not.
+__device__ __forceinline__ unsigned refit_tokens(int b, unsigned left, int &e) {
+    const int lane = threadIdx.x & 31;
+    unsigned rest = left & __ballot_sync(0xffffffffu, b > 1);
+    const int n = __popc(rest);
+    while (true) {
+        e = __reduce_max_sync(0xffffffffu, (rest >> lane & 1u) ? b : 0);
+        const unsigned in = rest & __ballot_sync(0xffffffffu, b >= e - (kTileWindow - kHeadroom));
+        rest &= ~in;
+        if (4 * __popc(in) >= n || rest == 0u) break;
+    }
+    e = max(e + kHeadroom, kLeastE);
+    return left & __ballot_sync(0xffffffffu, misfit(b, e));
+}
+
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -151,10 +187,9 @@ struct StepInfo {
     float key_up[4];          // 2^F of 32 tokens each
     float val_exp[4];         // E
     float val_down[4];        // 2^-E
-    uint8_t gone[4];          // of each 32 tokens, a bit for either 16: their page id is out of range
-    __device__ __forceinline__ unsigned gone_bits() const {
-        return static_cast<unsigned>(gone[0]) | gone[1] << 2 | gone[2] << 4 | gone[3] << 6;
-    }
+    unsigned out[4];          // of each 32 tokens, those that sit out
+    int step;                 // which step of the item it is; negative (and one less): the last one
+    uint8_t gone[4];          // of each 32 tokens, a bit for either 16, their page id is out of range; 4: some sit out
 };
 
 template <int C, int GC>
@@ -248,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
     if (warp >= kMmaWarp) {
         if (warp == kMmaWarp && steps > 0) {
             const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
-            const int todo = __shfl_sync(0xffffffffu, steps, 0), row_tiles = __shfl_sync(0xffffffffu, tiles, 0);
+            const int row_tiles = __shfl_sync(0xffffffffu, tiles, 0);
             const uint32_t bar0 = smem_u32(bars);         // barriers as above, 8 bytes each
             const uint64_t q0 = smem_desc_k128(smem_u32(sq)), k0 = smem_desc_k128(smem_u32(sk)), v0 = smem_desc_k128(smem_u32(sv_));
             // S_i = Q_i K^T of step j (descriptors count 16-byte units)
@@ -266,10 +301,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 constexpr uint32_t id = idesc_f16_f32(kTile, D);
                 const uint64_t vb = v0 + (j & 1) * (F::V_BYTES / 16);
                 const uint32_t pa = t0 + i * kTile, d = t0 + 2 * kTile + i * kTile;
-                const uint32_t more = j > 0 ? 1u : 0u;
+                const uint32_t sum = j > 0 ? 1u : 0u;
 #pragma unroll
                 for (int k = 0; k < kTile / 16; ++k)      // either half's P stands where its scores began
-                    mma_ts_one(d, pa + (k >> 2) * kHalf + 8 * (k & 3), vb + (k >> 2) * (D * 8) + 2 * (k & 3), id, k == 0 ? more : 1u);
+                    mma_ts_one(d, pa + (k >> 2) * kHalf + 8 * (k & 3), vb + (k >> 2) * (D * 8) + 2 * (k & 3), id, k == 0 ? sum : 1u);
             };
             bool ok = wait_warp(q_full, 0u) && wait_warp(&k_full[0], 0u);
             tc_fence_after();
@@ -277,15 +312,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 for (int i = 0; i < row_tiles; ++i) scores(i, 0);
                 commit_one(smem_u32(&k_empty[0]));
             }
-            for (int j = 0; ok && j < todo; ++j) {
+            for (int j = 0, more = 1; ok && more; ++j) {
+                more = __shfl_sync(0xffffffffu, static_cast<volatile int &>(info[j % kInfos].step), 0) >= 0;
                 ok = wait_warp(&v_full[j & 1], (j >> 1) & 1u);
-                if (ok && j + 1 < todo) ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
+                if (ok && more) ok = wait_warp(&k_full[(j + 1) & 1], ((j + 1) >> 1) & 1u);
                 for (int i = 0; ok && i < row_tiles; ++i) {
                     ok = wait_warp(&p_full[i], j & 1u);
                     if (!ok) break;
                     tc_fence_after();
                     values(i, j);
-                    if (j + 1 < todo) scores(i, j + 1);
+                    if (more) scores(i, j + 1);
                     else commit_one(bar0 + 8 * (10 + i));
                 }
                 if (ok) {                                 // step j's V and step j + 1's K have been multiplied
@@ -320,31 +356,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             return big == 0 ? 0 : e < -100 ? -100 : e;
         };
         auto power = [](int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); };
-        constexpr int PER = (16 * NG + 31) / 32;          // (pair of tokens, group)s of a lane
-        auto pair_of = [&](int i) { return lane + 32 * i < 16 * NG ? lane + 32 * i : 16 * NG - 1; };
-        uint32_t vg0[PER], vg1[PER];
-        int vpage[PER];
-        auto value_pages = [&](int j) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) vpage[i] = table[near(begin + j * kTile + 32 * w4 + 2 * (pair_of(i) / NG)) >> a.g.page_shift];
-        };
-        auto value_grids = [&](int j) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int q = pair_of(i), t2 = begin + j * kTile + 32 * w4 + 2 * (q / NG);
-                bool out;
-                const uint32_t *p = reinterpret_cast<const uint32_t *>(block_of(vpage[i], out) + vg_off) + q % NG;
-                const bool on0 = !out && t2 >= lo && t2 < hi, on1 = !out && t2 + 1 >= lo && t2 + 1 < hi;
-                vg0[i] = on0 ? p[(t2 & page_mask) * NG] : 0u;
-                vg1[i] = on1 ? p[((t2 + 1) & page_mask) * NG] : 0u;
-            }
-        };
-        auto value_exponent = [&]() {
-            int big = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) big = max(big, max(static_cast<int>(vg0[i]), static_cast<int>(vg1[i])));
-            return exponent(big);
-        };
         const __half2 sixteenth = __float2half2_rn(0.0625f);
         bool ok = true;
         if (keys && steps > 0) {
@@ -367,23 +378,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 for (int g = 0; g < NG; ++g) kg[g] = out || tok < lo || tok >= hi ? 0u : pg[g];
             };
             key_page(0);
-            value_pages(0);
             key_codes(0);
-            value_grids(0);
-            if (steps > 1) {
-                key_page(1);
-                value_pages(1);
-            }
-            for (int j = 0; j < steps; ++j) {
-                const int s = j & 1;
+            if (steps > 1) key_page(1);
+            for (int j = 0, n = 0; j < steps; ++n) {      // n: steps as they are taken
+                const int s = n & 1;
                 int big = 0;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) big = max(big, kg[g] < 0x7F800000u ? static_cast<int>(kg[g]) : 0);
-                const int kf = exponent(big), ve = value_exponent();
-                if (!wait_warp(&k_empty[s], ((j >> 1) & 1u) ^ 1u)) {
-                    ok = false;
-                    break;
-                }
+                const int kf = exponent(big) - kKeyRoom;
+                const bool again = any_turning(false);
+                ok = ok && wait_warp(&k_empty[s], ((n >> 1) & 1u) ^ 1u);   // (once it gave up it goes along without waiting)
                 const float down = power(-kf);
                 uint8_t *row = sk + s * F::K_BYTES + tid * 128;
                 // the token's words stand as [t][w]: channels 32 w + 8 t .. + 7, one 16-byte chunk each
@@ -409,25 +413,66 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                         }
                 }
                 if (lane == 0) {
-                    StepInfo &in = info[j % kInfos];
+                    StepInfo &in = info[n % kInfos];
+                    if (w4 == 0) in.step = !again && j + 1 == steps ? -1 - j : j;
                     in.key_up[w4] = power(kf);
-                    in.val_exp[w4] = static_cast<float>(ve);
-                    in.val_down[w4] = power(-ve);
-                    in.gone[w4] = static_cast<uint8_t>(gone);
+                    in.gone[w4] = static_cast<uint8_t>(gone | (in.out[w4] ? 4u : 0u));
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&k_full[s]);
-                if (j + 1 < steps) {
-                    key_codes(j + 1);
-                    value_grids(j + 1);
-                    if (j + 2 < steps) {
-                        key_page(j + 2);
-                        value_pages(j + 2);
-                    }
+                if (again) continue;                      // (where nothing is left over, with no token)
+                ++j;
+                if (j < steps) {
+                    key_codes(j);
+                    if (j + 1 < steps) key_page(j + 1);
                 }
             }
         } else if (steps > 0) {
+            constexpr int PER = (NG + 1) / 2;                 // lanes p and p + 16 have the pair of tokens p, each other groups
+            const int pair = lane & 15;
+            uint32_t vg0[PER], vg1[PER], next0[PER], next1[PER];   // grids of this step, of the next
+            int vpage = 0;
+            auto value_page = [&](int j) { vpage = table[near(begin + j * kTile + 32 * w4 + 2 * pair) >> a.g.page_shift]; };
+            auto value_grids = [&](int j) {
+                const int t2 = begin + j * kTile + 32 * w4 + 2 * pair;
+                bool out;
+                const uint32_t *p = reinterpret_cast<const uint32_t *>(block_of(vpage, out) + vg_off);
+                const bool on0 = !out && t2 >= lo && t2 < hi, on1 = !out && t2 + 1 >= lo && t2 + 1 < hi;
+    #pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    next0[i] = on0 ? p[(t2 & page_mask) * NG + group_of<NG>(i)] : 0u;
+                    next1[i] = on1 ? p[((t2 + 1) & page_mask) * NG + group_of<NG>(i)] : 0u;
+                }
+            };
+            auto take_grids = [&](int j) {                // step j's; those of the one after it are asked for
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    vg0[i] = next0[i];
+                    vg1[i] = next1[i];
+                }
+                if (j + 1 < steps) value_grids(j + 1);
+                if (j + 2 < steps) value_page(j + 2);
+            };
+            // Of the 32 tokens those `left` to take, in the end those left over; val_exp is E + kValRoom, biased.
+            int val_exp = kLeastE;
+            unsigned left = 0xffffffffu;
+            auto fit = [&]() {
+                uint32_t top = 0x80008000u;                   // greatest scales of the two as bf16 (a bad token's is below 0)
+    #pragma unroll
+                for (int i = 0; i < PER; ++i) top = __vmaxs2(top, __byte_perm(vg0[i], vg1[i], 0x7632));
+                if constexpr (NG > 1) top = __vmaxs2(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                unsigned out = 0u;
+                if (left != 0xffffffffu || __any_sync(0xffffffffu, misfit(static_cast<int>(top >> 7 & 0xffu), val_exp) || misfit(static_cast<int>(top >> 23 & 0xffu), val_exp))) {
+                    const int b = static_cast<int>(__shfl_sync(0xffffffffu, top, lane >> 1) >> (lane & 1 ? 23 : 7) & 0xffu);
+                    const unsigned over = left == 0u ? 0u : refit_tokens(b, left, val_exp);
+                    out = ~left | over;
+                    left = over;
+                } else {
+                    left = 0u;
+                }
+                return out;
+            };
             const int vr = lane >> 2, vb = lane & 3;      // channels 4 vr .. + 3 of each chunk, 8-token block vb of the warp's 32
             uint2 *pairs = reinterpret_cast<uint2 *>(spairs) + w4 * 16 * NG;   // [group][pair]
             uint32_t vw[4 * C];
@@ -441,35 +486,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 for (int i = 0; i < C; ++i) *reinterpret_cast<uint4 *>(&vw[4 * i]) = pv[i];
             };
             code_page(0);
-            value_pages(0);
+            value_page(0);
             codes(0);
             value_grids(0);
             if (steps > 1) {
                 code_page(1);
-                value_pages(1);
+                value_page(1);
             }
+            take_grids(0);
             const __half2 m960 = __float2half2_rn(960.0f);
-            for (int j = 0; j < steps; ++j) {
-                const int s = j & 1;
+            // What step n takes is found, and the warps that turn keys told, before step n - 1 is turned, for which this
+            // warp has to wait longer.
+            unsigned out = 0u;
+            bool again = false;
+            auto look_at = [&](int n) {
+                out = fit();
+                if (lane == 0) {
+                    StepInfo &in = info[n % kInfos];
+                    in.out[w4] = out;
+                    in.val_exp[w4] = static_cast<float>(val_exp - 127 - kValRoom);
+                    in.val_down[w4] = power(127 + kValRoom - val_exp);
+                }
+                again = any_turning(left != 0u);
+            };
+            look_at(0);
+            for (int j = 0, n = 0; j < steps; ++n) {
+                const int s = n & 1;
                 // scales and zero points of pairs of tokens, turned once by the warp
-                const float down = power(-value_exponent());
+                const float down = power(127 + kValRoom - val_exp);
+                out >>= 2 * pair;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const __half2 s2 = __floats2half2_rn(__uint_as_float(vg0[i] & 0xFFFF0000u) * down, __uint_as_float(vg1[i] & 0xFFFF0000u) * down);
+                    const __half2 s2 = __floats2half2_rn(out & 1u ? 0.0f : __uint_as_float(vg0[i] & 0xFFFF0000u) * down,
+                                                         out & 2u ? 0.0f : __uint_as_float(vg1[i] & 0xFFFF0000u) * down);
                     const __half2 z2 = __floats2half2_rn(__uint_as_float(vg0[i] << 16) + 1024.0f, __uint_as_float(vg1[i] << 16) + 1024.0f);
-                    const int q = pair_of(i);
-                    if (16 * NG % 32 == 0 || lane + 32 * i < 16 * NG)
-                        pairs[(q % NG) * 16 + q / NG] = make_uint2(*reinterpret_cast<const uint32_t *>(&s2), *reinterpret_cast<const uint32_t *>(&z2));
+                    if (NG % 2 == 0 || 2 * i + (lane >> 4) < NG)
+                        pairs[group_of<NG>(i) * 16 + pair] = make_uint2(*reinterpret_cast<const uint32_t *>(&s2), *reinterpret_cast<const uint32_t *>(&z2));
                 }
                 __syncwarp();
-                if (j + 1 < steps) {
-                    value_grids(j + 1);
-                    if (j + 2 < steps) value_pages(j + 2);
+                const bool done = !again;
+                if (done && j + 1 < steps) {
+                    left = 0xffffffffu;
+                    take_grids(j + 1);
                 }
-                if (!wait_warp(&v_empty[s], ((j >> 1) & 1u) ^ 1u)) {
-                    ok = false;
-                    break;
-                }
+                if (!done || j + 1 < steps) look_at(n + 1);
+                ok = ok && wait_warp(&v_empty[s], ((n >> 1) & 1u) ^ 1u);
                 uint8_t *base = sv_ + s * F::V_BYTES + (w4 >> 1) * (D * 128);
                 const int ch = 4 * (w4 & 1) + vb;
 #pragma unroll
@@ -515,9 +576,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 fence_async_smem();
                 __syncwarp();                             // also: the pairs are read before the next step's are written
                 if (lane == 0) mbar_arrive(&v_full[s]);
-                if (j + 1 < steps) {
-                    codes(j + 1);
-                    if (j + 2 < steps) code_page(j + 2);
+                if (!done) continue;
+                ++j;
+                if (j < steps) {
+                    codes(j);
+                    if (j + 1 < steps) code_page(j + 1);
                 }
             }
         }
@@ -533,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         visible(a, sv, qi, qi, see_lo, see_hi);
         const int all_lo = __reduce_max_sync(0xffffffffu, see_lo), all_hi = __reduce_min_sync(0xffffffffu, see_hi);
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * kTile, to = lanes + 2 * kTile;
-        bool ok = true;                                   // once false the remaining waits return at once
+        bool ok = true;                                   // no wait gave up
         // Q: the warp's 32 rows, LR lanes to a row, scaled into fp16 by a power of two of the row
         constexpr int LR = D <= 64 ? 8 : 16, RI = 32 / LR;
         const int64_t q_at = (sv.row0 + qi) * a.q_row + head * a.q_head;
@@ -585,14 +648,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full);
         float m = kFloor, l = 0.0f, mult = 0.0f;
-        for (int j = 0; i < tiles && j < steps; ++j) {
-            ok = ok && wait_warp(&s_full[i], j & 1u);     // and the products of the step before have been taken
+        for (int j = 0, more = steps > 0; i < tiles && more; ++j) {
+            ok = wait_warp(&s_full[i], j & 1u);           // and the products of the step before have been taken
+            if (!ok && lane == 0) *abort_flag = 1;
             tc_fence_after();
             // (these products have read Q and K, so what came with them is there)
             if (j == 0) mult = row_mult[p];
             const StepInfo &in = info[j % kInfos];
-            const int j0 = begin + j * kTile + grp * kHalf, c0 = 2 * grp;
-            const unsigned gone = (in.gone_bits() >> (2 * c0)) & 15u;
+            more = in.step >= 0;
+            const int c0 = 2 * grp, j0 = begin + (more ? in.step : -1 - in.step) * kTile + grp * kHalf;
+            const unsigned gone = *reinterpret_cast<const uint16_t *>(&in.gone[c0]);
             const uint32_t ts = lanes + grp * kHalf;
             const bool edge = gone != 0u || j0 < all_lo || j0 + kHalf > all_hi;
             // what scores of 32 tokens are multiplied with: never 0, as masked ones are -inf by then (all-zero rows and
@@ -606,10 +671,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     asm volatile("" ::: "memory");        // a branch around this, not selects in every step
                     // bit e: the row sees token e of the 32
                     const int t0 = j0 + 32 * c, from = max(see_lo - t0, 0), upto = min(see_hi - t0, 32);
-                    unsigned bits = from < 32 ? 0xffffffffu << from : 0u;
+                    unsigned bits = (from < 32 ? 0xffffffffu << from : 0u) & ~in.out[c0 + c];
                     bits &= upto > 0 ? 0xffffffffu >> (32 - upto) : 0u;
-                    if ((gone >> (2 * c)) & 1u) bits &= 0xffff0000u;
-                    if ((gone >> (2 * c)) & 2u) bits &= 0x0000ffffu;
+                    if ((gone >> (8 * c)) & 1u) bits &= 0xffff0000u;
+                    if ((gone >> (8 * c)) & 2u) bits &= 0x0000ffffu;
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (!((bits >> e) & 1u)) v[e] = -CUDART_INF_F;
@@ -642,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
             const int pair_bar = 1 + 4 * i + quad;        // this warp and the other group's warp of these rows
             bool raise = j == 0;
             if (j > 0) {
-                // taken at the old maximum at once; only where one exceeds 2^kRaise (seldom) it is all done again
+                // taken at the old maximum at once; only where one exceeds 2^(kAbove + kRaise) (seldom) it is all done again
                 uint32_t h[32];
                 float v[32];
                 fetch(0, v);
@@ -657,7 +722,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 #pragma unroll
                     for (int q = 0; q < 4; ++q) x[q] = __hmax2(x[q], as_half2(h[e + q]));
                 x[0] = __hmax2(__hmax2(x[0], x[1]), __hmax2(x[2], x[3]));
-                raise = any_of_64(pair_bar, __hgt(__hmax(__low2half(x[0]), __high2half(x[0])), __float2half(256.0f)));
+                raise = any_of_64(pair_bar, !ok || __hgt(__hmax(__low2half(x[0]), __high2half(x[0])), __float2half(32768.0f)));
                 if (!raise) {
                     tmem_st_x32(ts, h);
                     l += sum;
@@ -670,12 +735,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 for (int c = 0; c < 2; ++c) {
                     float v[32];
                     fetch(c, v);
-                    top = fmaxf(top, highest(c, v));
+                    top = fmaxf(top, highest(c, v) - kAbove);
                 }
                 // the other half's, from the other group
-                row_max[grp * 2 * kTile + p] = top;
+                row_max[grp * 2 * kTile + p] = ok ? top : CUDART_NAN_F;
                 sync_64(pair_bar);
-                top = fmaxf(top, row_max[(1 - grp) * 2 * kTile + p]);
+                const float theirs = row_max[(1 - grp) * 2 * kTile + p];
+                ok = ok && theirs == theirs;
+                if (!ok) break;                           // one of the two gave up: both leave at the same barrier
+                top = fmaxf(top, theirs);
                 const float now = fmaxf(m, top), f = ex2(m - now);
                 m = now;
                 l *= f;
