@@ -432,7 +432,8 @@ typedef struct {
     const int32_t *q_start;      /* device, seqs + 1 values, ascending */
     const int32_t *kv_len;       /* device, seqs values */
     const int32_t *page_table;   /* device, seqs x table_ld: token j of sequence b is in page [b][j / page_size] */
-    int64_t table_ld;            /* kv_len above table_ld * page_size latches QE_ERR_INVALID_ARG and is cut */
+    int64_t table_ld;            /* pages a row, and the distance of rows; up to 2^30 tokens.  kv_len above
+                                  * table_ld * page_size latches QE_ERR_INVALID_ARG and is cut */
 } qe_attention;
 
 /* Bytes of workspace qe_cache_attention needs (0 where it needs none). */

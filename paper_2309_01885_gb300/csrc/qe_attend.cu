@@ -277,8 +277,7 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
     if (dtype != QE_BF16 && dtype != QE_F16) return dtype == QE_F32 ? QE_ERR_UNSUPPORTED : QE_ERR_INVALID_ARG;
     if (at->rows == 0 || at->max_q == 0) return QE_OK;
     if (!at->q_start || !at->kv_len || !at->page_table || at->table_ld < 1 || !Q || !out) return QE_ERR_INVALID_ARG;
-    if (at->table_ld > (int64_t{1} << 30) >> a.g.page_shift && at->table_ld << a.g.page_shift > (int64_t{1} << 30))
-        return QE_ERR_INVALID_ARG;
+    if (at->table_ld > (int64_t{1} << 30) >> a.g.page_shift) return QE_ERR_INVALID_ARG;
     if (((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(out)) & 1u) != 0 ||
         ((reinterpret_cast<uintptr_t>(at->q_start) | reinterpret_cast<uintptr_t>(at->kv_len) |
           reinterpret_cast<uintptr_t>(at->page_table) | reinterpret_cast<uintptr_t>(lse)) & 3u) != 0 ||

@@ -510,12 +510,16 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
                        workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of q (rows x q_heads x head_dim, bf16 or fp16) over the cache.  Sequence b has the rows
     q_start[b] .. q_start[b + 1] - 1 (int32, seqs + 1) and kv_len[b] (int32) cached tokens, the rows' own
-    among them; its token j is in page page_table[b, j // page_size] (int32).  No sequence has more than
-    max_q rows; max_kv is about the longest kv_len.  causal / window (0 = none) / scale (0 = 1 /
-    sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x q_heads, written.  workspace: optional
+    among them; its token j is in page page_table[b, j // page_size] (int32; copied where it is not
+    contiguous).  No sequence has more than max_q rows; max_kv is about the longest kv_len.  causal /
+    window (0 = none) / scale (0 = 1 / sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x
+    q_heads, written.  workspace: optional
     uint8 tensor of qe_cache_attention_workspace() bytes."""
     rows, heads, dim = q.shape
     q0, q1 = _cache_heads(cache, q, heads, "q")
+    if not page_table.is_contiguous():                   # the library's rows follow one another: a part of a wider table is copied
+        with torch.cuda.stream(stream):
+            page_table = page_table.contiguous()
     seqs, dtype = kv_len.shape[0], q.dtype
     if q_start.shape[0] != seqs + 1 or page_table.shape[0] != seqs:
         raise ValueError("q_start holds seqs + 1 values, page_table seqs rows")
@@ -532,7 +536,7 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
     at = QEAttention(seqs, rows, heads, causal, window, scale, max_q, max_kv,
                      _cache_index(cache, q_start, torch.int32, 1, "q_start"),
                      _cache_index(cache, kv_len, torch.int32, 1, "kv_len"),
-                     _cache_index(cache, page_table, torch.int32, 2, "page_table"), page_table.stride(0))
+                     _cache_index(cache, page_table, torch.int32, 2, "page_table"), page_table.shape[-1])
     ws, ws_bytes = None, 0
     if workspace is not None:
         if workspace.get_device() != cache._index or not workspace.is_contiguous():
