@@ -173,14 +173,15 @@ struct AttendPlan {
 };
 
 int sm_count() {
-    static const int n = [] {
-        int dev = 0, v = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1)
-            v = 152;
+    static std::atomic<int> known[64];                   // by device; 0: not asked yet
+    int dev = 0, v = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev < 64 && (v = known[dev].load(std::memory_order_relaxed)) > 0) return v;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1) {
         cudaGetLastError();
-        return v;
-    }();
-    return n;
+        return 152;
+    }
+    if (dev < 64) known[dev].store(v, std::memory_order_relaxed);
+    return v;
 }
 
 // (query row, head) pairs of a kv head up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles):

@@ -1,6 +1,8 @@
 // Arguments and launchers of attention over the 4-bit key/value cache.
 #pragma once
 
+#include <atomic>
+
 #include "qe_cache.cuh"
 
 namespace qe {
@@ -159,6 +161,19 @@ __device__ __forceinline__ void locate(const AttendArgs &a, int unit, const int6
 __device__ __forceinline__ int64_t worker_units(const AttendArgs &a, int64_t total) {
     const int64_t per = div_small(total + a.ctas - 1, a.ctas);
     return per < a.min_units ? a.min_units : per;
+}
+
+// Raises a kernel's limit of dynamic shared memory on the current device, once a device (the call takes longer than the
+// question whether it has been made); `raised`, a bit a device, is the kernel's own.  A refusal is not remembered.
+inline cudaError_t raise_smem(const void *kernel, int bytes, std::atomic<uint64_t> &raised) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+    if (raised.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // few query rows per kv head: `tiles` x 8 pairs an item; then the items that workers share are joined

@@ -701,9 +701,9 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
 template <int C, int GC, int NT, int W, bool WHOLE, bool HALF>
 cudaError_t launch_rows_as(const AttendArgs &a, cudaStream_t s) {
     using F = RowsCfg<C, GC, NT, W>;
-    static const cudaError_t once =
-        cudaFuncSetAttribute(k_attend_rows<C, GC, NT, W, WHOLE, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM);
-    if (once != cudaSuccess) return once;
+    static std::atomic<uint64_t> raised{0};
+    const cudaError_t e = raise_smem(reinterpret_cast<const void *>(k_attend_rows<C, GC, NT, W, WHOLE, HALF>), F::SMEM, raised);
+    if (e != cudaSuccess) return e;
     k_attend_rows<C, GC, NT, W, WHOLE, HALF><<<static_cast<unsigned>(WHOLE ? a.items : a.ctas), W * 32, F::SMEM, s>>>(a);
     return cudaGetLastError();
 }

@@ -891,9 +891,9 @@ __global__ void __launch_bounds__(256) k_attend_join_tiles(const AttendArgs a) {
 template <int C, int GC>
 cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) {
     using F = TcCfg<C, GC>;
-    static const cudaError_t once =
-        cudaFuncSetAttribute(k_attend_tiles<C, GC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM_ASKED);
-    if (once != cudaSuccess) return once;
+    static std::atomic<uint64_t> raised{0};
+    const cudaError_t e = raise_smem(reinterpret_cast<const void *>(k_attend_tiles<C, GC>), F::SMEM_ASKED, raised);
+    if (e != cudaSuccess) return e;
     k_attend_tiles<C, GC><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
     return cudaGetLastError();
 }

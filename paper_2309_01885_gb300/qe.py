@@ -403,6 +403,7 @@ def qe_quantize_layer_outlier(W: torch.Tensor, Sigma: torch.Tensor, bits: int, i
 
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _CACHE_DTYPES = {torch.float32: QE_F32, torch.bfloat16: QE_BF16, torch.float16: QE_F16}
 
 
@@ -428,6 +429,11 @@ class KVCache:
         self.head_dim, self.group_size, self.data, self.device = head_dim, group_size, data, data.device
         self._c = QECache(data.data_ptr(), data.numel(), pages, page_size, kv_heads, head_dim, group_size)
         self._ref, self._index = ctypes.addressof(self._c), data.get_device()
+
+
+def _elsewhere(cache: KVCache) -> bool:
+    """Whether the cache's GPU is not the current one, which the library launches on."""
+    return cache._index >= 0 and _current_device() != cache._index
 
 
 def _cache_heads(cache: KVCache, t: torch.Tensor, heads: int, what: str):
@@ -457,6 +463,9 @@ def _cache_dtype(t) -> int:
 def qe_cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """Quantize keys and values (tokens x kv_heads x head_dim, any row and head strides) into the
     cache's `slots` (int64 per token: page * page_size + position in the page; negative = skip)."""
+    if _elsewhere(cache):
+        with torch.cuda.device(cache._index):
+            return qe_cache_append(cache, k, v, slots, stream)
     at = _cache_index(cache, slots, torch.int64, 1, "slots")
     (k0, k1), (v0, v1) = _cache_heads(cache, k, cache.kv_heads, "k"), _cache_heads(cache, v, cache.kv_heads, "v")
     n, dtype = slots.shape[0], k.dtype
@@ -472,6 +481,9 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
                   v: torch.Tensor | None = None, stream=None) -> tuple:
     """(keys, values) of the cache's `slots`, tokens x kv_heads x head_dim, rounded once to `dtype`;
     written into `k` and `v` where given (any row and head strides)."""
+    if _elsewhere(cache):
+        with torch.cuda.device(cache._index):
+            return qe_cache_read(cache, slots, dtype, k, v, stream)
     at = _cache_index(cache, slots, torch.int64, 1, "slots")
     n, heads, dim = slots.shape[0], cache.kv_heads, cache.head_dim
     k0, k1, v0, v1 = heads * dim, dim, heads * dim, dim
@@ -497,6 +509,9 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
 def qe_cache_attention_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int, *,
                                  causal: bool = True, window: int = 0) -> int:
     """Bytes of workspace qe_cache_attention takes for such a batch (a call without the window never takes less)."""
+    if _elsewhere(cache):
+        with torch.cuda.device(cache._index):
+            return qe_cache_attention_workspace(cache, seqs, q_heads, rows, max_q, max_kv, causal=causal, window=window)
     at = QEAttention(seqs=seqs, rows=rows, q_heads=q_heads, causal=causal, window=window, max_q=max_q, max_kv=max_kv)
     n = ctypes.c_size_t(0)
     _check(load().qe_cache_attention_workspace(cache._ref, ctypes.addressof(at), ctypes.byref(n)),
@@ -515,6 +530,10 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
     window (0 = none) / scale (0 = 1 / sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x
     q_heads, written.  workspace: optional
     uint8 tensor of qe_cache_attention_workspace() bytes."""
+    if _elsewhere(cache):
+        with torch.cuda.device(cache._index):
+            return qe_cache_attention(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal=causal, window=window, scale=scale,
+                                      out=out, lse=lse, workspace=workspace, stream=stream)
     rows, heads, dim = q.shape
     q0, q1 = _cache_heads(cache, q, heads, "q")
     if not page_table.is_contiguous():                   # the library's rows follow one another: a part of a wider table is copied
