@@ -436,7 +436,9 @@ typedef struct {
                                   * table_ld * page_size latches QE_ERR_INVALID_ARG and is cut */
 } qe_attention;
 
-/* Bytes of workspace qe_cache_attention needs (0 where it needs none). */
+/* Bytes of workspace that qe_cache_attention needs at most on the current device, for
+ * this batch and for every one with no more seqs, max_q and max_kv of the same
+ * cache and q_heads, whatever its window (0 where none needs any). */
 qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention *at, size_t *bytes);
 
 /*

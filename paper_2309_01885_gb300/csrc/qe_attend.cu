@@ -235,6 +235,29 @@ size_t attend_bytes(const AttendPlan &p, const CacheGeom &g) {
     return static_cast<size_t>(2) * p.ctas * p.rows_cap * (g.D + 2) * sizeof(float);
 }
 
+int64_t smaller(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// The most that any batch needs which has no more sequences, query rows a sequence and tokens than this one.  (What one
+// batch needs does not grow with it: 19 sequences may fill the GPU in whole items, which one alone has to be cut for.)
+size_t attend_most_bytes(const CacheGeom &g, const qe_attention &at) {
+    const int64_t pairs = at.max_q * (at.q_heads / g.kv_heads), row = static_cast<int64_t>(g.D + 2) * sizeof(float);
+    int64_t most = 0;
+    for (int tiles = 1; tiles <= (g.D <= 64 ? 4 : 2); tiles *= 2) {
+        if (tiles > 1 && pairs <= 4 * tiles) break;       // no batch of these takes so many tiles
+        const int cap = 8 * tiles;
+        const int64_t end = tiles == (g.D <= 64 ? 4 : 2) ? few_pairs(g.D) : cap;
+        const int64_t units = at.seqs * ceil_div(smaller(pairs, end), cap) * g.kv_heads * ceil_div(at.max_kv + kRowsUnit, kRowsUnit);
+        const int64_t ctas = smaller(ceil_div(units, 8), static_cast<int64_t>(sm_count()) * rows_blocks(g.D / 32, tiles));
+        if (ctas > 1 && 2 * ctas * cap * row > most) most = 2 * ctas * cap * row;
+    }
+    const int64_t pieces = ceil_div(at.max_kv, 128) / 4;  // of an item of tiles
+    if (pairs > few_pairs(g.D) && pieces > 1 && sm_count() / g.kv_heads > 1) {
+        const int64_t all = smaller(sm_count(), at.seqs * ceil_div(pairs, 256) * g.kv_heads * pieces) * 256 * row;
+        if (all > most) most = all;
+    }
+    return static_cast<size_t>(most);
+}
+
 // Geometry of a cache that may have no memory yet (the workspace query takes it either way).
 qe_status shape_geom(const qe_cache *cache, CacheGeom *g) {
     if (!cache) return QE_ERR_INVALID_ARG;
@@ -264,7 +287,7 @@ qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention
     qe_status st = shape_geom(cache, &g);
     if (st != QE_OK) return st;
     if ((st = check_shape(g, at)) != QE_OK) return st;
-    *bytes = attend_bytes(attend_plan(g, *at), g);
+    *bytes = attend_most_bytes(g, *at);
     return QE_OK;
 }
 

@@ -508,7 +508,8 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
 
 def qe_cache_attention_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int, *,
                                  causal: bool = True, window: int = 0) -> int:
-    """Bytes of workspace qe_cache_attention takes for such a batch (a call without the window never takes less)."""
+    """Bytes of workspace that do for such a batch and for every one with no more sequences, rows a sequence and
+    tokens, whatever its window."""
     if _elsewhere(cache):
         with torch.cuda.device(cache._index):
             return qe_cache_attention_workspace(cache, seqs, q_heads, rows, max_q, max_kv, causal=causal, window=window)
