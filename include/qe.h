@@ -457,7 +457,9 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
                              size_t workspace_bytes, qe_stream_t stream);
 
 /* Waits for `stream`, then returns and clears the error latched on the current
- * device (QE_ERR_NUMERIC / QE_ERR_TIMEOUT / QE_ERR_INVALID_ARG for an index out of range), or QE_ERR_CUDA if the stream failed.
+ * device, or QE_ERR_CUDA if the stream failed: QE_ERR_TIMEOUT, which leaves nothing
+ * else to report; QE_ERR_INVALID_ARG for an index out of range; QE_ERR_NUMERIC.  Of
+ * the last two, where both are latched, either has a call of its own.
  * The error word is a file-scope device variable whose address the library looks
  * up once per device and caches; calling the library on a device after a
  * cudaDeviceReset of that device is not supported. */

@@ -41,6 +41,8 @@ static unsigned *error_word() {
 
 unsigned *device_error_word() { return error_word(); }
 
+__global__ void k_latch(unsigned *word, unsigned bits) { set_error(word, bits); }
+
 static int sm_count() {
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 148;
@@ -857,7 +859,16 @@ qe_status qe_sync_status(qe_stream_t stream) {
         return QE_ERR_CUDA;
     }
     if (v & ERR_TIMEOUT) return QE_ERR_TIMEOUT;
-    if (v & ERR_RANGE) return QE_ERR_INVALID_ARG;
+    if (v & ERR_RANGE) {
+        if (v & ERR_NUMERIC) {                            // the next call's answer
+            k_latch<<<1, 1, 0, s>>>(e, ERR_NUMERIC);
+            if (cudaStreamSynchronize(s) != cudaSuccess) {
+                cudaGetLastError();
+                return QE_ERR_CUDA;
+            }
+        }
+        return QE_ERR_INVALID_ARG;
+    }
     if (v & ERR_NUMERIC) return QE_ERR_NUMERIC;
     return QE_OK;
 }
