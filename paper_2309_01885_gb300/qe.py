@@ -481,9 +481,9 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
                   v: torch.Tensor | None = None, stream=None) -> tuple:
     """(keys, values) of the cache's `slots`, tokens x kv_heads x head_dim, rounded once to `dtype`;
     written into `k` and `v` where given (any row and head strides)."""
-    if _elsewhere(cache):
-        with torch.cuda.device(cache._index):
-            return qe_cache_read(cache, slots, dtype, k, v, stream)
+    if stream is not None or _elsewhere(cache):          # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(cache._index):
+            return qe_cache_read(cache, slots, dtype, k, v)
     at = _cache_index(cache, slots, torch.int64, 1, "slots")
     n, heads, dim = slots.shape[0], cache.kv_heads, cache.head_dim
     k0, k1, v0, v1 = heads * dim, dim, heads * dim, dim
@@ -500,7 +500,7 @@ def qe_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
         if v.shape[0] != n or v.dtype is not dtype:
             raise ValueError("v holds the tokens of slots, in dtype")
     st = (_lib or load()).qe_cache_read(cache._ref, at, n, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, _cache_dtype(dtype),
-                                        _raw_stream(cache._index) if stream is None else stream.cuda_stream)
+                                        _raw_stream(cache._index))
     if st != QE_OK:
         raise QEError(st, "qe_cache_read")
     return k, v
@@ -531,15 +531,14 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
     window (0 = none) / scale (0 = 1 / sqrt(head_dim)) as in include/qe.h.  lse: optional fp32 rows x
     q_heads, written.  workspace: optional
     uint8 tensor of qe_cache_attention_workspace() bytes."""
-    if _elsewhere(cache):
-        with torch.cuda.device(cache._index):
+    if stream is not None or _elsewhere(cache):          # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(cache._index):
             return qe_cache_attention(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal=causal, window=window, scale=scale,
-                                      out=out, lse=lse, workspace=workspace, stream=stream)
+                                      out=out, lse=lse, workspace=workspace)
     rows, heads, dim = q.shape
     q0, q1 = _cache_heads(cache, q, heads, "q")
     if not page_table.is_contiguous():                   # the library's rows follow one another: a part of a wider table is copied
-        with torch.cuda.stream(stream):
-            page_table = page_table.contiguous()
+        page_table = page_table.contiguous()
     seqs, dtype = kv_len.shape[0], q.dtype
     if q_start.shape[0] != seqs + 1 or page_table.shape[0] != seqs:
         raise ValueError("q_start holds seqs + 1 values, page_table seqs rows")
@@ -564,7 +563,7 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     st = (_lib or load()).qe_cache_attention(cache._ref, ctypes.addressof(at), q.data_ptr(), q0, q1, out.data_ptr(), o0, o1,
                                              _cache_dtype(dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
-                                             _raw_stream(cache._index) if stream is None else stream.cuda_stream)
+                                             _raw_stream(cache._index))
     if st != QE_OK:
         raise QEError(st, "qe_cache_attention")
     return out
