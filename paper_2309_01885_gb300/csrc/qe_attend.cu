@@ -184,9 +184,11 @@ int sm_count() {
     return v;
 }
 
-// (query row, head) pairs of a kv head up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles):
-// 64 channels, 29 pairs 63 / 92; 128 channels, 20 pairs 82 / 97, 32 pairs 64 / 57.
-constexpr int64_t few_pairs(int D) { return D <= 64 ? 32 : 24; }
+// (query row, head) pairs of a kv head up to which the few-rows kernel takes a call.  Measured (us on the GPU, few rows /
+// tiles, caches out of L2, one row of so many heads on 8 kv heads): 2 x 30000 tokens, 64 channels 32 pairs 41 / 54, 33 pairs
+// 56 / 54, 96 channels 50 / 63 and 67 / 63, 128 channels 59 / 70 and 79 / 70; 32 x 4096 tokens, 128 channels 101 / 143 and
+// 137 / 143.
+constexpr int kFewPairs = 32;
 
 AttendPlan attend_plan(const CacheGeom &g, const qe_attention &at) {
     const int64_t seqs = at.seqs, max_q = at.max_q, max_kv = at.max_kv, window = at.causal ? at.window : 0;
@@ -196,7 +198,7 @@ AttendPlan attend_plan(const CacheGeom &g, const qe_attention &at) {
     const int64_t span = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;   // most that a row sees
     p.splits = 1;
     p.warps = 0;
-    if (pairs > few_pairs(g.D)) {
+    if (pairs > kFewPairs) {
         p.tiles = 0;
         p.rows_cap = 256;
         p.items = seqs * ceil_div(pairs, 256) * g.kv_heads;
@@ -245,13 +247,13 @@ size_t attend_most_bytes(const CacheGeom &g, const qe_attention &at) {
     for (int tiles = 1; tiles <= (g.D <= 64 ? 4 : 2); tiles *= 2) {
         if (tiles > 1 && pairs <= 4 * tiles) break;       // no batch of these takes so many tiles
         const int cap = 8 * tiles;
-        const int64_t end = tiles == (g.D <= 64 ? 4 : 2) ? few_pairs(g.D) : cap;
+        const int64_t end = tiles == (g.D <= 64 ? 4 : 2) ? kFewPairs : cap;
         const int64_t units = at.seqs * ceil_div(smaller(pairs, end), cap) * g.kv_heads * ceil_div(at.max_kv + kRowsUnit, kRowsUnit);
         const int64_t ctas = smaller(ceil_div(units, 8), static_cast<int64_t>(sm_count()) * rows_blocks(g.D / 32, tiles));
         if (ctas > 1 && 2 * ctas * cap * row > most) most = 2 * ctas * cap * row;
     }
     const int64_t pieces = ceil_div(at.max_kv, 128) / 4;  // of an item of tiles
-    if (pairs > few_pairs(g.D) && pieces > 1 && sm_count() / g.kv_heads > 1) {
+    if (pairs > kFewPairs && pieces > 1 && sm_count() / g.kv_heads > 1) {
         const int64_t all = smaller(sm_count(), at.seqs * ceil_div(pairs, 256) * g.kv_heads * pieces) * 256 * row;
         if (all > most) most = all;
     }
