@@ -217,10 +217,13 @@ AttendPlan attend_plan(const CacheGeom &g, const qe_attention &at) {
     p.rows_cap = 8 * p.tiles;
     p.min_units = 8;
     const int64_t items = p.items = seqs * ceil_div(pairs, p.rows_cap) * g.kv_heads;
-    // short contexts: a CTA for each item saves the dealing out and the joining.  Measured (32 heads of 128, us,
-    // dealt out / CTAs of 8 warps / of 4): 32 items of 513 tokens 15.6 / 8.5 / 10.0, 128 of 1000 .. 2000 21.5 /
-    // 16.3 / 21.5, 512 of up to 1024 35 / 34 / 23, 2048 of 300 .. 600 59 / 103 / 70
-    p.warps = items <= 152 && span <= 2048 ? 8 : items <= 1216 && span <= 1088 ? 4 : 0;
+    // short contexts: a CTA for each item saves the dealing out and the joining.  Measured (us on 152 SMs, caches out of L2,
+    // dealt out / CTAs of 8 warps / of 4; single tokens, 4 heads of 128 a kv head, lengths from half the span up): 32 items
+    // of 2048 tokens 18 / 17 / 23, of 3000 18 / 23 / 32; 152 of 2048 26 / 18 / 24, of 4096 34 / 30 / 42; 160 of 1024
+    // 25 / 19 / 16, of 1536 28 / 22 / 21; 512 of 1024 32 / 39 / 31, of 1536 37 / 49 / 41; 1216 of 512 42 / 57 / 40, of 1024
+    // 60 / 85 / 62; 1280 of 512 43 / 61 / 45.  The limits are those of the most items of either form, and leave something to
+    // fewer (160 of 1100: 25 for 17) and to smaller heads (64 channels, 1280 of 512: 32 for 24).
+    p.warps = items <= sm_count() && span <= 2048 ? 8 : items <= 8 * sm_count() && span <= 1088 ? 4 : 0;
     if (p.warps > 0) {
         p.ctas = 1;
         return p;

@@ -24,3 +24,17 @@ def test_up_to_32_pairs_are_few(lib, dim, group):
             assert "k_attend_rows" in form(lib, host.cache(8, dim, group), host.batch(3, q, kv, 8 * per_kv)), (per_kv, q)
         for per_kv, q in ((33, 1), (1, 33), (4, 9), (71, 1)):
             assert "k_attend_tiles" in form(lib, host.cache(8, dim, group), host.batch(3, q, kv, 8 * per_kv)), (per_kv, q)
+
+
+@pytest.mark.parametrize("device,sms", [(0, 152), (1, 76), (2, 148)])
+def test_forms_for_short_contexts_go_by_the_devices_size(lib, device, sms):
+    """A CTA of 8 warps for each item while they fit one an SM, of 4 up to 8 an SM; grids tell the items."""
+    lib.fake_device(device, sms)
+    c = host.cache(1, 128, 32)
+    for items, span, warps in ((sms, 2048, 8), (sms + 1, 1088, 4), (8 * sms, 1088, 4), (8 * sms + 1, 1088, 0), (sms, 2049, 0), (sms + 1, 1089, 0)):
+        name = form(lib, c, host.batch(items, 1, span, 4))
+        # k_attend_rows<C, GC, NT, warps, WHOLE, HALF>
+        assert (f"Li{warps}ELb1E" if warps else "Li2ELb0E") in name, (items, span, name)
+        if warps:
+            assert lib.fake_grid(0) == items
+    lib.fake_device(0, 152)
