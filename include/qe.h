@@ -418,7 +418,19 @@ qe_status qe_cache_read(const qe_cache *cache, const int64_t *slots, int64_t tok
  * rows and L tokens, row i sits at position L - n + i.  It sees all L tokens
  * (causal = 0), or those up to its position (causal = 1), of which with
  * window = W > 0 the last W.  Query head h reads kv head h / (q_heads / kv_heads).
- * A row that sees no token is zero, with lse -inf.
+ * A row that sees no token is zero, with lse -inf.  Rows that belong to no sequence
+ * (before q_start[0], from q_start[seqs] on) are left as they were.
+ *
+ * Rounding: scores, maxima and sums are binary32.  Up to 32 (query row, head) pairs of
+ * a kv head in a sequence, probabilities are rounded to 11 bits and their products
+ * with value scales again (once for fp16 results); with more pairs, probabilities,
+ * keys and values each once.  Errors are relative to each result's own terms: tokens
+ * and channel groups of other sizes do not enter.  What ends that is fp16's range: of
+ * probability times the token's largest value scale, what is 2^-21 below the greatest
+ * of its row keeps fewer bits and what is 2^-31 below adds nothing (2^-9 and 2^-20 where
+ * value scales differ by up to 2^12, beyond which tokens are kept apart); with more
+ * than 32 pairs, keys and channel groups of values 2^-24 below the largest of 32 tokens.
+ * Value scales outside 2^-47 .. 2^41 are correct, but slow, up to 32 pairs.
  */
 typedef struct {
     int64_t seqs;                /* 1 .. 65535 */
@@ -427,7 +439,8 @@ typedef struct {
     int causal;
     int64_t window;              /* 0 = none; needs causal */
     float scale;                 /* 0 = 1 / sqrt(head_dim) */
-    int64_t max_q;               /* no sequence has more query rows (more latch QE_ERR_INVALID_ARG and are left out) */
+    int64_t max_q;               /* no sequence has more query rows (more latch QE_ERR_INVALID_ARG and are left as
+                                  * they were); 0: nothing is done */
     int64_t max_kv;              /* about the longest kv_len: plans the work, right or not */
     const int32_t *q_start;      /* device, seqs + 1 values, ascending */
     const int32_t *kv_len;       /* device, seqs values */

@@ -7,8 +7,8 @@
 // move whole words.  A group's minimum and maximum meet in shuffles.  Bound by HBM: 2 +
 // 0.5 + 4 / G bytes for each 16-bit channel.  Measured: 32768 tokens, 8 heads of 128, read
 // back in 37 us (4.6 TB/s, kernel and call); 16384 tokens, 32 heads of 128, written in 119
-// us (2.9 TB/s: minima, maxima and rounding bound it, one exact rounding and one code a
-// channel) and read in 64 (5.4 TB/s).  A few tokens take 2 to 4 us on the GPU.
+// us (2.9 TB/s: minima, maxima, one exact rounding and one code a channel fill 75% of the
+// issue slots) and read in 64 (5.4 TB/s).  A few tokens take 2 to 4 us on the GPU.
 #include <cuda_fp16.h>
 
 #include <type_traits>
