@@ -428,8 +428,9 @@ qe_status qe_cache_read(const qe_cache *cache, const int64_t *slots, int64_t tok
  * and channel groups of other sizes do not enter.  What ends that is fp16's range: of
  * probability times the token's largest value scale, what is 2^-21 below the greatest
  * of its row keeps fewer bits and what is 2^-31 below adds nothing (2^-9 and 2^-20 where
- * value scales differ by up to 2^12, beyond which tokens are kept apart); with more
- * than 32 pairs, keys and channel groups of values 2^-24 below the largest of 32 tokens.
+ * value scales differ by up to 2^12, beyond which tokens are kept apart; a token of zeros
+ * counts with its neighbours' scale); with more than 32 pairs, keys and channel groups of
+ * values 2^-24 below the largest of 32 tokens.
  * Value scales outside 2^-47 .. 2^41 are correct, but slow, up to 32 pairs.
  */
 typedef struct {
