@@ -42,12 +42,12 @@ typedef enum {
     QE_ERR_INVALID_ARG = 1,   /* bad size, pointer, alignment or option; an index found out of range on the device */
     QE_ERR_CUDA = 2,          /* a CUDA runtime/driver call failed */
     QE_ERR_OOM = 3,           /* workspace allocation failed or too small */
-    QE_ERR_NUMERIC = 4,       /* non-finite value in W, Sigma, K or V (device-detected) */
+    QE_ERR_NUMERIC = 4,       /* non-finite value in W, Sigma, K, V or a layer's grids (device-detected) */
     QE_ERR_TIMEOUT = 5,       /* a bounded device-side wait gave up (device-detected) */
     QE_ERR_UNSUPPORTED = 6    /* option or layout not implemented */
 } qe_status;
 
-typedef enum { QE_F32 = 0, QE_BF16 = 1, QE_F16 = 2 /* the key/value cache only */ } qe_dtype;
+typedef enum { QE_F32 = 0, QE_BF16 = 1, QE_F16 = 2 /* not in quantization */ } qe_dtype;
 
 typedef enum {
     QE_FEATURE_MAJOR = 0,     /* X is p x n row-major: the paper's X (Sec. 2.1) */
@@ -469,6 +469,204 @@ qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention
 qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, const void *Q, int64_t q_row, int64_t q_head,
                              void *out, int64_t o_row, int64_t o_head, qe_dtype dtype, float *lse, void *workspace,
                              size_t workspace_bytes, qe_stream_t stream);
+
+/*
+ * Pages, slots and positions for the tokens that a batch of sequences appends to
+ * the cache, worked out on the GPU from their lengths (nothing is read back, so
+ * that a captured step keeps its books by itself).
+ *
+ * Free pages wait in a ring: ring[(first + i) mod pages], i < count, in the order
+ * in which they are taken.  Sequence b holds kv_len[b] tokens in the pages of its
+ * row of the page table.  Where ends[b] is not 0 the sequence is over: its pages
+ * behind the prefix go to the ring's end (sequences in order, a sequence's pages in
+ * order; they can be taken from the next call on), and its place begins anew with
+ * the `prefix` tokens that all sequences share, whose pages are never taken or given
+ * back.  Then it takes new_tokens[b] tokens:
+ *     l = ends[b] ? prefix : kv_len[b],   kv_len_out[b] = l + new_tokens[b];
+ * pages ceil(l / P) .. ceil(kv_len_out[b] / P) - 1 come from the ring's front and
+ * are written to page_table[b], sequences in order.  The batch's tokens follow one
+ * another, sequence b's from q_start[b] on:
+ *     positions[q_start[b] + i] = l + i,
+ *     slots[q_start[b] + i] = page_table[b][(l + i) / P] * P + (l + i) mod P,
+ * and entries behind the last token are -1 (slots: qe_cache_append skips them) and
+ * 0 (positions).
+ * All or nothing: where a length is negative or does not fit the page table's row,
+ * tokens do not fit max_tokens, the ring has too few pages or would get more than
+ * `pages`, or its state is out of range, QE_ERR_INVALID_ARG is latched, q_start is
+ * all 0, slots all -1, positions all 0, and lengths, table and ring stay as they are.
+ */
+typedef struct {
+    int64_t seqs;                /* 1 .. 65535 */
+    int64_t max_tokens;          /* entries of slots and positions, 0 .. 2^30 */
+    int64_t prefix;              /* tokens that all sequences share: a multiple of page_size, 0 .. 2^30 */
+    int64_t table_ld;            /* pages a row of page_table, and the distance of rows; up to 2^30 tokens */
+    const int32_t *new_tokens;   /* device, seqs */
+    const uint8_t *ends;         /* device, seqs, or NULL: none */
+    const int32_t *kv_len;       /* device, seqs */
+    int32_t *kv_len_out;         /* device, seqs; may be kv_len */
+    int32_t *page_table;         /* device, seqs x table_ld, in and out */
+    int32_t *ring;               /* device, the cache's `pages` entries, in and out */
+    const int32_t *state;        /* device, {first, count} */
+    int32_t *state_out;          /* device, {first, count}; may be state */
+    int32_t *q_start;            /* device, seqs + 1, out: as qe_attention takes it */
+    int64_t *slots;              /* device, max_tokens, out: as qe_cache_append takes them */
+    int32_t *positions;          /* device, max_tokens, out, or NULL */
+} qe_growth;
+
+/* Bytes of workspace that qe_cache_grow needs for so many sequences or fewer. */
+qe_status qe_cache_grow_workspace(int64_t seqs, size_t *bytes);
+
+/*
+ *   cache      pages and page_size count; its data is not touched.
+ *   workspace  device, 256-byte aligned; NULL: allocated and freed on `stream`
+ *              inside the call.  Not used across calls, need not be initialised.
+ * No two arrays overlap but kv_len with kv_len_out and state with state_out (each
+ * then the same array).  Asynchronous on `stream`.
+ */
+qe_status qe_cache_grow(const qe_cache *cache, const qe_growth *growth, void *workspace, size_t workspace_bytes,
+                        qe_stream_t stream);
+
+/*
+ * The rotation of queries and keys by their positions.  Pair i of a head's first
+ * 2 * pairs channels, i and i + pairs (or 2 i and 2 i + 1 with interleaved = 1),
+ * turns by the angle position * inv_freq[i]:
+ *     (a, b) -> (a cos - b sin, b cos + a sin).
+ * qe_rope_init fills the structure (on the host; no CUDA call).  Frequencies are
+ * held as fractions of a turn in 64 bits, so that position * frequency is a product
+ * of integers modulo one turn: far positions lose nothing.
+ *   inv_freq  host, `pairs` finite doubles, radians per position (for a base theta:
+ *             theta^(-i / pairs)).
+ * QE_ERR_INVALID_ARG for pairs outside 1 .. 128 or a frequency that is not finite.
+ */
+typedef struct {
+    int pairs;
+    int interleaved;
+    uint64_t turns[128];         /* inv_freq / (2 pi) modulo 1, times 2^64 */
+} qe_rope;
+
+qe_status qe_rope_init(const double *inv_freq, int pairs, int interleaved, qe_rope *rope);
+
+/*
+ * Norms of queries and keys, each head by itself, and their rotation in the same pass:
+ *     x <- x w / sqrt(mean(x^2) + eps)        where a weight is given,
+ *     then the rotation                       where `rope` is given,
+ * computed in binary32 and rounded once to dtype.  (bf16 and fp32 squares above
+ * 2^127 overflow, as the formula says in binary32.)
+ */
+typedef struct {
+    int64_t tokens;
+    int q_heads, k_heads;        /* 0: no queries (no keys) */
+    int head_dim;                /* a multiple of 8, 8 .. 256 */
+    qe_dtype dtype;              /* of Q, K and their results: fp32, bf16 or fp16 */
+    qe_dtype weight_dtype;       /* of the weights */
+    const void *Q, *K;           /* device: token i's head h at Q + i * q_token + h * q_head (elements; channels contiguous) */
+    int64_t q_token, q_head, k_token, k_head;
+    void *q_out, *k_out;         /* may be Q (K) itself, with the same strides */
+    int64_t qo_token, qo_head, ko_token, ko_head;
+    const void *q_weight, *k_weight;   /* device, head_dim each; NULL: not normed */
+    float eps;                   /* >= 0 */
+    const int32_t *positions;    /* device, tokens; a negative one leaves the token's results as they were */
+    const qe_rope *rope;         /* host, 2 * pairs <= head_dim; NULL: not rotated (positions may then be NULL) */
+} qe_heads;
+
+/* Asynchronous on `stream`; allocates nothing.  `rope` has been read when the call returns. */
+qe_status qe_norm_rotate(const qe_heads *heads, qe_stream_t stream);
+
+/*
+ * Products with a quantized layer: Y = act(X What^T + bias) + residual, with
+ * What_ij = scales_ig (codes_ij - zeros_ig) as qe_quantize_layer leaves it.
+ *
+ * qe_linear_pack lays a layer out once, in the library's own order: `bits` bits a
+ * code (5, 6 and 7 take 8), a scale and a zero for each row and group.
+ *   data        device, 256-byte aligned, qe_linear_size() bytes, owned by the caller.
+ *   q, p        outputs and inputs, 1 .. 2^24 each.
+ *   bits        2 .. 8.
+ *   group_size  columns a grid: 0 (or >= p) = one grid per row, else a multiple of 64.
+ */
+typedef struct {
+    void *data;
+    size_t bytes;
+    int64_t q, p;
+    int bits;
+    int64_t group_size;
+} qe_layer;
+
+/* Bytes of a layer's data. */
+qe_status qe_linear_size(int64_t q, int64_t p, int bits, int64_t group_size, size_t *bytes);
+
+/*
+ * Writes layer->data.
+ *   codes          device, q x p uint8, leading dimension ldc >= p; their low `bits` bits count.
+ *   scales, zeros  device, fp32, q x ceil(p / group_size) (q with one grid per row).
+ * A scale that is not finite, or a zero that is not a whole number of 0 .. 2^bits - 1,
+ * latches QE_ERR_NUMERIC, and every result of that row is NaN.
+ * Asynchronous on `stream`; allocates nothing.
+ */
+qe_status qe_linear_pack(const qe_layer *layer, const uint8_t *codes, int64_t ldc, const float *scales, const float *zeros,
+                         qe_stream_t stream);
+
+typedef enum {
+    QE_ACT_NONE = 0,
+    QE_ACT_RELU = 1,
+    QE_ACT_GELU = 2,             /* y Phi(y), with erf */
+    QE_ACT_GELU_TANH = 3,        /* y / 2 (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) */
+    QE_ACT_SILU = 4              /* y / (1 + exp(-y)) */
+} qe_activation;
+
+/*
+ * Codes less zeros are whole numbers that both 16-bit types hold exactly, so products
+ * are exact; sums, scales and the rest are binary32, rounded once to dtype.  Sums of
+ * (codes - zeros) x have to stay inside binary32's range.
+ */
+typedef struct {
+    int64_t rows;                /* 0: nothing is done */
+    qe_dtype dtype;              /* of X, residual and Y: bf16 or fp16 (fp32 is QE_ERR_UNSUPPORTED) */
+    qe_dtype bias_dtype;
+    const void *X;               /* device, rows x p, leading dimension ldx >= p; where it and ldx are multiples of 16
+                                  * bytes the loads are wide */
+    int64_t ldx;
+    const void *bias;            /* device, q values, or NULL */
+    qe_activation act;
+    const void *residual;        /* device, rows x q, leading dimension ldr >= q, or NULL; may be Y with ldr = ldy */
+    int64_t ldr;
+    void *Y;                     /* device, rows x q, leading dimension ldy >= q */
+    int64_t ldy;
+} qe_product;
+
+/* Bytes of workspace that qe_linear needs at most for so many rows or fewer, whatever X's alignment. */
+qe_status qe_linear_workspace(const qe_layer *layer, int64_t rows, size_t *bytes);
+
+/*
+ *   workspace  device, 256-byte aligned; NULL: allocated and freed on `stream` inside
+ *              the call, where any is needed.  Not used across calls, need not be
+ *              initialised.
+ * Y overlaps neither X nor the layer.  Asynchronous on `stream`.
+ */
+qe_status qe_linear(const qe_layer *layer, const qe_product *product, void *workspace, size_t workspace_bytes,
+                    qe_stream_t stream);
+
+/*
+ * Attention as qe_cache_attention, for a batch whose sequences begin with the same
+ * `prefix` tokens: these lie in prefix_pages, are read once for all sequences' rows
+ * together, and join each sequence's own tokens behind them.  Token j of a sequence
+ * is in prefix_pages[j / page_size] for j < prefix and in page_table[b][j / page_size]
+ * from there on (a prefix may end inside a page: the sequence's table then has a page
+ * of its own for that place, whose first tokens are not looked at).  A sequence that does not
+ * reach past the prefix (kv_len[b] less its rows below `prefix`; without `causal`,
+ * kv_len[b] below it), such as an idle place of the batch, has all its tokens in its page table.
+ *   prefix_pages  device, int32, ceil(prefix / page_size) page ids.
+ *   prefix        0 .. 2^30; 0 is qe_cache_attention.
+ *   max_kv        of `at`: about the longest kv_len, the prefix included.
+ * A window is QE_ERR_UNSUPPORTED.  Both parts' results meet in binary32, so that
+ * results are rounded as qe_cache_attention's.  Other arguments as there.
+ */
+qe_status qe_cache_attention_shared(const qe_cache *cache, const qe_attention *at, const int32_t *prefix_pages, int64_t prefix,
+                                    const void *Q, int64_t q_row, int64_t q_head, void *out, int64_t o_row, int64_t o_head,
+                                    qe_dtype dtype, float *lse, void *workspace, size_t workspace_bytes, qe_stream_t stream);
+
+/* Bytes of workspace that qe_cache_attention_shared needs at most on the current device, for this batch and for every
+ * one with no more seqs, rows, max_q, max_kv and prefix of the same cache and q_heads. */
+qe_status qe_cache_attention_shared_workspace(const qe_cache *cache, const qe_attention *at, int64_t prefix, size_t *bytes);
 
 /* Waits for `stream`, then returns and clears the error latched on the current
  * device, or QE_ERR_CUDA if the stream failed: QE_ERR_TIMEOUT, which leaves nothing

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(N) k_attend_join(const AttendArgs a, int unit,
         }
         if (on && team == 0) {
             const unsigned pr = first + row, q = pr / static_cast<unsigned>(a.per_kv);
-            finish(a, at.v.row0 + q, kvh * a.per_kv + static_cast<int>(pr - q * a.per_kv), d, v, big, sum);
+            finish(a, at.v, at.v.row0 + q, kvh * a.per_kv + static_cast<int>(pr - q * a.per_kv), d, v, big, sum);
         }
     }
 }
@@ -282,23 +282,47 @@ qe_status check_shape(const CacheGeom &g, const qe_attention *at) {
     return QE_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention *at, size_t *bytes) {
-    CacheGeom g;
-    if (!bytes) return QE_ERR_INVALID_ARG;
-    qe_status st = shape_geom(cache, &g);
-    if (st != QE_OK) return st;
-    if ((st = check_shape(g, at)) != QE_OK) return st;
-    *bytes = attend_most_bytes(g, *at);
-    return QE_OK;
+qe_status check_prefix(const qe_attention &at, int64_t prefix) {
+    if (prefix < 0 || prefix > (1 << 30)) return QE_ERR_INVALID_ARG;
+    return prefix > 0 && at.window > 0 ? QE_ERR_UNSUPPORTED : QE_OK;
 }
 
-qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, const void *Q, int64_t q_row, int64_t q_head,
-                             void *out, int64_t o_row, int64_t o_head, qe_dtype dtype, float *lse, void *workspace,
-                             size_t workspace_bytes, qe_stream_t stream) {
+cudaError_t launch_plan(AttendArgs a, const AttendPlan &p, cudaStream_t s) {
+    a.rows_cap = p.rows_cap;
+    a.ctas = p.ctas;
+    a.items = p.items;
+    a.splits = p.splits;
+    a.min_units = p.min_units;
+    return p.tiles == 0 ? launch_attend_tiles(a, s) : p.warps == 8   ? launch_attend_whole8(a, p.tiles, s)
+           : p.warps == 4 ? launch_attend_whole4(a, p.tiles, s)
+                          : launch_attend_rows(a, p.tiles, s);
+}
+
+// The prefix's pass, all rows of the batch as one sequence's, and the one over what is behind it.
+qe_attention front_of(const qe_attention &at, int64_t prefix) {
+    qe_attention f = at;
+    f.seqs = 1;
+    f.max_q = at.rows;
+    f.max_kv = prefix;
+    f.causal = 0;
+    f.window = 0;
+    return f;
+}
+
+qe_attention back_of(const qe_attention &at, int64_t prefix) {
+    qe_attention b = at;
+    b.max_kv = at.max_kv > prefix ? at.max_kv - prefix : 0;
+    return b;
+}
+
+size_t first_bytes(const CacheGeom &g, const qe_attention &at) {
+    return static_cast<size_t>(round_up(at.rows * at.q_heads * (g.D + 2) * static_cast<int64_t>(sizeof(float)), 256));
+}
+
+// Attention, with `shared` tokens in prefix_pages before each sequence's own where these are given.
+qe_status attend(const qe_cache *cache, const qe_attention *at, const int32_t *prefix_pages, int64_t shared, const void *Q, int64_t q_row,
+                 int64_t q_head, void *out, int64_t o_row, int64_t o_head, qe_dtype dtype, float *lse, void *workspace,
+                 size_t workspace_bytes, qe_stream_t stream) {
     AttendArgs a{};
     qe_status st = cache_geom(cache, &a.g);
     if (st != QE_OK) return st;
@@ -337,36 +361,94 @@ qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, cons
     a.lse = lse;
     a.err = device_error_word();
     if (!a.err) return QE_ERR_CUDA;
-    const AttendPlan p = attend_plan(a.g, *at);
-    a.rows_cap = p.rows_cap;
-    a.ctas = p.ctas;
-    a.items = p.items;
-    a.splits = p.splits;
-    a.min_units = p.min_units;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const size_t need = attend_bytes(p, a.g);
+    const int64_t prefix = prefix_pages ? shared : 0;
+    const AttendPlan p = attend_plan(a.g, back_of(*at, prefix));
+    AttendPlan p1{};
+    if (prefix > 0) p1 = attend_plan(a.g, front_of(*at, prefix));
+    // the workers' unfinished items, of either pass, lie behind what the first pass leaves
+    const size_t kept = prefix > 0 ? first_bytes(a.g, *at) : 0;
+    size_t need = attend_bytes(p, a.g);
+    if (prefix > 0 && attend_bytes(p1, a.g) > need) need = attend_bytes(p1, a.g);
+    need += kept;
     void *own = nullptr;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
     if (need > 0) {
         if (workspace) {
             if (workspace_bytes < need) return QE_ERR_OOM;
-            a.part = static_cast<float *>(workspace);
         } else {
             if (cudaMallocAsync(&own, need, s) != cudaSuccess) {
                 cudaGetLastError();
                 return QE_ERR_OOM;
             }
-            a.part = static_cast<float *>(own);
+            ws = static_cast<uint8_t *>(own);
         }
+        a.part = reinterpret_cast<float *>(ws + kept);
     }
-    const cudaError_t e = p.tiles == 0 ? launch_attend_tiles(a, s) : p.warps == 8   ? launch_attend_whole8(a, p.tiles, s)
-                          : p.warps == 4 ? launch_attend_whole4(a, p.tiles, s)
-                                         : launch_attend_rows(a, p.tiles, s);
+    cudaError_t e = cudaSuccess;
+    if (prefix > 0) {
+        a.prefix = static_cast<int>(prefix);
+        a.first = reinterpret_cast<float *>(ws);
+        AttendArgs f = a;
+        f.first_pass = 1;
+        f.batch_seqs = at->seqs;
+        f.seqs = 1;
+        f.max_q = at->rows;
+        f.causal = 0;
+        f.table = prefix_pages;
+        f.table_ld = ceil_div(prefix, int64_t{1} << a.g.page_shift);
+        e = launch_plan(f, p1, s);
+    }
+    if (e == cudaSuccess) e = launch_plan(a, p, s);
     if (own) cudaFreeAsync(own, s);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return QE_ERR_CUDA;
     }
     return QE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+qe_status qe_cache_attention_workspace(const qe_cache *cache, const qe_attention *at, size_t *bytes) {
+    CacheGeom g;
+    if (!bytes) return QE_ERR_INVALID_ARG;
+    qe_status st = shape_geom(cache, &g);
+    if (st != QE_OK) return st;
+    if ((st = check_shape(g, at)) != QE_OK) return st;
+    *bytes = attend_most_bytes(g, *at);
+    return QE_OK;
+}
+
+qe_status qe_cache_attention(const qe_cache *cache, const qe_attention *at, const void *Q, int64_t q_row, int64_t q_head,
+                             void *out, int64_t o_row, int64_t o_head, qe_dtype dtype, float *lse, void *workspace,
+                             size_t workspace_bytes, qe_stream_t stream) {
+    return attend(cache, at, nullptr, 0, Q, q_row, q_head, out, o_row, o_head, dtype, lse, workspace, workspace_bytes, stream);
+}
+
+qe_status qe_cache_attention_shared_workspace(const qe_cache *cache, const qe_attention *at, int64_t prefix, size_t *bytes) {
+    CacheGeom g;
+    if (!bytes) return QE_ERR_INVALID_ARG;
+    qe_status st = shape_geom(cache, &g);
+    if (st != QE_OK) return st;
+    if ((st = check_shape(g, at)) != QE_OK) return st;
+    if ((st = check_prefix(*at, prefix)) != QE_OK) return st;
+    const size_t back = attend_most_bytes(g, *at), front = attend_most_bytes(g, front_of(*at, prefix));   // (a shorter prefix leaves more)
+    *bytes = (back > front ? back : front) + first_bytes(g, *at);
+    return QE_OK;
+}
+
+qe_status qe_cache_attention_shared(const qe_cache *cache, const qe_attention *at, const int32_t *prefix_pages, int64_t prefix,
+                                    const void *Q, int64_t q_row, int64_t q_head, void *out, int64_t o_row, int64_t o_head,
+                                    qe_dtype dtype, float *lse, void *workspace, size_t workspace_bytes, qe_stream_t stream) {
+    if (!at) return QE_ERR_INVALID_ARG;
+    const qe_status st = check_prefix(*at, prefix);
+    if (st != QE_OK) return st;
+    if (prefix > 0 && (!prefix_pages || (reinterpret_cast<uintptr_t>(prefix_pages) & 3u) != 0)) return QE_ERR_INVALID_ARG;
+    return attend(cache, at, prefix > 0 ? prefix_pages : nullptr, prefix, Q, q_row, q_head, out, o_row, o_head, dtype, lse, workspace,
+                  workspace_bytes, stream);
 }
 
 }  // extern "C"

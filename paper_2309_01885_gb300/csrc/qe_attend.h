@@ -30,6 +30,12 @@ struct AttendArgs {
     int min_units;            // a worker (or a piece) takes at least this many
     int splits;               // tiles of 128 rows: pieces of an item's tokens
     float *part;              // unfinished items: [2 ctas][rows_cap x D sums, rows_cap maxima, rows_cap totals]
+    // a prefix that sequences share (0 tokens: none): first its own pass, with every sequence's rows as one sequence's,
+    // leaves sums, maxima and totals in `first`; then each sequence's tokens behind it, joined with these on the way out
+    int prefix;
+    int first_pass;
+    int64_t batch_seqs;       // in the first pass: sequences of the batch (seqs is 1)
+    float *first;             // [rows x q_heads][D] sums, [rows x q_heads] maxima, [rows x q_heads] totals
     unsigned *err;
 };
 
@@ -37,10 +43,19 @@ struct AttendArgs {
 struct SeqView {
     int64_t row0;             // first query row
     int n, len;               // query rows, cached tokens
+    int from;                 // tokens that the first pass has seen to
 };
 
 __device__ __forceinline__ SeqView seq_view(const AttendArgs &a, int64_t b, bool report) {
     SeqView v;
+    if (a.first_pass) {                                   // (what is wrong with the batch is reported by the second one)
+        const int64_t r0 = max(a.q_start[0], 0), r1 = min(static_cast<int64_t>(a.q_start[a.batch_seqs]), a.rows);
+        v.row0 = r0 < a.rows ? r0 : a.rows;
+        v.n = static_cast<int>(r1 > v.row0 ? r1 - v.row0 : 0);
+        v.len = a.prefix;
+        v.from = 0;
+        return v;
+    }
     int64_t r0 = a.q_start[b], r1 = a.q_start[b + 1];
     int64_t len = a.kv_len[b];
     bool bad = false;
@@ -59,12 +74,13 @@ __device__ __forceinline__ SeqView seq_view(const AttendArgs &a, int64_t b, bool
     v.row0 = r0;
     v.n = static_cast<int>(r1 - r0);
     v.len = static_cast<int>(len);
+    v.from = a.prefix > 0 && v.len - (a.causal ? v.n : 0) >= a.prefix ? a.prefix : 0;   // all its rows see all of the prefix
     return v;
 }
 
 // Tokens that query rows i0 .. i1 (of n) see between them: [lo, hi), empty if hi <= lo.
 __device__ __forceinline__ void visible(const AttendArgs &a, const SeqView &v, int i0, int i1, int &lo, int &hi) {
-    lo = 0;
+    lo = v.from;              // (with a window there is no prefix)
     hi = v.len;
     if (a.causal) {
         const int last = v.len - v.n + i1 + 1;

@@ -145,8 +145,36 @@ __device__ __forceinline__ void q_powers(float big, float &down, float &up) {
     up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
-// Four channels of a finished row, from the unnormalised sums relative to the maximum `m` (log2 units).
-__device__ __forceinline__ void finish(const AttendArgs &a, int64_t row, int head, int d, const float4 &v, float m, float l) {
+// Where the first pass keeps a row's head: sums, and the offsets of maxima and totals behind all of them.
+struct First {
+    float *sums, *most, *total;
+};
+
+__device__ __forceinline__ First first_of(const AttendArgs &a, int64_t row, int head) {
+    const int64_t all = a.rows * a.q_heads, at = row * a.q_heads + head;
+    float *stats = a.first + all * a.g.D;
+    return First{a.first + at * a.g.D, stats + at, stats + all + at};
+}
+
+// Four channels of a finished row of the sequence, from the unnormalised sums relative to the maximum `m` (log2 units).
+__device__ __forceinline__ void finish(const AttendArgs &a, const SeqView &sv, int64_t row, int head, int d, float4 v, float m, float l) {
+    if (a.first_pass) {
+        const First f = first_of(a, row, head);
+        *reinterpret_cast<float4 *>(f.sums + d) = v;
+        if (d == 0) {
+            *f.most = m;
+            *f.total = l;
+        }
+        return;
+    }
+    if (sv.from > 0) {                                    // what the prefix adds
+        const First f = first_of(a, row, head);
+        const float4 u = *reinterpret_cast<const float4 *>(f.sums + d);
+        const float most = *f.most, top = fmaxf(m, most), mine = ex2(m - top), its = ex2(most - top);
+        v = make_float4(fmaf(its, u.x, mine * v.x), fmaf(its, u.y, mine * v.y), fmaf(its, u.z, mine * v.z), fmaf(its, u.w, mine * v.w));
+        l = fmaf(its, *f.total, mine * l);
+        m = top;
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;       // a row that sees nothing is zero; NaN stays
     uint16_t *to = reinterpret_cast<uint16_t *>(a.out) + row * a.o_row + head * a.o_head + d;
     uint2 w;

@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
                 }
             } else if (d < a.g.dim) {
                 const unsigned pr = first + row, i = pr / static_cast<unsigned>(a.per_kv);
-                finish(a, sv.row0 + i, kvh * a.per_kv + static_cast<int>(pr - i * a.per_kv), d, v, big, sum);
+                finish(a, sv, sv.row0 + i, kvh * a.per_kv + static_cast<int>(pr - i * a.per_kv), d, v, big, sum);
             }
         }
         pos += take;

@@ -784,7 +784,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
         if (i < tiles) {
             float *slot = a.part + (static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x) * a.splits * (2 * kTile * (D + 2)) +
                           static_cast<int64_t>(blockIdx.y) * (2 * kTile * (D + 2));
+            const bool store = a.first_pass && pieces == 1, joins = sv.from > 0 && pieces == 1;
+            const First its = store || joins ? first_of(a, sv.row0 + qi, head) : First{nullptr, nullptr, nullptr};
+            float mine = 1.0f, theirs = 0.0f;             // factors of the sums and of the prefix's
+            if (joins) {
+                const float top = fmaxf(m, *its.most);
+                mine = ex2(m - top);
+                theirs = ex2(*its.most - top);
+                l = fmaf(theirs, *its.total, mine * l);
+                m = top;
+            }
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees nothing is zero; NaN stays
+            mine *= inv;
+            theirs *= inv;
             // whole rows go through shared memory (every product has been taken, Q's place is free) and out
             // LR lanes to a row: a thread's own row would be 8 to 16 bytes a line in each store
             uint8_t *stage = sq + i * F::Q_BYTES + quad * 32 * (F::DQ * 2);
@@ -797,18 +809,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0.0f;
                 }
-                if (pieces > 1) {
+                if (pieces > 1 || store) {
+                    float *to_row = store ? its.sums : slot + p * D;
                     if (on)
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<float4 *>(slot + p * D + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                            *reinterpret_cast<float4 *>(to_row + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                 } else {
+                    if (joins) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 u = on ? *reinterpret_cast<const float4 *>(its.sums + 32 * c + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            v[e] = fmaf(theirs, u.x, mine * v[e]);
+                            v[e + 1] = fmaf(theirs, u.y, mine * v[e + 1]);
+                            v[e + 2] = fmaf(theirs, u.z, mine * v[e + 2]);
+                            v[e + 3] = fmaf(theirs, u.w, mine * v[e + 3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] *= inv;
+                    }
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         uint32_t w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float x = v[e + 2 * k] * inv, y = v[e + 2 * k + 1] * inv;
+                            const float x = v[e + 2 * k], y = v[e + 2 * k + 1];
                             w[k] = a.half ? pack_f16(x, y) : pack_bf16(x, y);
                         }
                         *reinterpret_cast<uint4 *>(stage + lane * (F::DQ * 2) + (((4 * c + e / 8) ^ (lane & (LR - 1))) << 4)) =
@@ -816,7 +842,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                     }
                 }
             }
-            if (pieces == 1) {
+            if (store) {
+                if (on && grp == 0) {
+                    *its.most = m;
+                    *its.total = l;
+                }
+            } else if (pieces == 1) {
                 if (on && a.lse && grp == 0)
                     a.lse[(sv.row0 + qi) * a.q_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945309f;
                 asm volatile("bar.sync %0, 256;" ::"r"(9 + i) : "memory");
@@ -884,7 +915,7 @@ __global__ void __launch_bounds__(256) k_attend_join_tiles(const AttendArgs a) {
             v = make_float4(fmaf(f, u.x, v.x), fmaf(f, u.y, v.y), fmaf(f, u.z, v.z), fmaf(f, u.w, v.w));
         }
         const unsigned pr = first + row, q = pr / static_cast<unsigned>(a.per_kv);
-        finish(a, sv.row0 + q, kvh * a.per_kv + static_cast<int>(pr - q * a.per_kv), d, v, big, sum);
+        finish(a, sv, sv.row0 + q, kvh * a.per_kv + static_cast<int>(pr - q * a.per_kv), d, v, big, sum);
     }
 }
 

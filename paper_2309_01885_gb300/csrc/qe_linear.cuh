@@ -1,0 +1,214 @@
+// A quantized layer as products take it: the layout of its bytes, and turning codes into
+// matrix operands.
+//
+// Codes come in units of 16 rows x 64 columns, a row tile's units one after the other, so
+// that whoever walks along a row tile reads one stream.  A unit has B words for each of 32
+// lanes (B bits a code: 2, 3, 4 or 8).  Lane 4 r + t holds rows r and r + 8 (half h = 0, 1),
+// of either 32-column chunk c = 0, 1 the eight columns 8 t .. 8 t + 7: four pairs p, each in
+// the low bits of a word's two halves once shifted, which is where the m16n8k16 operand and a
+// 16-byte piece of a row of an operand tile both want them (columns are summed over, so
+// an operand's columns may stand in any order that both operands share).
+//   B = 2  word c, bits 2 (4 h + p);   B = 4  word 2 c + h, bits 4 p;
+//   B = 8  word 4 c + 2 h + p / 2, bits 8 (p mod 2);
+//   B = 3  pairs i = 8 c + 4 h + p: word i / 5, bits 3 (i mod 5); i = 15 takes the bit that each
+//          half has left over, bit j of its code in word j: 32 codes in 96 bits.
+// (Bits are those of the pair's first column; its second column's are 16 above.)
+// Behind the codes lie scales (fp32) and zeros (one byte), 16 to a row tile and group.
+//
+// c - z is exact in both 16-bit types.  A code below the leading bit of 2^7 (bf16) or 2^10
+// (fp16) makes 2^7 + c 2^s by or-ing alone; one fused multiply-add takes s and the zero out.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "../../include/qe.h"
+#include "qe_common.cuh"
+
+namespace qe {
+
+constexpr int kUnitCols = 64, kTileRows = 16;
+
+struct LinearGeom {
+    const uint8_t *codes;
+    const float *scales;
+    const uint8_t *zeros;
+    int64_t q, p;
+    int bits;                 // as stored: 2, 3, 4 or 8
+    int units;                // of a row tile
+    int row_tiles;
+    int groups, group_units;  // grids of a row; units that share one
+};
+
+struct LinearArgs {
+    LinearGeom g;
+    const void *x;
+    int64_t ldx, rows;
+    int half;                 // fp16, else bf16
+    int x_vec;                // 16-byte loads of x are aligned
+    const void *bias;
+    int bias_dtype;
+    int act;
+    const void *residual;
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+    unsigned *err;
+};
+
+__host__ __device__ constexpr int stored_bits(int bits) { return bits <= 4 ? bits : 8; }
+
+// Word of a lane's B and place in a unit's words.
+__host__ __device__ constexpr int unit_word(int B, int lane, int j) {
+    return B == 3 ? 32 * j + lane : B == 8 ? 128 * (j >> 2) + 4 * lane + (j & 3) : B * lane + j;
+}
+
+template <int B>
+__device__ __forceinline__ void load_unit(const uint8_t *unit, int lane, uint32_t (&w)[B]) {
+    if constexpr (B == 3) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[j]) : "l"(unit + 128 * j + 4 * lane));
+    } else if constexpr (B == 2) {
+        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(unit + 8 * lane));
+    } else {
+#pragma unroll
+        for (int j = 0; j < B; j += 4)
+            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[j]), "=r"(w[j + 1]), "=r"(w[j + 2]), "=r"(w[j + 3])
+                         : "l"(unit + 128 * j + 16 * lane));
+    }
+}
+
+// Pairs of 16-bit floats as words.
+template <bool HALF>
+struct Pairs {
+    static constexpr int kBase = HALF ? 1024 : 128;
+    static constexpr uint32_t kLead = HALF ? 0x64006400u : 0x43004300u;
+    static __device__ __forceinline__ uint32_t of(float v) {
+        if constexpr (HALF) {
+            const __half2 t = __float2half2_rn(v);
+            return *reinterpret_cast<const uint32_t *>(&t);
+        } else {
+            const __nv_bfloat162 t = __float2bfloat162_rn(v);
+            return *reinterpret_cast<const uint32_t *>(&t);
+        }
+    }
+    static __device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) {
+        if constexpr (HALF) {
+            const __half2 t = __hadd2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+            return *reinterpret_cast<const uint32_t *>(&t);
+        } else {
+            const __nv_bfloat162 t = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+            return *reinterpret_cast<const uint32_t *>(&t);
+        }
+    }
+    static __device__ __forceinline__ uint32_t fma(uint32_t a, uint32_t b, uint32_t c) {
+        if constexpr (HALF) {
+            const __half2 t = __hfma2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&c));
+            return *reinterpret_cast<const uint32_t *>(&t);
+        } else {
+            const __nv_bfloat162 t = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b),
+                                             *reinterpret_cast<const __nv_bfloat162 *>(&c));
+            return *reinterpret_cast<const uint32_t *>(&t);
+        }
+    }
+};
+
+// How a type's pairs of B-bit codes are turned: positions 2^s a pair may stand at without a
+// shift (s = 0, S, 2 S below LEVELS S), each with its own constant -(base / 2^s + z).
+template <int B, bool HALF>
+struct Turn {
+    static constexpr int S = B;                                            // bits between neighbouring pairs
+    static constexpr int LEVELS = B == 8 ? 1 : HALF ? (B == 4 ? 2 : 3) : (B == 2 ? 3 : B == 3 ? 2 : 1);
+    using P = Pairs<HALF>;
+
+    static __device__ __forceinline__ void zero(float z, uint32_t (&k)[LEVELS]) {
+#pragma unroll
+        for (int i = 0; i < LEVELS; ++i) k[i] = P::of(B == 8 && !HALF ? -z : -(static_cast<float>(P::kBase >> (i * S)) + z));
+    }
+
+    // pair number j (from bit 0) of a word
+    static __device__ __forceinline__ uint32_t pair(uint32_t w, int j, const uint32_t (&k)[LEVELS]) {
+        constexpr uint32_t mask = B == 8 ? 0x00ff00ffu : ((1u << B) - 1u) * 0x00010001u;
+        if constexpr (B == 8) {
+            if constexpr (HALF) {
+                const uint32_t v = __byte_perm(w, 0x64646464u, j == 0 ? 0x4240 : 0x4341);   // 1024 + c
+                return P::add(v, k[0]);
+            } else {                                       // 16 upper + lower, both from 2^7
+                const uint32_t lo = ((j ? w >> 8 : w) & 0x000f000fu) | P::kLead, hi = ((w >> (4 + 8 * j)) & 0x000f000fu) | P::kLead;
+                const uint32_t l = P::add(lo, 0xC300C300u);                                  // less 128
+                const uint32_t h = P::fma(hi, 0x41804180u, 0xC500C500u);                     // times 16, less 2048
+                return P::add(P::add(h, l), k[0]);
+            }
+        } else {
+            const int level = j % LEVELS, shift = (j - level) * S;
+            const uint32_t v = ((w >> shift) & (mask << (level * S))) | P::kLead;
+            return level == 0 ? P::add(v, k[0]) : P::fma(v, P::of(1.0f / static_cast<float>(1 << (level * S))), k[level]);
+        }
+    }
+
+    // out[c][h][p]: c - z of the lane's pairs
+    static __device__ __forceinline__ void unit(const uint32_t (&w)[B], const uint32_t (&k)[2][LEVELS], uint32_t (&out)[2][2][4]) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    if constexpr (B == 2) out[c][h][p] = pair(w[c], 4 * h + p, k[h]);
+                    if constexpr (B == 4) out[c][h][p] = pair(w[2 * c + h], p, k[h]);
+                    if constexpr (B == 8) out[c][h][p] = pair(w[4 * c + 2 * h + (p >> 1)], p & 1, k[h]);
+                    if constexpr (B == 3) {
+                        const int i = 8 * c + 4 * h + p;
+                        if (i < 15) {
+                            out[c][h][p] = pair(w[i / 5], i % 5, k[h]);
+                        } else {
+                            const uint32_t v = ((w[0] >> 15) & 0x00010001u) | ((w[1] >> 14) & 0x00020002u) | ((w[2] >> 13) & 0x00040004u) | P::kLead;
+                            out[c][h][p] = P::add(v, k[h][0]);
+                        }
+                    }
+                }
+    }
+};
+
+__device__ __forceinline__ float to_f32(const void *p, int dtype, int64_t i) {
+    if (dtype == QE_F32) return static_cast<const float *>(p)[i];
+    if (dtype == QE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    return __half2float(static_cast<const __half *>(p)[i]);
+}
+
+__device__ __forceinline__ float activated(float y, int act) {
+    switch (act) {
+        case QE_ACT_RELU: return y < 0.0f ? 0.0f : y;      // NaN stays
+        case QE_ACT_GELU: return 0.5f * y * erfcf(-0.70710678118654752f * y);
+        case QE_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * fmaf(0.044715f * y * y, y, y);
+            return y / (1.0f + expf(-2.0f * u));           // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+        }
+        case QE_ACT_SILU: return y / (1.0f + expf(-y));
+        default: return y;
+    }
+}
+
+// A finished sum (scaled) of output i for row m: bias, activation, residual, one rounding.
+__device__ __forceinline__ float finished(const LinearArgs &a, float v, int64_t m, int64_t i, float bias) {
+    v = activated(v + bias, a.act);
+    if (a.residual) v += to_f32(a.residual, a.half ? QE_F16 : QE_BF16, m * a.ldr + i);
+    return v;
+}
+
+__device__ __forceinline__ void put(const LinearArgs &a, float v, int64_t m, int64_t i) {
+    if (a.half) static_cast<__half *>(a.y)[m * a.ldy + i] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(a.y)[m * a.ldy + i] = __float2bfloat16_rn(v);
+}
+
+// Checks a layer and fills the geometry; QE_ERR_INVALID_ARG / QE_ERR_UNSUPPORTED otherwise.
+qe_status linear_geom(const qe_layer *layer, LinearGeom *g);
+
+cudaError_t launch_linear_rows(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_rows_2(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_rows_3(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_rows_4(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_rows_8(const LinearArgs &a, cudaStream_t s);
+
+}  // namespace qe

@@ -1,0 +1,8 @@
+// Few-rows products with codes held in 3 bits.
+#include "qe_linear_rows.cuh"
+
+namespace qe {
+
+cudaError_t launch_linear_rows_3(const LinearArgs &a, cudaStream_t s) { return launch_rows_bits<3>(a, s); }
+
+}  // namespace qe

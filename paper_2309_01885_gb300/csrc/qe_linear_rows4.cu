@@ -1,0 +1,8 @@
+// Few-rows products with codes held in 4 bits.
+#include "qe_linear_rows.cuh"
+
+namespace qe {
+
+cudaError_t launch_linear_rows_4(const LinearArgs &a, cudaStream_t s) { return launch_rows_bits<4>(a, s); }
+
+}  // namespace qe

@@ -7,6 +7,7 @@ calls raise.  The function names are those of the C ABI.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -25,7 +26,10 @@ EXPORTED = ("qe_build_sigma", "qe_quantize_layer", "qe_quantize_layer_outlier",
             "qe_build_sigma_static", "qe_timer_create", "qe_timer_read", "qe_timer_reset",
             "qe_timer_destroy", "qe_build_sigma_host", "qe_pack_codes", "qe_unpack_codes",
             "qe_hard_threshold", "qe_hard_threshold_workspace", "qe_cache_size", "qe_cache_append",
-            "qe_cache_read", "qe_cache_attention", "qe_cache_attention_workspace")
+            "qe_cache_read", "qe_cache_attention", "qe_cache_attention_workspace", "qe_cache_grow",
+            "qe_cache_grow_workspace", "qe_rope_init", "qe_norm_rotate", "qe_linear_size", "qe_linear_pack",
+            "qe_linear_workspace", "qe_linear", "qe_cache_attention_shared", "qe_cache_attention_shared_workspace")
+QE_ACT_NONE, QE_ACT_RELU, QE_ACT_GELU, QE_ACT_GELU_TANH, QE_ACT_SILU = range(5)
 QE_KERNEL_PINIT_GEMM, QE_KERNEL_RESIDUAL_GEMM, QE_KERNEL_TRAIL_GEMM, QE_KERNEL_CD_BLOCK, \
     QE_KERNEL_CD_LISTS, QE_KERNEL_COUNT = range(6)
 
@@ -61,6 +65,43 @@ class QEAttention(ctypes.Structure):
                 ("causal", ctypes.c_int), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
                 ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64), ("q_start", ctypes.c_void_p),
                 ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("table_ld", ctypes.c_int64)]
+
+
+class QEGrowth(ctypes.Structure):
+    """Mirror of ``qe_growth``."""
+    _fields_ = [("seqs", ctypes.c_int64), ("max_tokens", ctypes.c_int64), ("prefix", ctypes.c_int64), ("table_ld", ctypes.c_int64),
+                ("new_tokens", ctypes.c_void_p), ("ends", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("kv_len_out", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("ring", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("state_out", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class QERope(ctypes.Structure):
+    """Mirror of ``qe_rope``."""
+    _fields_ = [("pairs", ctypes.c_int), ("interleaved", ctypes.c_int), ("turns", ctypes.c_uint64 * 128)]
+
+
+class QEHeads(ctypes.Structure):
+    """Mirror of ``qe_heads``."""
+    _fields_ = [("tokens", ctypes.c_int64), ("q_heads", ctypes.c_int), ("k_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("weight_dtype", ctypes.c_int), ("Q", ctypes.c_void_p), ("K", ctypes.c_void_p),
+                ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64), ("k_token", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("qo_token", ctypes.c_int64), ("qo_head", ctypes.c_int64),
+                ("ko_token", ctypes.c_int64), ("ko_head", ctypes.c_int64), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p)]
+
+
+class QELayer(ctypes.Structure):
+    """Mirror of ``qe_layer``."""
+    _fields_ = [("data", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("q", ctypes.c_int64), ("p", ctypes.c_int64),
+                ("bits", ctypes.c_int), ("group_size", ctypes.c_int64)]
+
+
+class QEProduct(ctypes.Structure):
+    """Mirror of ``qe_product``."""
+    _fields_ = [("rows", ctypes.c_int64), ("dtype", ctypes.c_int), ("bias_dtype", ctypes.c_int), ("X", ctypes.c_void_p),
+                ("ldx", ctypes.c_int64), ("bias", ctypes.c_void_p), ("act", ctypes.c_int), ("residual", ctypes.c_void_p),
+                ("ldr", ctypes.c_int64), ("Y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
 
 
 _lib = None
@@ -124,6 +165,26 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.qe_cache_attention_workspace.restype = st
     L.qe_cache_attention.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp, vp, ctypes.c_size_t, vp]
     L.qe_cache_attention.restype = st
+    L.qe_cache_grow_workspace.argtypes = [i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_cache_grow_workspace.restype = st
+    L.qe_cache_grow.argtypes = [vp, vp, vp, ctypes.c_size_t, vp]
+    L.qe_cache_grow.restype = st
+    L.qe_rope_init.argtypes = [ctypes.POINTER(ctypes.c_double), i32, i32, vp]
+    L.qe_rope_init.restype = st
+    L.qe_norm_rotate.argtypes = [vp, vp]
+    L.qe_norm_rotate.restype = st
+    L.qe_linear_size.argtypes = [i64, i64, i32, i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_linear_size.restype = st
+    L.qe_linear_pack.argtypes = [vp, vp, i64, vp, vp, vp]
+    L.qe_linear_pack.restype = st
+    L.qe_linear_workspace.argtypes = [vp, i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_linear_workspace.restype = st
+    L.qe_linear.argtypes = [vp, vp, vp, ctypes.c_size_t, vp]
+    L.qe_linear.restype = st
+    L.qe_cache_attention_shared_workspace.argtypes = [vp, vp, i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.qe_cache_attention_shared_workspace.restype = st
+    L.qe_cache_attention_shared.argtypes = [vp, vp, vp, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, ctypes.c_size_t, vp]
+    L.qe_cache_attention_shared.restype = st
     _lib = L
     return L
 
@@ -535,6 +596,11 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
         with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(cache._index):
             return qe_cache_attention(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal=causal, window=window, scale=scale,
                                       out=out, lse=lse, workspace=workspace)
+    return _attend(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal, window, scale, out, lse, workspace, None, 0)
+
+
+def _attend(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal, window, scale, out, lse, workspace, prefix_pages, prefix):
+    """qe_cache_attention, or with prefix_pages qe_cache_attention_shared, on the current device and stream."""
     rows, heads, dim = q.shape
     q0, q1 = _cache_heads(cache, q, heads, "q")
     if not page_table.is_contiguous():                   # the library's rows follow one another: a part of a wider table is copied
@@ -561,9 +627,286 @@ def qe_cache_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, k
         if workspace.get_device() != cache._index or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous tensor on the cache's device")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = (_lib or load()).qe_cache_attention(cache._ref, ctypes.addressof(at), q.data_ptr(), q0, q1, out.data_ptr(), o0, o1,
-                                             _cache_dtype(dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
-                                             _raw_stream(cache._index))
+    tail = (q.data_ptr(), q0, q1, out.data_ptr(), o0, o1, _cache_dtype(dtype), None if lse is None else lse.data_ptr(), ws, ws_bytes,
+            _raw_stream(cache._index))
+    if prefix_pages is None:
+        what = "qe_cache_attention"
+        st = (_lib or load()).qe_cache_attention(cache._ref, ctypes.addressof(at), *tail)
+    else:
+        what = "qe_cache_attention_shared"
+        pages = _cache_index(cache, prefix_pages, torch.int32, 1, "prefix_pages")
+        if prefix_pages.shape[0] * cache.page_size < prefix:
+            raise ValueError("prefix_pages holds a page for each page_size tokens of the prefix")
+        st = (_lib or load()).qe_cache_attention_shared(cache._ref, ctypes.addressof(at), pages, prefix, *tail)
     if st != QE_OK:
-        raise QEError(st, "qe_cache_attention")
+        raise QEError(st, what)
+    return out
+
+
+def qe_cache_attention_shared_workspace(cache: KVCache, seqs: int, q_heads: int, rows: int, max_q: int, max_kv: int, prefix: int, *,
+                                        causal: bool = True) -> int:
+    """Bytes of workspace that do for such a batch and for every one with no more sequences, rows, tokens and prefix."""
+    if _elsewhere(cache):
+        with torch.cuda.device(cache._index):
+            return qe_cache_attention_shared_workspace(cache, seqs, q_heads, rows, max_q, max_kv, prefix, causal=causal)
+    at = QEAttention(seqs=seqs, rows=rows, q_heads=q_heads, causal=causal, max_q=max_q, max_kv=max_kv)
+    n = ctypes.c_size_t(0)
+    _check(load().qe_cache_attention_shared_workspace(cache._ref, ctypes.addressof(at), prefix, ctypes.byref(n)),
+           "qe_cache_attention_shared_workspace")
+    return n.value
+
+
+def qe_cache_attention_shared(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+                              max_q: int, max_kv: int, prefix_pages: torch.Tensor, prefix: int, *, causal: bool = True,
+                              scale: float = 0.0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """qe_cache_attention for sequences that begin with the same `prefix` tokens, which lie in the pages prefix_pages
+    (int32) and are read once for all of them; page_table is looked up behind them only (and for sequences that do not
+    reach past the prefix).  kv_len and max_kv count the prefix.  workspace: optional uint8 tensor of
+    qe_cache_attention_shared_workspace() bytes.  Other arguments as for qe_cache_attention."""
+    if stream is not None or _elsewhere(cache):          # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(cache._index):
+            return qe_cache_attention_shared(cache, q, q_start, kv_len, page_table, max_q, max_kv, prefix_pages, prefix, causal=causal,
+                                             scale=scale, out=out, lse=lse, workspace=workspace)
+    return _attend(cache, q, q_start, kv_len, page_table, max_q, max_kv, causal, 0, scale, out, lse, workspace, prefix_pages, prefix)
+
+
+class PagePool:
+    """The free pages of a cache: a ring of page ids (`ring`, int32, one entry a page) and its `state` (int32: where its
+    front lies, how many pages wait).  Made here, every page is free, in order."""
+
+    def __init__(self, cache: KVCache, ring: torch.Tensor | None = None, state: torch.Tensor | None = None):
+        if ring is None:
+            ring = torch.arange(cache.pages, dtype=torch.int32, device=cache.device)
+        if state is None:
+            state = torch.tensor([0, cache.pages], dtype=torch.int32, device=cache.device)
+        for t, n, what in ((ring, cache.pages, "ring"), (state, 2, "state")):
+            _cache_index(cache, t, torch.int32, 1, what)
+            if t.shape[0] != n:
+                raise ValueError(f"{what}: expected {n} entries")
+        self.ring, self.state = ring, state
+
+
+def qe_cache_grow_workspace(seqs: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().qe_cache_grow_workspace(seqs, ctypes.byref(n)), "qe_cache_grow_workspace")
+    return n.value
+
+
+def qe_cache_grow(cache: KVCache, pool: PagePool, kv_len: torch.Tensor, new_tokens: torch.Tensor, page_table: torch.Tensor,
+                  max_tokens: int, *, ends: torch.Tensor | None = None, prefix: int = 0, kv_len_out: torch.Tensor | None = None,
+                  state_out: torch.Tensor | None = None, q_start: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                  positions: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> tuple:
+    """Pages, slots and positions for the new_tokens[b] (int32) tokens that each sequence appends behind its kv_len[b]
+    (int32): takes pages from the pool, enters them in page_table (int32 seqs x pages, contiguous, changed in place),
+    gives back those of sequences with ends[b] (uint8 or bool) set, which begin anew with the `prefix` tokens that all
+    share, and brings kv_len and the pool's state up to date (in place, or into kv_len_out / state_out).  Returns
+    (q_start, slots, positions): int32 seqs + 1, int64 and int32 max_tokens (entries behind the last token -1 and 0).
+    Nothing is read back; what does not fit changes nothing and is reported by qe_sync_status (include/qe.h)."""
+    if stream is not None or _elsewhere(cache):          # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(cache._index):
+            return qe_cache_grow(cache, pool, kv_len, new_tokens, page_table, max_tokens, ends=ends, prefix=prefix, kv_len_out=kv_len_out,
+                                 state_out=state_out, q_start=q_start, slots=slots, positions=positions, workspace=workspace)
+    seqs = kv_len.shape[0]
+
+    def index(t, dtype, n, what):
+        at = _cache_index(cache, t, dtype, 1, what)
+        if t.shape[0] != n:
+            raise ValueError(f"{what}: expected {n} entries")
+        return at
+
+    if not page_table.is_contiguous() or page_table.shape[0] != seqs:
+        raise ValueError("page_table: expected a contiguous tensor of seqs rows")
+    dev = cache.device
+    q_start = torch.empty(seqs + 1, dtype=torch.int32, device=dev) if q_start is None else q_start
+    slots = torch.empty(max_tokens, dtype=torch.int64, device=dev) if slots is None else slots
+    positions = torch.empty(max_tokens, dtype=torch.int32, device=dev) if positions is None else positions
+    if ends is not None and ends.dtype is torch.bool:
+        ends = ends.view(torch.uint8)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.get_device() != cache._index or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the cache's device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    lens, state = index(kv_len, torch.int32, seqs, "kv_len"), index(pool.state, torch.int32, 2, "state")
+    gr = QEGrowth(seqs, max_tokens, prefix, page_table.shape[-1], index(new_tokens, torch.int32, seqs, "new_tokens"),
+                  None if ends is None else index(ends, torch.uint8, seqs, "ends"), lens,
+                  lens if kv_len_out is None else index(kv_len_out, torch.int32, seqs, "kv_len_out"),
+                  _cache_index(cache, page_table, torch.int32, 2, "page_table"), index(pool.ring, torch.int32, cache.pages, "ring"), state,
+                  state if state_out is None else index(state_out, torch.int32, 2, "state_out"),
+                  index(q_start, torch.int32, seqs + 1, "q_start"), index(slots, torch.int64, max_tokens, "slots"),
+                  index(positions, torch.int32, max_tokens, "positions"))
+    st = (_lib or load()).qe_cache_grow(cache._ref, ctypes.addressof(gr), ws, ws_bytes, _raw_stream(cache._index))
+    if st != QE_OK:
+        raise QEError(st, "qe_cache_grow")
+    return q_start, slots, positions
+
+
+# ---- queries and keys: norms and rotation ---------------------------------------------------------------------------------
+
+class Rope:
+    """Frequencies of the rotation of a head's first rotary_dim channels: theta^(-2 i / rotary_dim) for pair i, or those of
+    inv_freq (radians per position).  Pair i is channels i and i + rotary_dim / 2, or 2 i and 2 i + 1 (interleaved)."""
+
+    def __init__(self, rotary_dim: int, theta: float = 10000.0, interleaved: bool = False, inv_freq=None):
+        if inv_freq is None:
+            if rotary_dim < 2 or rotary_dim % 2 or not theta > 0.0:
+                raise ValueError("rotary_dim is an even number of channels, theta above 0")
+            inv_freq = [theta ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+        inv_freq = [float(f) for f in inv_freq]
+        if 2 * len(inv_freq) != rotary_dim:
+            raise ValueError("inv_freq holds rotary_dim / 2 frequencies")
+        self.rotary_dim, self.interleaved, self._c = rotary_dim, interleaved, QERope()
+        _check(load().qe_rope_init((ctypes.c_double * len(inv_freq))(*inv_freq), len(inv_freq), int(interleaved),
+                                   ctypes.addressof(self._c)), "qe_rope_init")
+        self._ref = ctypes.addressof(self._c)
+
+
+def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tensor | None = None, rope: Rope | None = None, *,
+                   q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                   q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None) -> tuple:
+    """(q, k), tokens x heads x head_dim with any token and head strides, each head normed (x w / sqrt(mean x^2 + eps), where
+    a weight is given) and rotated by its token's position (int32; where a Rope is given; a negative one leaves the token's
+    results as they were).  Written into q_out and k_out where given (q and k themselves are allowed).  Either of q and k
+    may be None."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k is given")
+    index = first.get_device()
+    if stream is not None or (index >= 0 and _current_device() != index):   # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(index):
+            return qe_norm_rotate(q, k, positions, rope, q_weight=q_weight, k_weight=k_weight, eps=eps, q_out=q_out, k_out=k_out)
+    if first.dim() != 3:
+        raise ValueError("expected tokens x heads x head_dim")
+    n, dim, dtype = first.shape[0], first.shape[2], first.dtype
+    h = QEHeads(tokens=n, head_dim=dim, dtype=_cache_dtype(dtype), eps=eps)
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    for w in weights:
+        if w.shape != (dim,) or not w.is_contiguous() or w.get_device() != index or w.dtype is not weights[0].dtype:
+            raise ValueError("weights: expected contiguous tensors of head_dim entries on q's device, of one dtype")
+    if weights:
+        h.weight_dtype = _cache_dtype(weights[0].dtype)
+    if rope is not None:
+        if positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or not positions.is_contiguous() or \
+                positions.get_device() != index:
+            raise ValueError("positions: expected a contiguous int32 tensor of tokens entries on q's device")
+        h.positions, h.rope = positions.data_ptr(), rope._ref
+
+    def heads(t, what, like=None):
+        if t.dim() != 3 or t.shape[0] != n or t.shape[2] != dim or (t.stride(2) != 1 and dim > 1) or t.dtype is not dtype or \
+                t.get_device() != index or (like is not None and t.shape != like.shape):
+            raise ValueError(f"{what}: expected {n} x heads x {dim} with contiguous channels, of one dtype and device")
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    found = []
+    for name, t, out, w in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
+        if t is None:
+            if out is not None or w is not None:
+                raise ValueError(f"{name} is not given")
+            found.append(None)
+            continue
+        at, token, head = heads(t, name)
+        if out is None:
+            out = torch.empty(t.shape, dtype=dtype, device=t.device)
+        o_at, o_token, o_head = heads(out, name + "_out", t)
+        wp = None if w is None else w.data_ptr()
+        if name == "q":
+            h.q_heads, h.Q, h.q_token, h.q_head, h.q_out, h.qo_token, h.qo_head, h.q_weight = t.shape[1], at, token, head, o_at, o_token, o_head, wp
+        else:
+            h.k_heads, h.K, h.k_token, h.k_head, h.k_out, h.ko_token, h.ko_head, h.k_weight = t.shape[1], at, token, head, o_at, o_token, o_head, wp
+        found.append(out)
+    st = (_lib or load()).qe_norm_rotate(ctypes.addressof(h), _raw_stream(index))
+    if st != QE_OK:
+        raise QEError(st, "qe_norm_rotate")
+    return tuple(found)
+
+
+# ---- products with a quantized layer --------------------------------------------------------------------------------------
+
+ACTIVATIONS = {"none": QE_ACT_NONE, "relu": QE_ACT_RELU, "gelu": QE_ACT_GELU, "gelu_tanh": QE_ACT_GELU_TANH, "silu": QE_ACT_SILU}
+
+
+def qe_linear_size(q: int, p: int, bits: int, group_size: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().qe_linear_size(q, p, bits, group_size, ctypes.byref(n)), "qe_linear_size")
+    return n.value
+
+
+class QuantizedWeights:
+    """A quantized layer laid out for qe_linear: codes (q x p uint8), scales and zeros (fp32, q or q x groups) as
+    qe_quantize_layer returns them, with a grid for each row (group_size 0) or each group_size columns.  What is laid out
+    is held in `data` (a uint8 device tensor of qe_linear_size() bytes; allocated here when not given)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int, *, group_size: int = 0,
+                 data: torch.Tensor | None = None, stream=None):
+        q, p = codes.shape
+        groups = -(-p // group_size) if 0 < group_size < p else 1
+        if codes.dtype is not torch.uint8 or not codes.is_cuda:
+            raise ValueError("codes: expected a uint8 device tensor")
+        for t, what in ((scales, "scales"), (zeros, "zeros")):
+            if t.dtype is not torch.float32 or t.shape not in ((q, groups), (q,) if groups == 1 else (q, groups)) or not t.is_contiguous() \
+                    or t.device != codes.device:
+                raise ValueError(f"{what}: expected a contiguous fp32 tensor on the codes' device, {q} x {groups}")
+        need = qe_linear_size(q, p, bits, group_size)
+        with torch.cuda.device(codes.device), torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            if data is None:
+                data = torch.empty(need, dtype=torch.uint8, device=codes.device)
+            if data.device != codes.device or data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() < need:
+                raise ValueError(f"expected a contiguous uint8 tensor of at least {need} bytes on the codes' device")
+            self.q, self.p, self.bits, self.group_size, self.data, self.device = q, p, bits, group_size, data, data.device
+            self._c = QELayer(data.data_ptr(), data.numel(), q, p, bits, group_size)
+            self._ref, self._index = ctypes.addressof(self._c), data.get_device()
+            _check(load().qe_linear_pack(self._ref, _ptr(codes), _rowmajor_ld(codes), _ptr(scales), _ptr(zeros), _stream(None)),
+                   "qe_linear_pack")
+
+
+def qe_linear_workspace(weights: QuantizedWeights, rows: int) -> int:
+    """Bytes of workspace that do for so many rows or fewer."""
+    n = ctypes.c_size_t(0)
+    _check(load().qe_linear_workspace(weights._ref, rows, ctypes.byref(n)), "qe_linear_workspace")
+    return n.value
+
+
+def qe_linear(weights: QuantizedWeights, x: torch.Tensor, *, bias: torch.Tensor | None = None, activation: str = "none",
+              residual: torch.Tensor | None = None, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+              stream=None) -> torch.Tensor:
+    """act(x What^T + bias) + residual for x (rows x p, bf16 or fp16, rows any distance apart), in x's dtype.  bias: q values;
+    activation: none, relu, gelu, gelu_tanh or silu; residual: rows x q in x's dtype (`out` itself is allowed).  workspace:
+    optional uint8 tensor of qe_linear_workspace() bytes."""
+    index = weights._index
+    if stream is not None or (index >= 0 and _current_device() != index):   # what is made here belongs to the stream
+        with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(index):
+            return qe_linear(weights, x, bias=bias, activation=activation, residual=residual, out=out, workspace=workspace)
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation: one of {', '.join(ACTIVATIONS)}")
+    dtype, q, p = x.dtype, weights.q, weights.p
+    if x.dim() != 2 or x.shape[1] != p:
+        raise ValueError(f"x: expected rows x {p}")
+    rows = x.shape[0]
+    if out is None:
+        out = torch.empty((rows, q), dtype=dtype, device=weights.device)
+
+    def matrix(t, cols, what):
+        if t.dim() != 2 or t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1) or t.dtype is not dtype or t.get_device() != index:
+            raise ValueError(f"{what}: expected {rows} x {cols} with contiguous columns, in x's dtype, on the layer's device")
+        return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+    pr = QEProduct(rows=rows, dtype=_cache_dtype(dtype), act=act)
+    pr.X, pr.ldx = matrix(x, p, "x")
+    pr.Y, pr.ldy = matrix(out, q, "out")
+    if residual is not None:
+        pr.residual, pr.ldr = matrix(residual, q, "residual")
+    if bias is not None:
+        if bias.shape != (q,) or not bias.is_contiguous() or bias.get_device() != index:
+            raise ValueError(f"bias: expected a contiguous tensor of {q} values on the layer's device")
+        pr.bias, pr.bias_dtype = bias.data_ptr(), _cache_dtype(bias.dtype)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the layer's device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = (_lib or load()).qe_linear(weights._ref, ctypes.addressof(pr), ws, ws_bytes, _raw_stream(index))
+    if st != QE_OK:
+        raise QEError(st, "qe_linear")
     return out
