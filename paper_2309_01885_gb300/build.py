@@ -28,6 +28,7 @@ SOURCES = ["qe_sweep_seq256.cu", "qe_sweep_chg256.cu", "qe_sweep_rows256.cu", "q
            "qe_outlier.cu", "qe_noalloc.cu", "qe_stream.cu", "qe_pack.cu", "qe_select.cu",
            "qe_cache.cu", "qe_attend.cu", "qe_attend_whole8.cu", "qe_attend_whole4.cu",
            "qe_attend_tc.cu", "qe_linear_rows3.cu", "qe_linear_rows4.cu", "qe_linear_rows2.cu", "qe_linear_rows8.cu",
+           "qe_linear_tiles3.cu", "qe_linear_tiles4.cu", "qe_linear_tiles2.cu", "qe_linear_tiles8.cu",
            "qe_linear.cu", "qe_rotate.cu", "qe_grow.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",

@@ -1,5 +1,5 @@
 // Products with a quantized layer: the entry points, and laying a layer out (layout:
-// qe_linear.cuh; kernels: qe_linear_rows.cuh for a few rows).
+// qe_linear.cuh; kernels: qe_linear_rows.cuh for a few rows, qe_linear_tiles.cuh for many).
 #include "qe_internal.h"
 #include "qe_linear.cuh"
 
@@ -108,7 +108,9 @@ qe_status linear_geom(const qe_layer *layer, LinearGeom *g) {
     return QE_OK;
 }
 
-cudaError_t launch_linear_rows(const LinearArgs &a, cudaStream_t s) {
+namespace {
+
+cudaError_t launch_rows(const LinearArgs &a, cudaStream_t s) {
     switch (a.g.bits) {
         case 2: return launch_linear_rows_2(a, s);
         case 3: return launch_linear_rows_3(a, s);
@@ -116,6 +118,20 @@ cudaError_t launch_linear_rows(const LinearArgs &a, cudaStream_t s) {
         default: return launch_linear_rows_8(a, s);
     }
 }
+
+cudaError_t launch_tiles(const LinearArgs &a, cudaStream_t s) {
+    switch (a.g.bits) {
+        case 2: return launch_linear_tiles_2(a, s);
+        case 3: return launch_linear_tiles_3(a, s);
+        case 4: return launch_linear_tiles_4(a, s);
+        default: return launch_linear_tiles_8(a, s);
+    }
+}
+
+// Rows of x up to which the few-rows kernel takes a call.
+constexpr int kFewRows = 32;
+
+}  // namespace
 
 }  // namespace qe
 
@@ -192,11 +208,34 @@ qe_status qe_linear(const qe_layer *layer, const qe_product *pr, void *workspace
     a.ldr = pr->ldr;
     a.y = pr->Y;
     a.ldy = pr->ldy;
+    a.r_vec = (reinterpret_cast<uintptr_t>(pr->residual) & 15u) == 0 && pr->ldr % 8 == 0;
+    a.y_vec = (reinterpret_cast<uintptr_t>(pr->Y) & 15u) == 0 && pr->ldy % 8 == 0;
     a.err = device_error_word();
     if (!a.err) return QE_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    (void)workspace_bytes;
-    const cudaError_t e = launch_linear_rows(a, s);
+    cudaError_t e = cudaSuccess;
+    void *own = nullptr;
+    if (pr->rows <= kFewRows) {
+        e = launch_rows(a, s);
+    } else {
+        if (!a.x_vec) {                                   // TMA wants rows that begin on 16 bytes
+            const int64_t ld = aligned_ld(a.g.p);
+            const size_t need = static_cast<size_t>(2 * pr->rows * ld);
+            if (workspace && workspace_bytes < need) return QE_ERR_OOM;
+            if (!workspace && cudaMallocAsync(&own, need, s) != cudaSuccess) {
+                cudaGetLastError();
+                return QE_ERR_OOM;
+            }
+            uint16_t *to = static_cast<uint16_t *>(workspace ? workspace : own);
+            const dim3 grid(static_cast<unsigned>(ceil_div(a.g.p, 2048)), static_cast<unsigned>(pr->rows < 65535 ? pr->rows : 65535));
+            k_linear_align<<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(a.x), a.ldx, a.rows, a.g.p, to, ld);
+            e = cudaGetLastError();
+            a.x = to;
+            a.ldx = ld;
+        }
+        if (e == cudaSuccess) e = launch_tiles(a, s);
+    }
+    if (own) cudaFreeAsync(own, s);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return QE_ERR_CUDA;

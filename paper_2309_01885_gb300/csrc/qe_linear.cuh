@@ -21,6 +21,8 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "../../include/qe.h"
 #include "qe_common.cuh"
 
@@ -52,6 +54,7 @@ struct LinearArgs {
     int64_t ldr;
     void *y;
     int64_t ldy;
+    int r_vec, y_vec;         // 16-byte accesses of residual and y are aligned
     unsigned *err;
 };
 
@@ -76,6 +79,28 @@ __device__ __forceinline__ void load_unit(const uint8_t *unit, int lane, uint32_
             asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(w[j]), "=r"(w[j + 1]), "=r"(w[j + 2]), "=r"(w[j + 3])
                          : "l"(unit + 128 * j + 16 * lane));
+    }
+}
+
+// The same from shared memory.
+template <int B>
+__device__ __forceinline__ void read_unit(const uint8_t *unit, int lane, uint32_t (&w)[B]) {
+    if constexpr (B == 3) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) w[j] = reinterpret_cast<const uint32_t *>(unit)[32 * j + lane];
+    } else if constexpr (B == 2) {
+        const uint2 v = reinterpret_cast<const uint2 *>(unit)[lane];
+        w[0] = v.x;
+        w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < B; j += 4) {
+            const uint4 v = reinterpret_cast<const uint4 *>(unit + 128 * j)[lane];
+            w[j] = v.x;
+            w[j + 1] = v.y;
+            w[j + 2] = v.z;
+            w[j + 3] = v.w;
+        }
     }
 }
 
@@ -202,13 +227,59 @@ __device__ __forceinline__ void put(const LinearArgs &a, float v, int64_t m, int
     else static_cast<__nv_bfloat16 *>(a.y)[m * a.ldy + i] = __float2bfloat16_rn(v);
 }
 
+// Eight neighbouring outputs from i on (some may lie past the last) of row m, sums scaled.
+__device__ __forceinline__ void finish_eight(const LinearArgs &a, float (&v)[8], int64_t m, int64_t i) {
+    const bool all = i + 8 <= a.g.q;
+    union { uint4 u; uint16_t h[8]; } t;
+    t.u = make_uint4(0u, 0u, 0u, 0u);
+    if (a.residual) {
+        const uint16_t *from = static_cast<const uint16_t *>(a.residual) + m * a.ldr + i;
+        if (a.r_vec && all) t.u = *reinterpret_cast<const uint4 *>(from);
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i + k < a.g.q) t.h[k] = from[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float bias = a.bias && i + k < a.g.q ? to_f32(a.bias, a.bias_dtype, i + k) : 0.0f;
+        v[k] = activated(v[k] + bias, a.act);
+        if (a.residual) v[k] += a.half ? __half2float(__ushort_as_half(t.h[k])) : __uint_as_float(static_cast<uint32_t>(t.h[k]) << 16);
+        t.h[k] = a.half ? __half_as_ushort(__float2half_rn(v[k])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[k]));
+    }
+    uint16_t *to = static_cast<uint16_t *>(a.y) + m * a.ldy + i;
+    if (a.y_vec && all) *reinterpret_cast<uint4 *>(to) = t.u;
+    else
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k < a.g.q) to[k] = t.h[k];
+}
+
+// Raises a kernel's limit of dynamic shared memory on the current device, once a device; `raised`, a bit a device, is the
+// kernel's own.  A refusal is not remembered.
+inline cudaError_t raise_limit(const void *kernel, int bytes, std::atomic<uint64_t> &raised) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+    if (raised.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 // Checks a layer and fills the geometry; QE_ERR_INVALID_ARG / QE_ERR_UNSUPPORTED otherwise.
 qe_status linear_geom(const qe_layer *layer, LinearGeom *g);
 
-cudaError_t launch_linear_rows(const LinearArgs &a, cudaStream_t s);
+// few rows of x (and, slowly, any number of them), and many: x's address and pitch are then multiples of 16 bytes
 cudaError_t launch_linear_rows_2(const LinearArgs &a, cudaStream_t s);
 cudaError_t launch_linear_rows_3(const LinearArgs &a, cudaStream_t s);
 cudaError_t launch_linear_rows_4(const LinearArgs &a, cudaStream_t s);
 cudaError_t launch_linear_rows_8(const LinearArgs &a, cudaStream_t s);
+
+cudaError_t launch_linear_tiles_2(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_tiles_3(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_tiles_4(const LinearArgs &a, cudaStream_t s);
+cudaError_t launch_linear_tiles_8(const LinearArgs &a, cudaStream_t s);
 
 }  // namespace qe

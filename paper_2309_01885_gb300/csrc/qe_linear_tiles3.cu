@@ -1,0 +1,8 @@
+// Many-rows products with codes held in 3 bits.
+#include "qe_linear_tiles.cuh"
+
+namespace qe {
+
+cudaError_t launch_linear_tiles_3(const LinearArgs &a, cudaStream_t s) { return launch_tiles_bits<3>(a, s); }
+
+}  // namespace qe
