@@ -75,6 +75,9 @@ bool make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t 
 bool make_tmap_f16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols,
                    uint64_t ld, uint32_t box_rows);
 
+// Builds a 2-D map of 32-bit words (rows x cols, one after the other, cols a multiple of 4), not swizzled.
+bool make_tmap_words(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows);
+
 // Launches the tcgen05 GEMM with BN in {64, 128, 256} output columns per CTA.
 // grid = (ceil(N / BN), ceil(M / 128), splits).
 cudaError_t launch_tc_gemm(int BN, const CUtensorMap &ta, const CUtensorMap &tb,

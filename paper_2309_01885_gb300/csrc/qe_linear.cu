@@ -37,11 +37,11 @@ __global__ void __launch_bounds__(256) k_linear_codes(const LinearGeom g, uint8_
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t i = tile * kTileRows + r + 8 * h, k = col + 32 * c + 8 * t;
+            const int64_t i = tile * kTileRows + r + 8 * h, k = col + 32 * c + 2 * t;
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) enter<B>(w, c, h, p, e, i < g.q && k + 2 * p + e < g.p ? codes[i * ldc + k + 2 * p + e] & mask : 0u);
+                for (int e = 0; e < 2; ++e) enter<B>(w, c, h, p, e, i < g.q && k + 8 * p + e < g.p ? codes[i * ldc + k + 8 * p + e] & mask : 0u);
         }
     uint32_t *out = reinterpret_cast<uint32_t *>(to + unit * (128 * B));
 #pragma unroll
@@ -106,6 +106,36 @@ qe_status linear_geom(const qe_layer *layer, LinearGeom *g) {
     g->scales = reinterpret_cast<const float *>(at);
     g->zeros = at + round_up(4 * grid_count(*g), 256);
     return QE_OK;
+}
+
+int linear_sms() {
+    static std::atomic<int> known[64];                   // by device; 0: not asked yet
+    int dev = 0, v = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev < 64 && (v = known[dev].load(std::memory_order_relaxed)) > 0) return v;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1) {
+        cudaGetLastError();
+        return 152;
+    }
+    if (dev < 64) known[dev].store(v, std::memory_order_relaxed);
+    return v;
+}
+
+RowsPlan rows_plan(const LinearArgs &a) {
+    const int64_t blocks = ceil_div(a.rows, a.rows <= 8 ? 8 : a.rows <= 16 ? 16 : 32), slots = 2 * linear_sms();
+    RowsPlan best{1, 1};
+    int64_t least = -1;
+    for (int tiles = a.g.bits == 8 ? 1 : 2; tiles >= 1; --tiles) {
+        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * blocks;
+        for (int ranks = 1; ranks <= 8; ++ranks) {
+            // rounds of CTAs, each with its units and what a CTA costs besides, in units
+            const int64_t cost = ceil_div(groups * ranks, slots) * (tiles * ceil_div(a.g.units, ranks) + 12);
+            if (least < 0 || cost < least) {
+                least = cost;
+                best = RowsPlan{tiles, ranks};
+            }
+        }
+    }
+    return best;
 }
 
 namespace {

@@ -4,10 +4,9 @@
 // Codes come in units of 16 rows x 64 columns, a row tile's units one after the other, so
 // that whoever walks along a row tile reads one stream.  A unit has B words for each of 32
 // lanes (B bits a code: 2, 3, 4 or 8).  Lane 4 r + t holds rows r and r + 8 (half h = 0, 1),
-// of either 32-column chunk c = 0, 1 the eight columns 8 t .. 8 t + 7: four pairs p, each in
-// the low bits of a word's two halves once shifted, which is where the m16n8k16 operand and a
-// 16-byte piece of a row of an operand tile both want them (columns are summed over, so
-// an operand's columns may stand in any order that both operands share).
+// of either 32-column chunk c = 0, 1 four pairs p of neighbouring columns, 32 c + 8 p + 2 t and
+// the next, each in the low bits of a word's two halves once shifted: so the m16n8k16 operand
+// wants them, and so a 16 x 128-bit store of tensor memory takes them.
 //   B = 2  word c, bits 2 (4 h + p);   B = 4  word 2 c + h, bits 4 p;
 //   B = 8  word 4 c + 2 h + p / 2, bits 8 (p mod 2);
 //   B = 3  pairs i = 8 c + 4 h + p: word i / 5, bits 3 (i mod 5); i = 15 takes the bit that each
@@ -270,6 +269,14 @@ inline cudaError_t raise_limit(const void *kernel, int bytes, std::atomic<uint64
 
 // Checks a layer and fills the geometry; QE_ERR_INVALID_ARG / QE_ERR_UNSUPPORTED otherwise.
 qe_status linear_geom(const qe_layer *layer, LinearGeom *g);
+
+// How the few-rows kernel is cut up: row tiles of a warp, CTAs that share a layer's columns.
+struct RowsPlan {
+    int tiles, ranks;
+};
+RowsPlan rows_plan(const LinearArgs &a);
+
+int linear_sms();                         // of the current device
 
 // few rows of x (and, slowly, any number of them), and many: x's address and pitch are then multiples of 16 bytes
 cudaError_t launch_linear_rows_2(const LinearArgs &a, cudaStream_t s);

@@ -1,14 +1,15 @@
 // Products with a quantized layer for a few rows of x: y = act(x What^T + bias) + residual.
 //
 // Bound by reading the codes once, closely followed by turning them into operands: at
-// 6.8 TB/s an SM is handed some 47 4-bit codes a cycle.  A warp takes RT row tiles of 16
-// outputs and a run of columns, reads their codes as two streams straight into registers,
-// a few units ahead, turns each pair of codes with two or three instructions into 16-bit
-// floats c - z (exact) and multiplies them with up to 8 NT rows of x on m16n8k16, the outputs
-// in the 16-high side.  Products are exact and sums binary32; the scale comes in at the end, or at
-// the end of every group.  The warps of a CTA share its outputs' columns out among them, and so
-// do the CTAs of a cluster: their sums meet in shared memory, warps and CTAs in order, so that
-// results do not depend on who is first.
+// 6.8 TB/s an SM is handed some 47 4-bit codes a cycle, and the integer pipe takes two cycles
+// for a warp's instruction.  A warp takes RT row tiles of 16 outputs, reads their codes as
+// streams straight into registers, four units (256 columns) ahead, turns each pair of codes
+// with two or three instructions into 16-bit floats c - z (exact) and multiplies them with up
+// to 8 NT rows of x on m16n8k16, the outputs in the 16-high side.  Products are exact and sums
+// binary32; the scale comes in at the end, or at the end of every group.  The eight warps of a CTA share
+// x, which passes through shared memory 256 columns at a time (swizzled by 16 bytes, read by
+// ldmatrix).  The CTAs of a cluster share a layer's columns out among them: their sums meet in
+// shared memory, in order, so that results do not depend on who is first.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -19,7 +20,7 @@
 namespace qe {
 namespace {
 
-constexpr int kRowWarps = 8;
+constexpr int kRowWarps = 8, kChunk = 4;   // kChunk: units of x in a stage, and units of codes in registers
 
 template <bool HALF>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -33,58 +34,83 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int B, int RT, int NT>
+__device__ __forceinline__ void ldmatrix_x4(uint32_t at, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+}
+
+template <int RT, int NT>
 struct RowsOf {
-    static constexpr int ROWS = kTileRows * RT, TOKENS = 8 * NT, LD = ROWS + 4;
-    static constexpr int AHEAD = 4 * (RT * B + 8 * NT) <= 64 ? 4 : 3 * (RT * B + 8 * NT) <= 64 ? 3 : 2;   // units in registers
-    static constexpr int SMEM = kRowWarps * TOKENS * LD * 4;
+    static constexpr int ROWS = kRowWarps * kTileRows * RT, TOKENS = 8 * NT, LD = ROWS + 4;
+    static constexpr int UNIT_BYTES = TOKENS * 128, STAGE = kChunk * UNIT_BYTES, STAGES = 3;
+    static constexpr int SUMS = TOKENS * LD * 4;
+    static constexpr int SMEM = STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS;
+    static constexpr int PIECES = TOKENS * 8 * kChunk / (kRowWarps * 32);   // 16-byte pieces of a stage a thread brings
 };
 
-// Eight columns of a row of x from column k on; columns past p, and rows that are not there, are zeros.
-__device__ __forceinline__ uint4 load_x8(const LinearArgs &a, const uint16_t *row, bool on, int64_t k) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (!on || k >= a.g.p) return v;
-    if (a.x_vec && k + 8 <= a.g.p) return *reinterpret_cast<const uint4 *>(row + k);
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = k + 2 * i < a.g.p ? row[k + 2 * i] : 0u, hi = k + 2 * i + 1 < a.g.p ? row[k + 2 * i + 1] : 0u;
-        w[i] = lo | hi << 16;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+// `bytes` (0 .. 16) from global memory, the rest zeros.
+__device__ __forceinline__ void cp_async16_part(uint32_t dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes) : "memory");
 }
 
 template <int B, int RT, int NT, bool HALF, bool GROUPED>
 __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs a) {
-    using F = RowsOf<B, RT, NT>;
+    using F = RowsOf<RT, NT>;
     using TU = Turn<B, HALF>;
-    constexpr int AHEAD = F::AHEAD;
-    extern __shared__ __align__(16) float met[];          // [warp][token][row], then [0]: this CTA's sums
+    extern __shared__ __align__(128) uint8_t smem[];
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
-    const int tile0 = static_cast<int>(blockIdx.x / static_cast<unsigned>(ranks)) * RT;
+    const int tile0 = static_cast<int>(blockIdx.x / static_cast<unsigned>(ranks)) * (kRowWarps * RT);
     const int64_t m0 = static_cast<int64_t>(blockIdx.y) * F::TOKENS;
-    const int64_t units = a.g.units;
-    const int shares = ranks * kRowWarps, share = rank * kRowWarps + warp;
-    const int begin = static_cast<int>(units * share / shares), end = static_cast<int>(units * (share + 1) / shares);
+    const int units = a.g.units;
+    const int begin = static_cast<int>(static_cast<int64_t>(units) * rank / ranks), end = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / ranks);
+    const int chunks = (end - begin + kChunk - 1) / kChunk;
 
     int tile[RT];
     const uint8_t *code[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {                        // (tiles that are not there repeat the last one, unused)
-        tile[i] = min(tile0 + i, a.g.row_tiles - 1);
-        code[i] = a.g.codes + (tile[i] * units + begin) * (128 * B);
+        tile[i] = min(tile0 + warp * RT + i, a.g.row_tiles - 1);
+        code[i] = a.g.codes + (static_cast<int64_t>(tile[i]) * units + begin) * (128 * B);
     }
-    const uint16_t *xr[NT];
-    bool on[NT];
+    uint32_t w[kChunk][RT][B];
+    auto fetch = [&](int c, int s) {                      // unit s of chunk c
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t m = m0 + 8 * n + r;
-        on[n] = m < a.rows;
-        xr[n] = static_cast<const uint16_t *>(a.x) + (on[n] ? m : 0) * a.ldx;
-    }
+        for (int i = 0; i < RT; ++i) load_unit<B>(code[i] + static_cast<int64_t>(c) * (kChunk * 128 * B) + s * (128 * B), lane, w[s][i]);
+    };
+#pragma unroll
+    for (int s = 0; s < kChunk; ++s)
+        if (begin + s < end) fetch(0, s);
+
+    // x: piece e of a stage is row e / 32's 16 bytes e mod 32
+    const uint32_t ring = smem_u32(smem);
+    auto bring = [&](int c) {
+        if (c < chunks) {
+            const uint32_t stage = ring + (c % F::STAGES) * F::STAGE;
+            const int64_t k0 = (static_cast<int64_t>(begin) + static_cast<int64_t>(c) * kChunk) * kUnitCols;
+#pragma unroll
+            for (int j = 0; j < F::PIECES; ++j) {
+                const int e = threadIdx.x + j * kRowWarps * 32, row = e >> 5, pc = e & 31;
+                const int64_t m = m0 + row, k = k0 + 8 * pc;
+                const uint32_t dst = stage + (pc >> 3) * F::UNIT_BYTES + row * 128 + (((pc & 7) ^ (row & 7)) << 4);
+                const int64_t left = m < a.rows ? a.g.p - k : 0;
+                const int n = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+                const uint16_t *src = static_cast<const uint16_t *>(a.x) + (n > 0 ? m * a.ldx + k : 0);
+                if (a.x_vec) {
+                    cp_async16_part(dst, src, 2 * n);
+                } else {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = (2 * q < n ? src[2 * q] : 0u) | (2 * q + 1 < n ? static_cast<uint32_t>(src[2 * q + 1]) << 16 : 0u);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int c = 0; c < F::STAGES - 1; ++c) bring(c);
 
     float sum[RT][NT][4], total[GROUPED ? RT : 1][GROUPED ? NT : 1][4];
 #pragma unroll
@@ -96,20 +122,6 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
                 sum[i][n][e] = 0.0f;
                 if constexpr (GROUPED) total[i][n][e] = 0.0f;
             }
-    uint32_t w[AHEAD][RT][B];
-    uint4 x[AHEAD][NT][2];
-    auto fetch = [&](int u, uint32_t (&wd)[RT][B], uint4 (&xd)[NT][2]) {
-#pragma unroll
-        for (int i = 0; i < RT; ++i) load_unit<B>(code[i] + static_cast<int64_t>(u - begin) * (128 * B), lane, wd[i]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) xd[n][c] = load_x8(a, xr[n], on[n], static_cast<int64_t>(u) * kUnitCols + 32 * c + 8 * t);
-    };
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
-        if (begin + s < end) fetch(begin + s, w[s], x[s]);
-
     uint32_t zero[RT][2][TU::LEVELS];
     float scale[RT][2];
     int next_grid = begin;                                // unit at which the grids change
@@ -137,9 +149,17 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
         }
     };
     if constexpr (!GROUPED) grids(0);
-    for (int u0 = begin; u0 < end; u0 += AHEAD) {
+    // matrix j of an ldmatrix: rows' piece 4 c + j; lane 8 j + i addresses row i
+    const int mrow = lane & 7, mpiece = lane >> 3;
+    const uint32_t mat0 = ring + mrow * 128 + ((mpiece ^ mrow) << 4), mat1 = ring + mrow * 128 + (((4 + mpiece) ^ mrow) << 4);
+    for (int c = 0; c < chunks; ++c) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(F::STAGES - 2) : "memory");
+        __syncthreads();                                  // the chunk is there, and everyone has done with the one before
+        bring(c + F::STAGES - 1);
+        const uint32_t stage = (c % F::STAGES) * F::STAGE;
+        const int u0 = begin + c * kChunk;
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s) {
+        for (int s = 0; s < kChunk; ++s) {
             const int u = u0 + s;
             if (u >= end) break;
             if constexpr (GROUPED) {
@@ -150,51 +170,50 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
                     next_grid = (g + 1) * a.g.group_units;
                 }
             }
+            uint32_t v[RT][2][2][4];
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                uint32_t v[2][2][4];
-                TU::unit(w[s][i], zero[i], v);
+            for (int i = 0; i < RT; ++i) TU::unit(w[s][i], zero[i], v[i]);
+            if (u + kChunk < end) fetch(c + 1, s);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                uint32_t x[2][4];
+                ldmatrix_x4(mat0 + stage + s * F::UNIT_BYTES + n * 1024, x[0]);
+                ldmatrix_x4(mat1 + stage + s * F::UNIT_BYTES + n * 1024, x[1]);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        mma_16816<HALF>(sum[i][n], v[c][0][0], v[c][1][0], v[c][0][1], v[c][1][1], x[s][n][c].x, x[s][n][c].y);
-                        mma_16816<HALF>(sum[i][n], v[c][0][2], v[c][1][2], v[c][0][3], v[c][1][3], x[s][n][c].z, x[s][n][c].w);
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        mma_16816<HALF>(sum[i][n], v[i][q][0][0], v[i][q][1][0], v[i][q][0][1], v[i][q][1][1], x[q][0], x[q][1]);
+                        mma_16816<HALF>(sum[i][n], v[i][q][0][2], v[i][q][1][2], v[i][q][0][3], v[i][q][1][3], x[q][2], x[q][3]);
                     }
             }
-            if (u + AHEAD < end) fetch(u + AHEAD, w[s], x[s]);
         }
     }
     if constexpr (GROUPED) {
         if (begin < end) fold();
     }
 
-    // ---- the warps' sums meet, then the cluster's ----
-    float *mine = met + warp * (F::TOKENS * F::LD);
+    // ---- the cluster's sums meet ----
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float *met = reinterpret_cast<float *>(smem);         // [row of x][output]
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float v = GROUPED ? total[GROUPED ? i : 0][GROUPED ? n : 0][e] : sum[i][n][e] * (begin < end ? scale[i][e >> 1] : 0.0f);
-                mine[(8 * n + 2 * t + (e & 1)) * F::LD + kTileRows * i + r + 8 * (e >> 1)] = v;
+                const float v = GROUPED ? total[GROUPED ? i : 0][GROUPED ? n : 0][e] : begin < end ? sum[i][n][e] * scale[i][e >> 1] : 0.0f;
+                met[(8 * n + 2 * t + (e & 1)) * F::LD + kTileRows * (warp * RT + i) + r + 8 * (e >> 1)] = v;
             }
-    __syncthreads();
-    constexpr int ALL = F::TOKENS * F::ROWS;
-    for (int e = threadIdx.x; e < ALL; e += kRowWarps * 32) {
-        float *p = met + (e / F::ROWS) * F::LD + e % F::ROWS;
-        float v = p[0];
-#pragma unroll
-        for (int k = 1; k < kRowWarps; ++k) v += p[k * (F::TOKENS * F::LD)];
-        p[0] = v;
-    }
     if (ranks > 1) cluster.sync();
     else __syncthreads();
-    for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < ALL; e += ranks * kRowWarps * 32) {
+    constexpr int ALL = F::TOKENS * F::ROWS;
+    const int here = a.rows - m0 < F::TOKENS ? static_cast<int>(a.rows - m0) * F::ROWS : ALL;
+    for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < here; e += ranks * kRowWarps * 32) {
         const int tok = e / F::ROWS, row = e % F::ROWS;
         const int64_t i = static_cast<int64_t>(tile0) * kTileRows + row, m = m0 + tok;
-        if (i >= a.g.q || m >= a.rows) continue;
+        if (i >= a.g.q) continue;
         float v = 0.0f;
         for (int k = 0; k < ranks; ++k) v += (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row];
         put(a, finished(a, v, m, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f), m, i);
@@ -203,11 +222,15 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
 }
 
 template <int B, int RT, int NT, bool HALF, bool GROUPED>
-cudaError_t launch_rows_as(const LinearArgs &a, cudaStream_t s) {
-    using F = RowsOf<B, RT, NT>;
-    const int64_t groups = ceil_div(a.g.row_tiles, RT), blocks = ceil_div(a.rows, F::TOKENS);
-    int ranks = 1;
-    while (ranks < 8 && groups * blocks * ranks < 304 && a.g.units >= 2 * ranks * kRowWarps * 2) ranks *= 2;
+cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
+    using F = RowsOf<RT, NT>;
+    const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps), blocks = ceil_div(a.rows, F::TOKENS);
+    static std::atomic<uint64_t> raised{0};
+    const void *kernel = reinterpret_cast<const void *>(k_linear_rows<B, RT, NT, HALF, GROUPED>);
+    if (F::SMEM > 48 * 1024) {
+        const cudaError_t e = raise_limit(kernel, F::SMEM, raised);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks), static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(kRowWarps * 32);
@@ -219,22 +242,30 @@ cudaError_t launch_rows_as(const LinearArgs &a, cudaStream_t s) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    static_assert(F::SMEM <= 48 * 1024, "no limit to raise");
     return cudaLaunchKernelEx(&cfg, k_linear_rows<B, RT, NT, HALF, GROUPED>, a);
 }
 
 template <int B, int RT, int NT>
-cudaError_t launch_rows_type(const LinearArgs &a, cudaStream_t s) {
-    if (a.g.groups > 1) return a.half ? launch_rows_as<B, RT, NT, true, true>(a, s) : launch_rows_as<B, RT, NT, false, true>(a, s);
-    return a.half ? launch_rows_as<B, RT, NT, true, false>(a, s) : launch_rows_as<B, RT, NT, false, false>(a, s);
+cudaError_t launch_rows_type(const LinearArgs &a, int ranks, cudaStream_t s) {
+    if (a.g.groups > 1) return a.half ? launch_rows_as<B, RT, NT, true, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, true>(a, ranks, s);
+    return a.half ? launch_rows_as<B, RT, NT, true, false>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false>(a, ranks, s);
+}
+
+template <int B, int RT>
+cudaError_t launch_rows_tokens(const LinearArgs &a, int ranks, cudaStream_t s) {
+    if (a.rows <= 8) return launch_rows_type<B, RT, 1>(a, ranks, s);
+    if (a.rows <= 16) return launch_rows_type<B, RT, 2>(a, ranks, s);
+    return launch_rows_type<B, RT, 4>(a, ranks, s);
 }
 
 template <int B>
 cudaError_t launch_rows_bits(const LinearArgs &a, cudaStream_t s) {
-    constexpr int RT = B == 8 ? 1 : 2;
-    if (a.rows <= 8) return launch_rows_type<B, RT, 1>(a, s);
-    if (a.rows <= 16) return launch_rows_type<B, RT, 2>(a, s);
-    return launch_rows_type<B, RT, 4>(a, s);
+    // a cluster's CTAs share the columns: as many as fill the GPU best, each with some chunks to itself
+    const RowsPlan plan = rows_plan(a);
+    if constexpr (B != 8) {
+        if (plan.tiles == 2) return launch_rows_tokens<B, 2>(a, plan.ranks, s);
+    }
+    return launch_rows_tokens<B, 1>(a, plan.ranks, s);
 }
 
 }  // namespace
