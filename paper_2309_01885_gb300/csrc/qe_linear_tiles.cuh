@@ -38,8 +38,8 @@ constexpr int kTurnWarp = 4, kFoldWarp = 12;
 
 template <int BN>
 struct TilesOf {
-    static constexpr int STAGE = BN * 128, STAGES = BN == 192 ? 5 : BN == 128 ? 6 : 8;   // of x
-    static constexpr int A_STAGES = BN == 192 ? 4 : 8, A_COLS = kUnitCols / 2;           // of turned codes, behind the two accumulators
+    static constexpr int STAGE = BN * 128, STAGES = BN == 192 ? 4 : BN == 128 ? 6 : 8;   // of x, and of turned codes:
+    static constexpr int A_COLS = kUnitCols / 2;                                         // these behind the two accumulators
     static constexpr int HALF = BN / 2;    // columns of a folding thread
     static constexpr int OUT_COLS = BN == 64 ? 32 : HALF / 2;                            // that leave at once
     static constexpr int CODE_RING = 32 * 1024, OUT_BYTES = 8 * OUT_COLS * 32 * 4;
@@ -47,7 +47,7 @@ struct TilesOf {
     // registers a thread: 96 at launch, dealt out anew by role (warps 0-3, two warpgroups that turn, two that fold)
     static constexpr int FOLD_REGS = BN == 192 ? 144 : 96, TURN_REGS = BN == 192 ? 72 : 96, LEAD_REGS = BN == 192 ? 48 : 96;
     static_assert(2 * FOLD_REGS + 2 * TURN_REGS + LEAD_REGS <= 5 * 96, "as many as the block was launched with");
-    static_assert(2 * BN + A_STAGES * A_COLS <= 512, "tensor memory");
+    static_assert(2 * BN + STAGES * A_COLS <= 512, "tensor memory");
     static_assert(BN * kTileOut * 4 <= STAGES * STAGE, "a cluster's sums fit the ring");
     static_assert(SMEM <= 232448, "shared memory");
 };
@@ -81,13 +81,23 @@ __device__ __forceinline__ void tmem_st_unit(uint32_t taddr, const uint32_t (&v)
         : "memory");
 }
 
-// D += A B with A in tensor memory.
-__device__ __forceinline__ void mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// D += A B with A in tensor memory; and an arrival on a barrier once all products so far have been taken.  Issued by one
+// elected lane of a warp that goes along together, so that addresses stay in uniform registers (a step's issue took 411
+// cycles from a lane by itself).
+__device__ __forceinline__ void mma_ts_one(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d),
         "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar)
         : "memory");
 }
 
@@ -124,13 +134,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
     uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
     uint8_t *code_ring = smem + F::STAGES * F::STAGE;
     float *out_stage = reinterpret_cast<float *>(code_ring + F::CODE_RING);
-    uint64_t *x_full = reinterpret_cast<uint64_t *>(code_ring + F::CODE_RING + F::OUT_BYTES);
-    uint64_t *x_empty = x_full + F::STAGES, *a_full = x_empty + F::STAGES, *a_empty = a_full + F::A_STAGES;
-    uint64_t *code_full = a_empty + F::A_STAGES, *code_empty = code_full + CODE_STAGES;
+    uint64_t *full = reinterpret_cast<uint64_t *>(code_ring + F::CODE_RING + F::OUT_BYTES), *empty = full + F::STAGES;
+    uint64_t *code_full = empty + F::STAGES, *code_empty = code_full + CODE_STAGES;
     uint64_t *acc_full = code_empty + CODE_STAGES, *acc_empty = acc_full + 2, *drain = acc_empty + 2;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    static_assert((2 * F::STAGES + 2 * F::A_STAGES + 5 + 2 * CODE_STAGES) * 8 + 8 <= 768, "room for the barriers");
+    static_assert((2 * F::STAGES + 5 + 2 * CODE_STAGES) * 8 + 8 <= 768, "room for the barriers");
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
@@ -145,12 +154,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            mbar_init(&x_full[s], 1);
-            mbar_init(&x_empty[s], 1);
-        }
-        for (int s = 0; s < F::A_STAGES; ++s) {
-            mbar_init(&a_full[s], 4);
-            mbar_init(&a_empty[s], 1);
+            mbar_init(&full[s], 1 + 4);
+            mbar_init(&empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&acc_full[b], 1);
@@ -194,52 +199,50 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
             for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
                 const int m0 = tile / out_tiles * BN;
                 for (int u = begin; u < end; ++u, ++n) {
-                    ok = wait_on(&x_empty[at.s], at.phase ^ 1u, abort_flag);
+                    ok = wait_on(&empty[at.s], at.phase ^ 1u, abort_flag);
                     if (!ok) break;
-                    mbar_arrive_expect_tx(&x_full[at.s], F::STAGE);
-                    tma_load_2d(&xmap, smem + at.s * F::STAGE, &x_full[at.s], u * kUnitCols, m0);
+                    mbar_arrive_expect_tx(&full[at.s], F::STAGE);
+                    tma_load_2d(&xmap, smem + at.s * F::STAGE, &full[at.s], u * kUnitCols, m0);
                     at.next();
                 }
             }
             if (!ok) give_up();
             // the last copy into each stage has landed before the CTA goes on
             for (int64_t k = n > F::STAGES ? n - F::STAGES : 0; k < n; ++k)
-                mbar_wait_bounded(&x_full[k % F::STAGES], static_cast<uint32_t>(k / F::STAGES) & 1u, nullptr);
+                mbar_wait_bounded(&full[k % F::STAGES], static_cast<uint32_t>(k / F::STAGES) & 1u, nullptr);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = HALF ? idesc_f16_f32(kTileOut, BN) : idesc_bf16_f32(kTileOut, BN);
-            Turnstile<F::STAGES> xs;
-            Turnstile<F::A_STAGES> as;
-            Turnstile<2> acc;
-            bool ok = true;
-            for (int tile = first_tile; ok && tile < tiles; tile += tile_step)
-                for (int u = begin; ok && u < end;) {
-                    ok = wait_on(&acc_empty[acc.s], acc.phase ^ 1u, abort_flag);
+        constexpr uint32_t idesc = HALF ? idesc_f16_f32(kTileOut, BN) : idesc_bf16_f32(kTileOut, BN);
+        const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), empty0 = smem_u32(empty), acc0 = smem_u32(acc_full);
+        const uint64_t x0 = smem_desc_k128(smem_u32(smem));
+        Turnstile<F::STAGES> at;
+        Turnstile<2> acc;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < tiles; tile += tile_step)
+            for (int u = begin; ok && u < end;) {
+                ok = wait_warp_on(&acc_empty[acc.s], acc.phase ^ 1u, abort_flag);
+                if (!ok) break;
+                const uint32_t dst = t0 + static_cast<uint32_t>(acc.s * BN);
+                const int upto = min((u / seg + 1) * seg, end);
+                for (uint32_t add = 0u; u < upto; ++u, add = 1u) {
+                    ok = wait_warp_on(&full[at.s], at.phase, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t dst = tmem + static_cast<uint32_t>(acc.s * BN);
-                    const int upto = min((u / seg + 1) * seg, end);
-                    for (int first = 1; u < upto; ++u, first = 0) {
-                        ok = wait_on(&x_full[xs.s], xs.phase, abort_flag) && wait_on(&a_full[as.s], as.phase, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t db = smem_desc_k128(smem_u32(smem + xs.s * F::STAGE));
-                        const uint32_t da = tmem + static_cast<uint32_t>(2 * BN + as.s * F::A_COLS);
+                    const uint64_t db = x0 + static_cast<uint64_t>(at.s * (F::STAGE / 16));
+                    const uint32_t da = t0 + static_cast<uint32_t>(2 * BN + at.s * F::A_COLS);
+                    mma_ts_one(dst, da, db, idesc, add);
 #pragma unroll
-                        for (int k = 0; k < kUnitCols / 16; ++k) mma_ts(dst, da + 8u * k, db + 2u * k, idesc, first && k == 0 ? 0u : 1u);
-                        mma_commit(&x_empty[xs.s]);
-                        mma_commit(&a_empty[as.s]);
-                        xs.next();
-                        as.next();
-                    }
-                    if (ok) mma_commit(&acc_full[acc.s]);
-                    acc.next();
+                    for (int k = 1; k < kUnitCols / 16; ++k) mma_ts_one(dst, da + 8u * k, db + 2u * k, idesc, 1u);
+                    commit_one(empty0 + 8u * at.s);
+                    at.next();
                 }
-            if (!ok) give_up();
-            mma_commit(drain);                            // nothing is in flight when tensor memory is freed
-            mbar_wait_bounded(drain, 0u, nullptr);
-        }
+                if (ok) commit_one(acc0 + 8u * acc.s);
+                acc.next();
+            }
+        if (!ok && lane == 0) give_up();
+        __syncwarp();
+        commit_one(smem_u32(drain));                      // nothing is in flight when tensor memory is freed
+        mbar_wait_bounded(drain, 0u, nullptr);
     } else if (warp == 2) {
         if (lane == 0) {                                  // (row tiles past the last are zeros)
             Turnstile<CODE_STAGES> at;
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         const uint32_t to = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(2 * BN);
         uint32_t zero[2][2][TU::LEVELS];
         Turnstile<CODE_STAGES> cs;
-        Turnstile<F::A_STAGES> as;
+        Turnstile<F::STAGES> as;
         int n = 0;
         bool ok = true;
         for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
@@ -291,7 +294,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
 #pragma unroll
                 for (int i = 0; i < 2; ++i) read_unit<B>(code_ring + cs.s * CODES + (2 * quad + i) * (128 * B), lane, w[i]);
                 TU::unit(w[0], zero[0], v);
-                ok = wait_warp_on(&a_empty[as.s], as.phase ^ 1u, abort_flag);
+                ok = wait_warp_on(&empty[as.s], as.phase ^ 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t dst = to + static_cast<uint32_t>(as.s * F::A_COLS);
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&code_empty[cs.s]);
-                    mbar_arrive(&a_full[as.s]);
+                    mbar_arrive(&full[as.s]);
                 }
             }
         }
