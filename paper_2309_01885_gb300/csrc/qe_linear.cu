@@ -138,6 +138,26 @@ RowsPlan rows_plan(const LinearArgs &a) {
     return best;
 }
 
+TilesPlan tiles_plan(const LinearArgs &a) {
+    const int64_t outs = ceil_div(a.g.q, 128), sms = linear_sms();
+    TilesPlan best{64, 64, 1};
+    if (a.rows > 64) {
+        // a group's end stops a tile of 256, which has one accumulator
+        const int room = a.rows <= 128 || (a.g.groups > 1 && a.g.group_units < 16) ? 128 : 256;
+        int64_t least = -1;
+        for (int rows = room; rows >= room / 2; rows -= 16) {
+            const int64_t cost = ceil_div(outs * ceil_div(a.rows, rows), sms) * (rows + 32);
+            if (least < 0 || cost < least) {
+                least = cost;
+                best = TilesPlan{room, rows, 1};
+            }
+        }
+    }
+    const int64_t tiles = outs * ceil_div(a.rows, best.rows);
+    while (best.ranks < 8 && tiles * best.ranks * 2 <= sms && a.g.units >= 8 * best.ranks) best.ranks *= 2;
+    return best;
+}
+
 namespace {
 
 cudaError_t launch_rows(const LinearArgs &a, cudaStream_t s) {
@@ -238,8 +258,6 @@ qe_status qe_linear(const qe_layer *layer, const qe_product *pr, void *workspace
     a.ldr = pr->ldr;
     a.y = pr->Y;
     a.ldy = pr->ldy;
-    a.r_vec = (reinterpret_cast<uintptr_t>(pr->residual) & 15u) == 0 && pr->ldr % 8 == 0;
-    a.y_vec = (reinterpret_cast<uintptr_t>(pr->Y) & 15u) == 0 && pr->ldy % 8 == 0;
     a.err = device_error_word();
     if (!a.err) return QE_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

@@ -21,6 +21,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "../../include/qe.h"
 #include "qe_common.cuh"
@@ -53,7 +54,6 @@ struct LinearArgs {
     int64_t ldr;
     void *y;
     int64_t ldy;
-    int r_vec, y_vec;         // 16-byte accesses of residual and y are aligned
     unsigned *err;
 };
 
@@ -201,57 +201,42 @@ __device__ __forceinline__ float to_f32(const void *p, int dtype, int64_t i) {
     return __half2float(static_cast<const __half *>(p)[i]);
 }
 
-__device__ __forceinline__ float activated(float y, int act) {
+template <int ACT>
+__device__ __forceinline__ float activated(float y) {
+    if constexpr (ACT == QE_ACT_RELU) return y < 0.0f ? 0.0f : y;      // NaN stays
+    if constexpr (ACT == QE_ACT_GELU) return 0.5f * y * erfcf(-0.70710678118654752f * y);
+    if constexpr (ACT == QE_ACT_GELU_TANH) {
+        const float u = 0.79788456080286536f * fmaf(0.044715f * y * y, y, y);
+        return y / (1.0f + expf(-2.0f * u));               // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+    }
+    if constexpr (ACT == QE_ACT_SILU) return y / (1.0f + expf(-y));
+    return y;
+}
+
+// f of the call's activation as a constant.  (Chosen for each value instead, all of them were computed: a tile of 128 x 224
+// results took 60000 cycles to leave, now 8000.)
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f) {
     switch (act) {
-        case QE_ACT_RELU: return y < 0.0f ? 0.0f : y;      // NaN stays
-        case QE_ACT_GELU: return 0.5f * y * erfcf(-0.70710678118654752f * y);
-        case QE_ACT_GELU_TANH: {
-            const float u = 0.79788456080286536f * fmaf(0.044715f * y * y, y, y);
-            return y / (1.0f + expf(-2.0f * u));           // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
-        }
-        case QE_ACT_SILU: return y / (1.0f + expf(-y));
-        default: return y;
+        case QE_ACT_RELU: f(std::integral_constant<int, QE_ACT_RELU>{}); break;
+        case QE_ACT_GELU: f(std::integral_constant<int, QE_ACT_GELU>{}); break;
+        case QE_ACT_GELU_TANH: f(std::integral_constant<int, QE_ACT_GELU_TANH>{}); break;
+        case QE_ACT_SILU: f(std::integral_constant<int, QE_ACT_SILU>{}); break;
+        default: f(std::integral_constant<int, QE_ACT_NONE>{});
     }
 }
 
 // A finished sum (scaled) of output i for row m: bias, activation, residual, one rounding.
-__device__ __forceinline__ float finished(const LinearArgs &a, float v, int64_t m, int64_t i, float bias) {
-    v = activated(v + bias, a.act);
-    if (a.residual) v += to_f32(a.residual, a.half ? QE_F16 : QE_BF16, m * a.ldr + i);
-    return v;
-}
-
-__device__ __forceinline__ void put(const LinearArgs &a, float v, int64_t m, int64_t i) {
-    if (a.half) static_cast<__half *>(a.y)[m * a.ldy + i] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16 *>(a.y)[m * a.ldy + i] = __float2bfloat16_rn(v);
-}
-
-// Eight neighbouring outputs from i on (some may lie past the last) of row m, sums scaled.
-__device__ __forceinline__ void finish_eight(const LinearArgs &a, float (&v)[8], int64_t m, int64_t i) {
-    const bool all = i + 8 <= a.g.q;
-    union { uint4 u; uint16_t h[8]; } t;
-    t.u = make_uint4(0u, 0u, 0u, 0u);
-    if (a.residual) {
-        const uint16_t *from = static_cast<const uint16_t *>(a.residual) + m * a.ldr + i;
-        if (a.r_vec && all) t.u = *reinterpret_cast<const uint4 *>(from);
-        else
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i + k < a.g.q) t.h[k] = from[k];
+template <int ACT>
+__device__ __forceinline__ void finish(const LinearArgs &a, float v, int64_t m, int64_t i, float bias) {
+    v = activated<ACT>(v + bias);
+    if (a.half) {
+        if (a.residual) v += __half2float(static_cast<const __half *>(a.residual)[m * a.ldr + i]);
+        static_cast<__half *>(a.y)[m * a.ldy + i] = __float2half_rn(v);
+    } else {
+        if (a.residual) v += __bfloat162float(static_cast<const __nv_bfloat16 *>(a.residual)[m * a.ldr + i]);
+        static_cast<__nv_bfloat16 *>(a.y)[m * a.ldy + i] = __float2bfloat16_rn(v);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float bias = a.bias && i + k < a.g.q ? to_f32(a.bias, a.bias_dtype, i + k) : 0.0f;
-        v[k] = activated(v[k] + bias, a.act);
-        if (a.residual) v[k] += a.half ? __half2float(__ushort_as_half(t.h[k])) : __uint_as_float(static_cast<uint32_t>(t.h[k]) << 16);
-        t.h[k] = a.half ? __half_as_ushort(__float2half_rn(v[k])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[k]));
-    }
-    uint16_t *to = static_cast<uint16_t *>(a.y) + m * a.ldy + i;
-    if (a.y_vec && all) *reinterpret_cast<uint4 *>(to) = t.u;
-    else
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i + k < a.g.q) to[k] = t.h[k];
 }
 
 // Raises a kernel's limit of dynamic shared memory on the current device, once a device; `raised`, a bit a device, is the
@@ -275,6 +260,12 @@ struct RowsPlan {
     int tiles, ranks;
 };
 RowsPlan rows_plan(const LinearArgs &a);
+
+// How the many-rows kernel is cut up: rows of x that its tiles have room for and have, CTAs that share a tile's columns.
+struct TilesPlan {
+    int room, rows, ranks;
+};
+TilesPlan tiles_plan(const LinearArgs &a);
 
 int linear_sms();                         // of the current device
 

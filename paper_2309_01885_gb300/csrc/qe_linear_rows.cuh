@@ -210,14 +210,16 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
     else __syncthreads();
     constexpr int ALL = F::TOKENS * F::ROWS;
     const int here = a.rows - m0 < F::TOKENS ? static_cast<int>(a.rows - m0) * F::ROWS : ALL;
-    for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < here; e += ranks * kRowWarps * 32) {
-        const int tok = e / F::ROWS, row = e % F::ROWS;
-        const int64_t i = static_cast<int64_t>(tile0) * kTileRows + row, m = m0 + tok;
-        if (i >= a.g.q) continue;
-        float v = 0.0f;
-        for (int k = 0; k < ranks; ++k) v += (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row];
-        put(a, finished(a, v, m, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f), m, i);
-    }
+    with_activation(a.act, [&](auto act) {
+        for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < here; e += ranks * kRowWarps * 32) {
+            const int tok = e / F::ROWS, row = e % F::ROWS;
+            const int64_t i = static_cast<int64_t>(tile0) * kTileRows + row;
+            if (i >= a.g.q) continue;
+            float v = 0.0f;
+            for (int k = 0; k < ranks; ++k) v += (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row];
+            finish<act.value>(a, v, m0 + tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
+        }
+    });
     if (ranks > 1) cluster.sync();                        // nobody leaves while its sums are read
 }
 
