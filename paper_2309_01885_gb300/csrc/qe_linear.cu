@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(256) k_linear_codes(const LinearGeom g, uint8_
 __global__ void __launch_bounds__(256) k_linear_grids(const LinearGeom g, float *scales, uint8_t *zeros, const float *from_s, const float *from_z,
                                                       float top, unsigned *err) {
     const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= static_cast<int64_t>(g.row_tiles) * g.groups * kTileRows) return;
+    // (of an odd number of row tiles the last pair's second one is written too)
+    if (n >= static_cast<int64_t>(g.row_tiles + (g.row_tiles & 1)) * g.groups * kTileRows) return;
     const int64_t tile = n / (g.groups * kTileRows), i = tile * kTileRows + n % kTileRows, grp = n / kTileRows % g.groups;
     float s = 0.0f, z = 0.0f;
     if (i < g.q) {
@@ -63,8 +64,9 @@ __global__ void __launch_bounds__(256) k_linear_grids(const LinearGeom g, float 
             set_error(err, ERR_NUMERIC);
         }
     }
-    scales[n] = s;
-    zeros[n] = static_cast<uint8_t>(z);
+    if (tile < g.row_tiles) scales[n] = s;
+    const int row = static_cast<int>(n % kTileRows);
+    zeros[((tile >> 1) * g.groups + grp) * 32 + 4 * (row & 7) + 2 * (tile & 1) + (row >> 3)] = static_cast<uint8_t>(z);
 }
 
 // Rows of x at a pitch of whole 16 bytes, for calls whose own rows are not aligned so.
@@ -76,6 +78,7 @@ __global__ void __launch_bounds__(256) k_linear_align(const uint16_t *x, int64_t
 
 int64_t code_bytes(const LinearGeom &g) { return static_cast<int64_t>(g.row_tiles) * g.units * (128 * g.bits); }
 int64_t grid_count(const LinearGeom &g) { return static_cast<int64_t>(g.row_tiles) * g.groups * kTileRows; }
+int64_t zero_count(const LinearGeom &g) { return static_cast<int64_t>(g.row_tiles + (g.row_tiles & 1)) * g.groups * kTileRows; }
 
 qe_status shape(int64_t q, int64_t p, int bits, int64_t group_size, LinearGeom *g, size_t *bytes) {
     if (q < 1 || p < 1 || q > (1 << 24) || p > (1 << 24) || bits < 2 || bits > 8 || group_size < 0) return QE_ERR_INVALID_ARG;
@@ -88,7 +91,7 @@ qe_status shape(int64_t q, int64_t p, int bits, int64_t group_size, LinearGeom *
     g->row_tiles = static_cast<int>(ceil_div(q, kTileRows));
     g->groups = grouped ? static_cast<int>(ceil_div(p, group_size)) : 1;
     g->group_units = grouped ? static_cast<int>(group_size / kUnitCols) : g->units;
-    *bytes = static_cast<size_t>(round_up(code_bytes(*g), 256) + round_up(4 * grid_count(*g), 256) + round_up(grid_count(*g), 256));
+    *bytes = static_cast<size_t>(round_up(code_bytes(*g), 256) + round_up(4 * grid_count(*g), 256) + round_up(zero_count(*g), 256));
     return QE_OK;
 }
 
@@ -104,7 +107,7 @@ qe_status linear_geom(const qe_layer *layer, LinearGeom *g) {
     g->codes = at;
     at += round_up(code_bytes(*g), 256);
     g->scales = reinterpret_cast<const float *>(at);
-    g->zeros = at + round_up(4 * grid_count(*g), 256);
+    g->zeros = reinterpret_cast<const uint32_t *>(at + round_up(4 * grid_count(*g), 256));
     return QE_OK;
 }
 
@@ -143,9 +146,9 @@ TilesPlan tiles_plan(const LinearArgs &a) {
     TilesPlan best{64, 64, 1};
     if (a.rows > 64) {
         // a group's end stops a tile of 256, which has one accumulator
-        const int room = a.rows <= 128 || (a.g.groups > 1 && a.g.group_units < 16) ? 128 : 256;
+        const int room = a.rows <= 128 ? 128 : 256;
         int64_t least = -1;
-        for (int rows = room; rows >= room / 2; rows -= 16) {
+        for (int rows = room; rows >= room / 2; rows -= 32) {
             const int64_t cost = ceil_div(outs * ceil_div(a.rows, rows), sms) * (rows + 32);
             if (least < 0 || cost < least) {
                 least = cost;
@@ -220,8 +223,8 @@ qe_status qe_linear_pack(const qe_layer *layer, const uint8_t *codes, int64_t ld
     else if (g.bits == 4) k_linear_codes<4><<<blocks, 256, 0, s>>>(g, to, codes, ldc, mask);
     else k_linear_codes<8><<<blocks, 256, 0, s>>>(g, to, codes, ldc, mask);
     if (cudaGetLastError() != cudaSuccess) return QE_ERR_CUDA;
-    k_linear_grids<<<static_cast<unsigned>(ceil_div(grid_count(g), 256)), 256, 0, s>>>(
-        g, const_cast<float *>(g.scales), const_cast<uint8_t *>(g.zeros), scales, zeros, static_cast<float>(mask), err);
+    k_linear_grids<<<static_cast<unsigned>(ceil_div(zero_count(g), 256)), 256, 0, s>>>(
+        g, const_cast<float *>(g.scales), reinterpret_cast<uint8_t *>(const_cast<uint32_t *>(g.zeros)), scales, zeros, static_cast<float>(mask), err);
     return cudaGetLastError() == cudaSuccess ? QE_OK : QE_ERR_CUDA;
 }
 

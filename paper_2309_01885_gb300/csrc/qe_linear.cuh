@@ -12,7 +12,8 @@
 //   B = 3  pairs i = 8 c + 4 h + p: word i / 5, bits 3 (i mod 5); i = 15 takes the bit that each
 //          half has left over, bit j of its code in word j: 32 codes in 96 bits.
 // (Bits are those of the pair's first column; its second column's are 16 above.)
-// Behind the codes lie scales (fp32) and zeros (one byte), 16 to a row tile and group.
+// Behind the codes lie scales (fp32), 16 to a row tile and group, and zeros (one byte): a word for
+// each pair of row tiles, group and r holds those of rows r and r + 8 of the first and of the second.
 //
 // c - z is exact in both 16-bit types.  A code below the leading bit of 2^7 (bf16) or 2^10
 // (fp16) makes 2^7 + c 2^s by or-ing alone; one fused multiply-add takes s and the zero out.
@@ -33,7 +34,7 @@ constexpr int kUnitCols = 64, kTileRows = 16;
 struct LinearGeom {
     const uint8_t *codes;
     const float *scales;
-    const uint8_t *zeros;
+    const uint32_t *zeros;
     int64_t q, p;
     int bits;                 // as stored: 2, 3, 4 or 8
     int units;                // of a row tile
@@ -194,6 +195,12 @@ struct Turn {
                 }
     }
 };
+
+// The word of zeros of a row tile's pair and a group; byte 2 i + h is row r + 8 h of row tile i of the pair.
+__device__ __forceinline__ const uint32_t *zero_words(const LinearGeom &g, int tile, int r) {
+    return g.zeros + static_cast<int64_t>(tile >> 1) * g.groups * 8 + r;
+}
+__device__ __forceinline__ float zero_of(uint32_t word, int byte) { return static_cast<float>(word >> (8 * byte) & 0xffu); }
 
 __device__ __forceinline__ float to_f32(const void *p, int dtype, int64_t i) {
     if (dtype == QE_F32) return static_cast<const float *>(p)[i];

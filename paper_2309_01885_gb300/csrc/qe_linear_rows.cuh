@@ -124,17 +124,34 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
             }
     uint32_t zero[RT][2][TU::LEVELS];
     float scale[RT][2];
-    int next_grid = begin;                                // unit at which the grids change
-    auto grids = [&](int g) {
+    int next_grid = begin, group = GROUPED ? begin / a.g.group_units : 0;   // unit at which the grids change, and to which
+    float scale_ahead[RT][2];                             // the next group's
+    uint32_t zero_ahead[RT];
+    const float *scales[RT];
+    const uint32_t *zeros[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        scales[i] = a.g.scales + static_cast<int64_t>(tile[i]) * a.g.groups * kTileRows + r;
+        zeros[i] = zero_words(a.g, tile[i], r);
+    }
+    auto load_grids = [&](int g) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) scale_ahead[i][h] = scales[i][g * kTileRows + 8 * h];
+            zero_ahead[i] = zeros[i][g * 8];
+        }
+    };
+    auto turn_grids = [&]() {
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t at = (static_cast<int64_t>(tile[i]) * a.g.groups + g) * kTileRows + r + 8 * h;
-                scale[i][h] = a.g.scales[at];
-                TU::zero(static_cast<float>(a.g.zeros[at]), zero[i][h]);
+                scale[i][h] = scale_ahead[i][h];
+                TU::zero(zero_of(zero_ahead[i], 2 * (tile[i] & 1) + h), zero[i][h]);
             }
     };
+    load_grids(group);
     auto fold = [&]() {
         if constexpr (GROUPED) {
 #pragma unroll
@@ -148,7 +165,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
                     }
         }
     };
-    if constexpr (!GROUPED) grids(0);
+    if constexpr (!GROUPED) turn_grids();
     // matrix j of an ldmatrix: rows' piece 4 c + j; lane 8 j + i addresses row i
     const int mrow = lane & 7, mpiece = lane >> 3;
     const uint32_t mat0 = ring + mrow * 128 + ((mpiece ^ mrow) << 4), mat1 = ring + mrow * 128 + (((4 + mpiece) ^ mrow) << 4);
@@ -165,9 +182,9 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
             if constexpr (GROUPED) {
                 if (u == next_grid) {
                     if (u > begin) fold();
-                    const int g = u / a.g.group_units;
-                    grids(g);
-                    next_grid = (g + 1) * a.g.group_units;
+                    turn_grids();
+                    if (++group < a.g.groups) load_grids(group);
+                    next_grid = group * a.g.group_units;
                 }
             }
             uint32_t v[RT][2][2][4];

@@ -104,23 +104,17 @@ __device__ __forceinline__ void commit_one(uint32_t bar) {
         : "memory");
 }
 
-__device__ __forceinline__ bool there(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}\n"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-// A wait that reads the clock only when it takes long (and not sooner: more tries held up the warps that work).
+// A wait that reads the clock only when it takes long.
 __device__ __forceinline__ bool wait_on(uint64_t *bar, uint32_t parity, volatile int *abort) {
-    if (there(bar, parity)) return true;
-    for (int n = 0; n < 16; ++n)
+    unsigned long long t0 = 0;
+    for (int n = 1;; ++n) {
         if (mbar_try_wait(bar, parity)) return true;
-    return mbar_wait_bounded(bar, parity, abort);
+        if ((n & 31) != 0) continue;
+        if (*abort) return false;
+        const unsigned long long now = globaltimer_ns();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > kWaitLimitNs) return false;
+    }
 }
 __device__ __forceinline__ bool wait_warp_on(uint64_t *bar, uint32_t parity, volatile int *abort) {
     return __all_sync(0xffffffffu, wait_on(bar, parity, abort)) != 0;
@@ -138,6 +132,41 @@ struct Turnstile {
         }
     }
 };
+
+// A lane's results leave: of output o, for `left` rows of x from m0 on.  Registers have no index, so eight rows at a time
+// pass through shared memory, in a loop: written out for all of them its instructions came from afar once a tile, and a
+// tile took 100000 cycles to leave.
+template <typename F, int ACT>
+__device__ __forceinline__ void leave(const LinearArgs &a, const float (&acc)[F::HALF], float *mine, int64_t m0, int left, int64_t o) {
+    constexpr int N = F::OUT_COLS;
+    const bool on = o < a.g.q;
+    const float bias = on && a.bias ? to_f32(a.bias, a.bias_dtype, o) : 0.0f;
+    const uint16_t *res = a.residual ? static_cast<const uint16_t *>(a.residual) + m0 * a.ldr + o : nullptr;
+    uint16_t *y = static_cast<uint16_t *>(a.y) + m0 * a.ldy + o;
+#pragma unroll 1
+    for (int part = 0; part < F::HALF / N && part * N < left; ++part) {
+#pragma unroll
+        for (int q = 0; q < F::HALF / N; ++q)
+            if (q == part)
+#pragma unroll
+                for (int i = 0; i < N; ++i) mine[i * 32] = acc[q * N + i];
+        uint16_t r[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            r[i] = 0;
+            if (res && on && part * N + i < left) r[i] = res[i * a.ldr];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float v = activated<ACT>(mine[i * 32] + bias);
+            if (res) v += a.half ? __half2float(__ushort_as_half(r[i])) : __uint_as_float(static_cast<uint32_t>(r[i]) << 16);
+            const uint16_t h = a.half ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
+            if (on && part * N + i < left) y[i * a.ldy] = h;
+        }
+        if (res) res += N * a.ldr;
+        y += N * a.ldy;
+    }
+}
 
 template <int B, int BN, bool HALF>
 __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearArgs a, const int bn, const __grid_constant__ CUtensorMap xmap,
@@ -168,6 +197,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
               end = static_cast<int>(static_cast<int64_t>(a.g.units) * (rank + 1) / ranks);
     const int steps = end - begin, stages = (steps + 1) / 2;    // of a tile: units, and pairs of them (the last may lack one)
     const int seg = a.g.groups > 1 ? a.g.group_units : kSegmentUnits;
+    // groups with one accumulator: a tile's two halves of rows take turns, one's products running while the other is folded
+    const int parts = F::BUFS == 1 && a.g.groups > 1 ? 2 : 1;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
@@ -180,7 +211,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&acc_full[b], 1);
-            mbar_init(&acc_empty[b], 8);
+            mbar_init(&acc_empty[b], parts == 2 ? 4 : 8);
         }
         for (int s = 0; s < CODE_STAGES; ++s) {
             mbar_init(&code_full[s], 1);
@@ -235,46 +266,50 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 mbar_wait_bounded(&x_full[k % F::STAGES], static_cast<uint32_t>(k / F::STAGES) & 1u, nullptr);
         }
     } else if (warp == 1) {
-        const uint32_t idesc = HALF ? idesc_f16_f32(kTileOut, bn) : idesc_bf16_f32(kTileOut, bn);
+        const uint32_t idesc = HALF ? idesc_f16_f32(kTileOut, bn / parts) : idesc_bf16_f32(kTileOut, bn / parts);
         const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), x_empty0 = smem_u32(x_empty), a_empty0 = smem_u32(a_empty), acc0 = smem_u32(acc_full);
         const uint64_t x0 = smem_desc_k128(smem_u32(smem));
         Turnstile<F::STAGES> xs;
         Turnstile<F::A_STAGES> as;
-        Turnstile<F::BUFS> acc;
+        Turnstile<F::BUFS> acc[2];                        // of either part
         bool ok = true;
         for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
-            int seg_end = begin;
-            uint32_t add = 0u;
-            for (int u = begin; u < end; ++u) {
-                const int second = (u - begin) & 1;
-                if (u == seg_end) {                       // a segment begins: its accumulator has been folded
-                    ok = wait_warp_on(&acc_empty[acc.s], acc.phase ^ 1u, abort_flag);
-                    if (!ok) break;
-                    seg_end = min((u / seg + 1) * seg, end);
-                    add = 0u;
-                }
-                if (second == 0) {
-                    ok = wait_warp_on(&x_full[xs.s], xs.phase, abort_flag) && wait_warp_on(&a_full[as.s], as.phase, abort_flag);
-                    if (!ok) break;
-                }
+            int seg_end[2] = {begin, begin};
+            for (int u = begin; ok && u < end; u += 2) {
+                ok = wait_warp_on(&x_full[xs.s], xs.phase, abort_flag) && wait_warp_on(&a_full[as.s], as.phase, abort_flag);
+                if (!ok) break;
                 tc_fence_after();
-                const uint32_t dst = t0 + static_cast<uint32_t>(acc.s * BN);
-                const uint64_t db = x0 + static_cast<uint64_t>((xs.s * F::STAGE + second * F::UNIT) / 16);
-                const uint32_t da = t0 + static_cast<uint32_t>(F::BUFS * BN + (2 * as.s + second) * F::A_COLS);
-                mma_ts_one(dst, da, db, idesc, add);
 #pragma unroll
-                for (int k = 1; k < kUnitCols / 16; ++k) mma_ts_one(dst, da + 8u * k, db + 2u * k, idesc, 1u);
-                add = 1u;
-                if (second == 1 || u + 1 == end) {
-                    commit_one(x_empty0 + 8u * xs.s);
-                    commit_one(a_empty0 + 8u * as.s);
-                    xs.next();
-                    as.next();
+                for (int part = 0; part < 2; ++part) {
+                    if (part == parts) break;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        if (u + k == end) break;
+                        uint32_t add = 1u;
+                        if (u + k == seg_end[part]) {     // a segment begins: its accumulator has been folded
+                            ok = ok && wait_warp_on(&acc_empty[part + acc[part].s], acc[part].phase ^ 1u, abort_flag);
+                            tc_fence_after();
+                            seg_end[part] = min(((u + k) / seg + 1) * seg, end);
+                            add = 0u;
+                        }
+                        if (!ok) break;
+                        const uint32_t dst = t0 + static_cast<uint32_t>(part * F::HALF + acc[part].s * BN);
+                        const uint64_t db = x0 + static_cast<uint64_t>((xs.s * F::STAGE + k * F::UNIT + part * (bn / 2) * 128) / 16);
+                        const uint32_t da = t0 + static_cast<uint32_t>(F::BUFS * BN + (2 * as.s + k) * F::A_COLS);
+                        mma_ts_one(dst, da, db, idesc, add);
+#pragma unroll
+                        for (int q = 1; q < kUnitCols / 16; ++q) mma_ts_one(dst, da + 8u * q, db + 2u * q, idesc, 1u);
+                        if (u + k + 1 == seg_end[part]) {
+                            commit_one(acc0 + 8u * (part + acc[part].s));
+                            acc[part].next();
+                        }
+                    }
                 }
-                if (u + 1 == seg_end) {
-                    commit_one(acc0 + 8u * acc.s);
-                    acc.next();
-                }
+                if (!ok) break;
+                commit_one(x_empty0 + 8u * xs.s);
+                commit_one(a_empty0 + 8u * as.s);
+                xs.next();
+                as.next();
             }
         }
         if (!ok && lane == 0) give_up();
@@ -320,12 +355,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         };
         int n = 0;                                        // stages so far: this group has those with n mod 2 == odd
         for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
-            const uint8_t *zeros[2];                      // of row r of either row tile; row r + 8's 8 behind
+            const uint32_t *zeros = zero_words(a.g, min(tile % out_tiles * (kTileOut / kTileRows) + 2 * quad, a.g.row_tiles - 1), r);
+            // the zeros of this group's next stage, on their way
+            uint32_t ahead[2];
+            auto load_zeros = [&](int u) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                zeros[i] = a.g.zeros + static_cast<int64_t>(min(tile % out_tiles * (kTileOut / kTileRows) + 2 * quad + i, a.g.row_tiles - 1)) *
-                                           a.g.groups * kTileRows + r;
-            int next_grid = begin;
+                for (int k = 0; k < 2; ++k) ahead[k] = zeros[a.g.groups > 1 ? static_cast<unsigned>(min(u + k, end - 1)) / static_cast<unsigned>(a.g.group_units) * 8 : 0];
+            };
+            load_zeros(begin + ((n & 1) != odd ? 2 : 0));
+            bool fresh = true;                            // (with one grid a row the first will do for all)
             for (int j = 0; ok && j < stages; ++j, ++n, as.next()) {
                 const int u0 = begin + 2 * j, both = u0 + 1 < end ? 2 : 1;
                 if ((n & 1) != odd) {
@@ -337,13 +375,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (k == both) break;
-                    if (u0 + k >= next_grid) {
-                        const int g = a.g.groups > 1 ? (u0 + k) / a.g.group_units : 0;
+                    if (fresh || a.g.groups > 1) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) TU::zero(static_cast<float>(zeros[i][g * kTileRows + 8 * h]), zero[i][h]);
-                        next_grid = (g + 1) * a.g.group_units;
+                            for (int h = 0; h < 2; ++h) TU::zero(zero_of(ahead[k], 2 * i + h), zero[i][h]);
+                        fresh = false;
                     }
                     codes();
                     if (!ok) break;
@@ -358,6 +395,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                     tmem_st_unit(dst + k * F::A_COLS + (16u << 16), v);
                 }
                 if (!ok) break;
+                if (a.g.groups > 1) load_zeros(u0 + 4);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
@@ -370,11 +408,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         const int quad = warp & 3, side = (warp - kFoldWarp) >> 2, row = quad * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(side * F::HALF);
         Turnstile<F::BUFS> buf;
+        const int part = parts == 2 ? side : 0, rows0 = parts == 2 ? side * (bn / 2) : side * F::HALF;   // the accumulator's, and the rows' place
+        const int cols = parts == 2 ? bn / 2 : min(bn - rows0, F::HALF);   // rows of x it has (none is left, or less, where bn is small)
         bool ok = true;
         for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
             const int out_tile = tile % out_tiles;
             const int64_t row_tile = min(out_tile * (kTileOut / kTileRows) + row / kTileRows, a.g.row_tiles - 1);
-            const int64_t m0 = static_cast<int64_t>(tile / out_tiles) * bn + side * F::HALF;
+            const int64_t m0 = static_cast<int64_t>(tile / out_tiles) * bn + rows0;
             float acc[F::HALF];
 #pragma unroll
             for (int i = 0; i < F::HALF; ++i) acc[i] = 0.0f;
@@ -384,7 +424,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
             for (int u = begin; u < end; buf.next()) {
                 const float scale = ahead;
                 if (g + 1 < a.g.groups) ahead = scales[++g * kTileRows];
-                ok = wait_warp_on(&acc_full[buf.s], buf.phase, abort_flag);
+                ok = wait_warp_on(&acc_full[part + buf.s], buf.phase, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -396,7 +436,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[buf.s]);
+                if (lane == 0) mbar_arrive(&acc_empty[part + buf.s]);
                 u = min((u / seg + 1) * seg, end);
             }
             if (!ok) break;
@@ -404,27 +444,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 // every product has been taken: x's ring is free for the sums, [row of x][output]
                 float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
-                for (int i = 0; i < F::HALF; ++i) sums[(side * F::HALF + i) * kTileOut + row] = acc[i];
+                for (int i = 0; i < F::HALF; ++i)
+                    if (i < cols) sums[(rows0 + i) * kTileOut + row] = acc[i];
                 continue;
             }
-            // out: a lane has an output, and OUT_COLS rows of x at a time pass through shared memory (registers have no index)
-            float *mine = out_stage + (warp - kFoldWarp) * (F::OUT_COLS * 32) + lane;
             const int64_t o = static_cast<int64_t>(out_tile) * kTileOut + row;
-            const bool on = o < a.g.q;
-            const float bias = on && a.bias ? to_f32(a.bias, a.bias_dtype, o) : 0.0f;
-            const int64_t left = min(a.rows - m0, static_cast<int64_t>(bn - side * F::HALF));   // rows of x that are there
-#pragma unroll
-            for (int part = 0; part < F::HALF / F::OUT_COLS; ++part) {
-#pragma unroll
-                for (int i = 0; i < F::OUT_COLS; ++i) mine[i * 32] = acc[part * F::OUT_COLS + i];
-                const int rows_here = static_cast<int>(left - part * F::OUT_COLS < F::OUT_COLS ? left - part * F::OUT_COLS : F::OUT_COLS);
-                if (!on) continue;
-                const int64_t m = m0 + part * F::OUT_COLS;
-                with_activation(a.act, [&](auto act) {
-#pragma unroll 4
-                    for (int i = 0; i < rows_here; ++i) finish<act.value>(a, mine[i * 32], m + i, o, bias);
-                });
-            }
+            const int64_t left = min(a.rows - m0, static_cast<int64_t>(cols));   // rows of x that are there
+            with_activation(a.act, [&](auto act) {
+                leave<F, act.value>(a, acc, out_stage + (warp - kFoldWarp) * (F::OUT_COLS * 32) + lane, m0, static_cast<int>(left), o);
+            });
         }
         if (!ok && lane == 0) give_up();
     }

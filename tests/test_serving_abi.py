@@ -140,7 +140,7 @@ def test_linear_size(bits, stored):
         tiles, units = -(-q // 16), -(-p // 64)
         groups = -(-p // group) if 0 < group < p else 1
         grids = tiles * groups * 16
-        assert qe.qe_linear_size(q, p, bits, group) == up(tiles * units * 128 * stored) + up(4 * grids) + up(grids)
+        assert qe.qe_linear_size(q, p, bits, group) == up(tiles * units * 128 * stored) + up(4 * grids) + up(-(-tiles // 2) * 2 * groups * 16)
 
 
 def test_linear_size_refuses(lib):
