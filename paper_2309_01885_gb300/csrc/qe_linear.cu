@@ -124,14 +124,17 @@ int linear_sms() {
 }
 
 RowsPlan rows_plan(const LinearArgs &a) {
-    const int64_t blocks = ceil_div(a.rows, a.rows <= 8 ? 8 : a.rows <= 16 ? 16 : 32), slots = 2 * linear_sms();
+    const int nt = static_cast<int>(a.rows <= 8 ? 1 : a.rows <= 16 ? 2 : a.rows <= 24 ? 3 : 4);
     RowsPlan best{1, 1};
     int64_t least = -1;
-    for (int tiles = a.g.bits == 8 ? 1 : 2; tiles >= 1; --tiles) {
-        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * blocks;
+    for (int tiles = a.g.bits == 8 || nt > 1 ? 1 : 2; tiles >= 1; --tiles) {
+        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * ceil_div(a.rows, 8 * nt);
         for (int ranks = 1; ranks <= 8; ++ranks) {
-            // rounds of CTAs, each with its units and what a CTA costs besides, in units
-            const int64_t cost = ceil_div(groups * ranks, slots) * (tiles * ceil_div(a.g.units, ranks) + 12);
+            // An SM's time goes by the units it turns: its CTAs', each with what a CTA costs besides; one CTA alone leaves
+            // pauses.  Measured (5 x 14848 x 59392, 4 bits, one or two row tiles a warp, us): 1: 2 ranks 139, 4 133, 8 115;
+            // 2: 2 ranks 172 (116 CTAs), 3 176, 5 110 (290), 7 115, 8 129.
+            const int64_t an_sm = ceil_div(groups * ranks, linear_sms());
+            const int64_t cost = an_sm * (tiles * ceil_div(a.g.units, ranks) + 10) * (an_sm == 1 ? 4 : 3);
             if (least < 0 || cost < least) {
                 least = cost;
                 best = RowsPlan{tiles, ranks};

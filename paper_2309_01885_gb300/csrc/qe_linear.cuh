@@ -60,25 +60,25 @@ struct LinearArgs {
 
 __host__ __device__ constexpr int stored_bits(int bits) { return bits <= 4 ? bits : 8; }
 
-// Word of a lane's B and place in a unit's words.
+// Place among a unit's words of a lane's word j of B.
 __host__ __device__ constexpr int unit_word(int B, int lane, int j) {
     return B == 3 ? 32 * j + lane : B == 8 ? 128 * (j >> 2) + 4 * lane + (j & 3) : B * lane + j;
 }
 
+// A lane's words of a unit; `from` is the lane's own place in it.
 template <int B>
-__device__ __forceinline__ void load_unit(const uint8_t *unit, int lane, uint32_t (&w)[B]) {
+__device__ __forceinline__ void load_unit(const uint8_t *from, uint32_t (&w)[B]) {
     if constexpr (B == 3) {
 #pragma unroll
-        for (int j = 0; j < 3; ++j)
-            asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[j]) : "l"(unit + 128 * j + 4 * lane));
+        for (int j = 0; j < 3; ++j) asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[j]) : "l"(from + 128 * j));
     } else if constexpr (B == 2) {
-        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(unit + 8 * lane));
+        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(from));
     } else {
 #pragma unroll
         for (int j = 0; j < B; j += 4)
             asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(w[j]), "=r"(w[j + 1]), "=r"(w[j + 2]), "=r"(w[j + 3])
-                         : "l"(unit + 128 * j + 16 * lane));
+                         : "l"(from + 128 * j));
     }
 }
 
@@ -147,9 +147,15 @@ struct Turn {
     static constexpr int LEVELS = B == 8 ? 1 : HALF ? (B == 4 ? 2 : 3) : (B == 2 ? 3 : B == 3 ? 2 : 1);
     using P = Pairs<HALF>;
 
-    static __device__ __forceinline__ void zero(float z, uint32_t (&k)[LEVELS]) {
+    // -(base / 2^s + z): a float with z 2^s as its last bits
+    static __device__ __forceinline__ void zero(uint32_t z, uint32_t (&k)[LEVELS]) {
+        if constexpr (B == 8 && !HALF) {
+            k[0] = P::of(-static_cast<float>(z));
+        } else {
+            constexpr uint32_t lead = P::kLead | 0x80008000u, step = HALF ? 0x04000400u : 0x00800080u;   // 1 of the exponent
 #pragma unroll
-        for (int i = 0; i < LEVELS; ++i) k[i] = P::of(B == 8 && !HALF ? -z : -(static_cast<float>(P::kBase >> (i * S)) + z));
+            for (int i = 0; i < LEVELS; ++i) k[i] = z * (0x00010001u << (i * S)) + (lead - step * static_cast<uint32_t>(i * S));
+        }
     }
 
     // pair number j (from bit 0) of a word
@@ -200,7 +206,7 @@ struct Turn {
 __device__ __forceinline__ const uint32_t *zero_words(const LinearGeom &g, int tile, int r) {
     return g.zeros + static_cast<int64_t>(tile >> 1) * g.groups * 8 + r;
 }
-__device__ __forceinline__ float zero_of(uint32_t word, int byte) { return static_cast<float>(word >> (8 * byte) & 0xffu); }
+__device__ __forceinline__ uint32_t zero_of(uint32_t word, int byte) { return word >> (8 * byte) & 0xffu; }
 
 __device__ __forceinline__ float to_f32(const void *p, int dtype, int64_t i) {
     if (dtype == QE_F32) return static_cast<const float *>(p)[i];

@@ -20,7 +20,7 @@
 namespace qe {
 namespace {
 
-constexpr int kRowWarps = 8, kChunk = 4;   // kChunk: units of x in a stage, and units of codes in registers
+constexpr int kRowWarps = 8, kChunk = 4;   // kChunk: units of x in a stage
 
 template <bool HALF>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -34,9 +34,24 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+template <int OFFSET>
 __device__ __forceinline__ void ldmatrix_x4(uint32_t at, uint32_t (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4 + %5];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(at), "n"(OFFSET));
 }
+
+// f(0) .. f(N - 1), as constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+
+// Units of codes on their way in a warp's registers.
+__host__ __device__ constexpr int rows_ahead(int B, int RT) { return RT == 2 ? 2 : B == 8 ? 2 : 4; }
 
 template <int RT, int NT>
 struct RowsOf {
@@ -52,8 +67,11 @@ __device__ __forceinline__ void cp_async16_part(uint32_t dst, const void *src, i
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes) : "memory");
 }
 
+// CTAs that an SM holds, by registers.
+__host__ __device__ constexpr int rows_ctas(int NT) { return NT == 1 ? 3 : 2; }
+
 template <int B, int RT, int NT, bool HALF, bool GROUPED>
-__global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs a) {
+__global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(const LinearArgs a) {
     using F = RowsOf<RT, NT>;
     using TU = Turn<B, HALF>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -74,36 +92,44 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
         tile[i] = min(tile0 + warp * RT + i, a.g.row_tiles - 1);
         code[i] = a.g.codes + (static_cast<int64_t>(tile[i]) * units + begin) * (128 * B);
     }
-    uint32_t w[kChunk][RT][B];
-    auto fetch = [&](int c, int s) {                      // unit s of chunk c
+    constexpr int AHEAD = rows_ahead(B, RT);
+    uint32_t w[AHEAD][RT][B];
+    auto fetch = [&](int s) {                             // unit s behind the beginning of the chunk that `code` stands at
 #pragma unroll
-        for (int i = 0; i < RT; ++i) load_unit<B>(code[i] + static_cast<int64_t>(c) * (kChunk * 128 * B) + s * (128 * B), lane, w[s][i]);
+        for (int i = 0; i < RT; ++i) load_unit<B>(code[i] + s * (128 * B), w[s % AHEAD][i]);
     };
 #pragma unroll
-    for (int s = 0; s < kChunk; ++s)
-        if (begin + s < end) fetch(0, s);
+    for (int i = 0; i < RT; ++i) code[i] += B == 3 ? 4 * lane : B == 2 ? 8 * lane : 16 * lane;
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (begin + s < end) fetch(s);
 
-    // x: piece e of a stage is row e / 32's 16 bytes e mod 32
+    // x: piece e of a stage is row e / 32's 16 bytes e mod 32: a thread brings the same piece of every eighth row
     const uint32_t ring = smem_u32(smem);
+    const int pc = threadIdx.x & 31, row0 = threadIdx.x >> 5;
+    const uint32_t x_to = ring + (pc >> 3) * F::UNIT_BYTES + row0 * 128 + (((pc & 7) ^ (row0 & 7)) << 4);
+    const int64_t x_col = static_cast<int64_t>(begin) * kUnitCols + 8 * pc, x_step = 8 * a.ldx;
+    const uint16_t *x_from = static_cast<const uint16_t *>(a.x) + (m0 + row0) * a.ldx + x_col;
+    const int x_rows = a.rows - m0 - row0 <= 0 ? 0 : static_cast<int>((a.rows - m0 - row0 + 7) / 8);   // of the thread's, that are there
+    const int x_chunks = a.x_vec ? static_cast<int>((a.g.p - static_cast<int64_t>(begin) * kUnitCols) / (kChunk * kUnitCols)) : 0;   // whole ones
     auto bring = [&](int c) {
         if (c < chunks) {
-            const uint32_t stage = ring + (c % F::STAGES) * F::STAGE;
-            const int64_t k0 = (static_cast<int64_t>(begin) + static_cast<int64_t>(c) * kChunk) * kUnitCols;
+            const uint32_t dst = x_to + (c % F::STAGES) * F::STAGE;
+            const uint16_t *src = x_from + static_cast<int64_t>(c) * (kChunk * kUnitCols);
+            if (c < x_chunks) {
 #pragma unroll
-            for (int j = 0; j < F::PIECES; ++j) {
-                const int e = threadIdx.x + j * kRowWarps * 32, row = e >> 5, pc = e & 31;
-                const int64_t m = m0 + row, k = k0 + 8 * pc;
-                const uint32_t dst = stage + (pc >> 3) * F::UNIT_BYTES + row * 128 + (((pc & 7) ^ (row & 7)) << 4);
-                const int64_t left = m < a.rows ? a.g.p - k : 0;
-                const int n = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
-                const uint16_t *src = static_cast<const uint16_t *>(a.x) + (n > 0 ? m * a.ldx + k : 0);
-                if (a.x_vec) {
-                    cp_async16_part(dst, src, 2 * n);
-                } else {
+                for (int j = 0; j < F::PIECES; ++j)
+                    cp_async16_part(dst + j * 1024, j < x_rows ? src + j * x_step : static_cast<const uint16_t *>(a.x), j < x_rows ? 16 : 0);
+            } else {                                      // the end of a row, or rows that are not aligned
+                const int64_t left = a.g.p - x_col - static_cast<int64_t>(c) * (kChunk * kUnitCols);
+#pragma unroll 1
+                for (int j = 0; j < F::PIECES; ++j) {
+                    const int n = j >= x_rows || left <= 0 ? 0 : left >= 8 ? 8 : static_cast<int>(left);
                     uint32_t v[4];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = (2 * q < n ? src[2 * q] : 0u) | (2 * q + 1 < n ? static_cast<uint32_t>(src[2 * q + 1]) << 16 : 0u);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                    for (int q = 0; q < 4; ++q)
+                        v[q] = (2 * q < n ? src[j * x_step + 2 * q] : 0u) | (2 * q + 1 < n ? static_cast<uint32_t>(src[j * x_step + 2 * q + 1]) << 16 : 0u);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + j * 1024), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
                 }
             }
         }
@@ -173,38 +199,48 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_linear_rows(const LinearArgs
         asm volatile("cp.async.wait_group %0;" ::"n"(F::STAGES - 2) : "memory");
         __syncthreads();                                  // the chunk is there, and everyone has done with the one before
         bring(c + F::STAGES - 1);
-        const uint32_t stage = (c % F::STAGES) * F::STAGE;
+        const uint32_t stage = (c % F::STAGES) * F::STAGE, at0 = mat0 + stage, at1 = mat1 + stage;
         const int u0 = begin + c * kChunk;
-#pragma unroll
-        for (int s = 0; s < kChunk; ++s) {
-            const int u = u0 + s;
-            if (u >= end) break;
+        auto unit = [&](auto s, bool more) {
             if constexpr (GROUPED) {
-                if (u == next_grid) {
-                    if (u > begin) fold();
+                if (u0 + s.value == next_grid) {
+                    if (u0 + s.value > begin) fold();
                     turn_grids();
                     if (++group < a.g.groups) load_grids(group);
                     next_grid = group * a.g.group_units;
                 }
             }
-            uint32_t v[RT][2][2][4];
+            // the few registers of x first, where there are more row tiles; else the turned codes
+            uint32_t x[NT][2][4], v[2][2][4];
+            auto operand = [&](auto n) {
+                ldmatrix_x4<s.value * F::UNIT_BYTES + n.value * 1024>(at0, x[n.value][0]);
+                ldmatrix_x4<s.value * F::UNIT_BYTES + n.value * 1024>(at1, x[n.value][1]);
+            };
+            auto products = [&](int i, int n) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) TU::unit(w[s][i], zero[i], v[i]);
-            if (u + kChunk < end) fetch(c + 1, s);
+                for (int q = 0; q < 2; ++q) {
+                    mma_16816<HALF>(sum[i][n], v[q][0][0], v[q][1][0], v[q][0][1], v[q][1][1], x[n][q][0], x[n][q][1]);
+                    mma_16816<HALF>(sum[i][n], v[q][0][2], v[q][1][2], v[q][0][3], v[q][1][3], x[n][q][2], x[n][q][3]);
+                }
+            };
+            if constexpr (RT > 1) each<NT>(operand);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                uint32_t x[2][4];
-                ldmatrix_x4(mat0 + stage + s * F::UNIT_BYTES + n * 1024, x[0]);
-                ldmatrix_x4(mat1 + stage + s * F::UNIT_BYTES + n * 1024, x[1]);
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        mma_16816<HALF>(sum[i][n], v[i][q][0][0], v[i][q][1][0], v[i][q][0][1], v[i][q][1][1], x[q][0], x[q][1]);
-                        mma_16816<HALF>(sum[i][n], v[i][q][0][2], v[i][q][1][2], v[i][q][0][3], v[i][q][1][3], x[q][2], x[q][3]);
-                    }
+            for (int i = 0; i < RT; ++i) {
+                TU::unit(w[s.value % AHEAD][i], zero[i], v);
+                if (i + 1 == RT && more) fetch(s.value + AHEAD);
+                each<NT>([&](auto n) {
+                    if constexpr (RT == 1) operand(n);
+                    products(i, n.value);
+                });
             }
-        }
+        };
+        if (u0 + kChunk + AHEAD <= end) each<kChunk>([&](auto s) { unit(s, true); });
+        else
+            each<kChunk>([&](auto s) {
+                if (u0 + s.value < end) unit(s, u0 + s.value + AHEAD < end);
+            });
+#pragma unroll
+        for (int i = 0; i < RT; ++i) code[i] += kChunk * 128 * B;
     }
     if constexpr (GROUPED) {
         if (begin < end) fold();
@@ -273,13 +309,15 @@ cudaError_t launch_rows_type(const LinearArgs &a, int ranks, cudaStream_t s) {
 template <int B, int RT>
 cudaError_t launch_rows_tokens(const LinearArgs &a, int ranks, cudaStream_t s) {
     if (a.rows <= 8) return launch_rows_type<B, RT, 1>(a, ranks, s);
-    if (a.rows <= 16) return launch_rows_type<B, RT, 2>(a, ranks, s);
-    return launch_rows_type<B, RT, 4>(a, ranks, s);
+    if constexpr (RT == 1) {
+        if (a.rows <= 16) return launch_rows_type<B, 1, 2>(a, ranks, s);
+        return a.rows <= 24 ? launch_rows_type<B, 1, 3>(a, ranks, s) : launch_rows_type<B, 1, 4>(a, ranks, s);
+    }
+    return cudaErrorInvalidValue;
 }
 
 template <int B>
 cudaError_t launch_rows_bits(const LinearArgs &a, cudaStream_t s) {
-    // a cluster's CTAs share the columns: as many as fill the GPU best, each with some chunks to itself
     const RowsPlan plan = rows_plan(a);
     if constexpr (B != 8) {
         if (plan.tiles == 2) return launch_rows_tokens<B, 2>(a, plan.ranks, s);

@@ -471,13 +471,30 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         const int failed = *abort_flag;
         if (!failed)
             with_activation(a.act, [&](auto act) {
-                for (int e = threadIdx.x - 32 * kFoldWarp; e < bn * kTileOut; e += 256) {
-                    const int tok = e / kTileOut, o = e % kTileOut;
-                    const int64_t m = m0 + tok, i = out0 + o;
-                    if (m >= a.rows || i >= a.g.q || tok % ranks != rank) continue;
-                    float v = 0.0f;
-                    for (int q = 0; q < ranks; ++q) v += cluster.map_shared_rank(sums, q)[tok * kTileOut + o];
-                    finish<act.value>(a, v, m, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
+                // four outputs of a row a thread, a warp a row
+                const int64_t i0 = out0 + 4 * lane;
+                float bias[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) bias[k] = a.bias && i0 + k < a.g.q ? to_f32(a.bias, a.bias_dtype, i0 + k) : 0.0f;
+                const int here = static_cast<int>(min(a.rows - m0, static_cast<int64_t>(bn)));
+#pragma unroll 1
+                for (int tok = (warp - kFoldWarp) * ranks + rank; tok < here; tok += 8 * ranks) {
+                    float4 part[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < ranks) part[q] = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(sums, q) + tok * kTileOut + 4 * lane);
+                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < ranks) {
+                            v[0] += part[q].x;
+                            v[1] += part[q].y;
+                            v[2] += part[q].z;
+                            v[3] += part[q].w;
+                        }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (i0 + k < a.g.q) finish<act.value>(a, v[k], m0 + tok, i0 + k, bias[k]);
                 }
             });
     }
