@@ -149,7 +149,7 @@ TilesPlan tiles_plan(const LinearArgs &a) {
     TilesPlan best{64, 64, 1};
     if (a.rows > 64) {
         // a group's end stops a tile of 256, which has one accumulator
-        const int room = a.rows <= 128 ? 128 : 256;
+        const int room = a.rows <= 128 ? 128 : a.g.bits == 8 ? 224 : 256;   // (8 bits' codes take shared memory from x)
         int64_t least = -1;
         for (int rows = room; rows >= room / 2; rows -= 32) {
             const int64_t cost = ceil_div(outs * ceil_div(a.rows, rows), sms) * (rows + 32);

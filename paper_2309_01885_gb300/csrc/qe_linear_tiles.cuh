@@ -39,15 +39,15 @@ constexpr int kTurnWarp = 4, kFoldWarp = 12;
 // BN: rows of x that a tile has room for; a call may use fewer (a multiple of 16).
 template <int BN>
 struct TilesOf {
-    static constexpr int UNIT = BN * 128, STAGE = 2 * UNIT, STAGES = BN == 256 ? 3 : BN == 128 ? 5 : 6;   // of x, two units each
-    static constexpr int BUFS = BN == 256 ? 1 : 2;                                   // accumulators
+    static constexpr int UNIT = BN * 128, STAGE = 2 * UNIT, STAGES = BN > 128 ? 3 : BN == 128 ? 4 : 6;   // of x, two units each
+    static constexpr int BUFS = BN > 128 ? 1 : 2;                                   // accumulators
     static constexpr int A_STAGES = 4, A_COLS = kUnitCols / 2;                       // of turned codes, two units each, behind these
     static constexpr int HALF = BN / 2;    // columns of a folding thread
     static constexpr int OUT_COLS = 8;     // that leave at once
-    static constexpr int CODE_RING = 24 * 1024, OUT_BYTES = 8 * OUT_COLS * 32 * 4;
+    static constexpr int CODE_RING = (BN == 256 ? 24 : BN > 128 ? 48 : BN == 128 ? 64 : 96) * 1024, OUT_BYTES = 8 * OUT_COLS * 32 * 4;
     static constexpr int SMEM = STAGES * STAGE + CODE_RING + OUT_BYTES + 1024 + 768;
     // registers a thread: 96 at launch, dealt out anew by role (warps 0-3, two warpgroups that turn, two that fold)
-    static constexpr int FOLD_REGS = BN == 256 ? 160 : 96, TURN_REGS = BN == 256 ? 56 : 96, LEAD_REGS = BN == 256 ? 48 : 96;
+    static constexpr int FOLD_REGS = BN > 128 ? 160 : 96, TURN_REGS = BN > 128 ? 56 : 96, LEAD_REGS = BN > 128 ? 48 : 96;
     static_assert(2 * FOLD_REGS + 2 * TURN_REGS + LEAD_REGS <= 5 * 96, "as many as the block was launched with");
     static_assert(BUFS * BN + A_STAGES * 2 * A_COLS <= 512, "tensor memory");
     static_assert(BN * kTileOut * 4 <= STAGES * STAGE, "a cluster's sums fit the ring");
@@ -136,58 +136,69 @@ struct Turnstile {
 // A lane's results leave: of output o, for `left` rows of x from m0 on.  Registers have no index, so eight rows at a time
 // pass through shared memory, in a loop: written out for all of them its instructions came from afar once a tile, and a
 // tile took 100000 cycles to leave.
-template <typename F, int ACT>
+template <typename F>
 __device__ __forceinline__ void leave(const LinearArgs &a, const float (&acc)[F::HALF], float *mine, int64_t m0, int left, int64_t o) {
     constexpr int N = F::OUT_COLS;
     const bool on = o < a.g.q;
     const float bias = on && a.bias ? to_f32(a.bias, a.bias_dtype, o) : 0.0f;
-    const uint16_t *res = a.residual ? static_cast<const uint16_t *>(a.residual) + m0 * a.ldr + o : nullptr;
+    const uint16_t *res = a.residual && on ? static_cast<const uint16_t *>(a.residual) + m0 * a.ldr + o : nullptr;
     uint16_t *y = static_cast<uint16_t *>(a.y) + m0 * a.ldy + o;
 #pragma unroll 1
     for (int part = 0; part < F::HALF / N && part * N < left; ++part) {
+        const int here = left - part * N;
+        uint16_t r[N];                                    // of the residual, on its way
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            r[i] = 0;
+            if (res && i < here) r[i] = res[i * a.ldr];
+        }
 #pragma unroll
         for (int q = 0; q < F::HALF / N; ++q)
             if (q == part)
 #pragma unroll
                 for (int i = 0; i < N; ++i) mine[i * 32] = acc[q * N + i];
-        uint16_t r[N];
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = mine[i * 32] + bias;
+        with_activation(a.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = activated<act.value>(v[i]);
+        });
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            r[i] = 0;
-            if (res && on && part * N + i < left) r[i] = res[i * a.ldr];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float v = activated<ACT>(mine[i * 32] + bias);
-            if (res) v += a.half ? __half2float(__ushort_as_half(r[i])) : __uint_as_float(static_cast<uint32_t>(r[i]) << 16);
-            const uint16_t h = a.half ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
-            if (on && part * N + i < left) y[i * a.ldy] = h;
+            if (res) v[i] += a.half ? __half2float(__ushort_as_half(r[i])) : __uint_as_float(static_cast<uint32_t>(r[i]) << 16);
+            const uint16_t h = a.half ? __half_as_ushort(__float2half_rn(v[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+            if (on && i < here) y[i * a.ldy] = h;
         }
         if (res) res += N * a.ldr;
         y += N * a.ldy;
     }
 }
 
-template <int B, int BN, bool HALF>
+// SHARED: a cluster's CTAs share a tile's columns.
+template <int B, int BN, bool HALF, bool SHARED>
 __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearArgs a, const int bn, const __grid_constant__ CUtensorMap xmap,
                                                                   const __grid_constant__ CUtensorMap cmap) {
     using F = TilesOf<BN>;
     using TU = Turn<B, HALF>;
-    constexpr int CODES = 8 * 128 * B, CODE_STAGES = F::CODE_RING / CODES;   // bytes of a unit's codes, of 128 outputs
+    constexpr int CODES = 8 * 128 * B;                    // bytes of a unit's codes, of 128 outputs
+    // Each group of turning warps has a ring of its own: a barrier's phases are told apart by one bit, so whoever waits on it
+    // has to see them all.
+    constexpr int CODE_FIT = F::CODE_RING / (2 * CODES), CODE_STAGES = CODE_FIT < 12 ? CODE_FIT : 12;
     extern __shared__ uint8_t raw_smem[];
     uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
     uint8_t *code_ring = smem + F::STAGES * F::STAGE;
     float *out_stage = reinterpret_cast<float *>(code_ring + F::CODE_RING);
     uint64_t *x_full = reinterpret_cast<uint64_t *>(code_ring + F::CODE_RING + F::OUT_BYTES), *x_empty = x_full + F::STAGES;
     uint64_t *a_full = x_empty + F::STAGES, *a_empty = a_full + F::A_STAGES;
-    uint64_t *code_full = a_empty + F::A_STAGES, *code_empty = code_full + CODE_STAGES;
-    uint64_t *acc_full = code_empty + CODE_STAGES, *acc_empty = acc_full + 2, *drain = acc_empty + 2;
+    uint64_t *code_full = a_empty + F::A_STAGES, *code_empty = code_full + 2 * CODE_STAGES;
+    uint64_t *acc_full = code_empty + 2 * CODE_STAGES, *acc_empty = acc_full + 2, *drain = acc_empty + 2;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    static_assert((2 * F::STAGES + 2 * F::A_STAGES + 5 + 2 * CODE_STAGES) * 8 + 8 <= 768, "room for the barriers");
+    static_assert((2 * F::STAGES + 2 * F::A_STAGES + 5 + 4 * CODE_STAGES) * 8 + 8 <= 768, "room for the barriers");
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
+    const int rank = SHARED ? static_cast<int>(cluster.block_rank()) : 0, ranks = SHARED ? static_cast<int>(cluster.num_blocks()) : 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // a tile's outputs run fastest; a cluster takes one tile, a CTA by itself every gridDim.x-th
     const int out_tiles = (a.g.row_tiles + 7) / 8;
@@ -213,7 +224,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
             mbar_init(&acc_full[b], 1);
             mbar_init(&acc_empty[b], parts == 2 ? 4 : 8);
         }
-        for (int s = 0; s < CODE_STAGES; ++s) {
+        for (int s = 0; s < 2 * CODE_STAGES; ++s) {
             mbar_init(&code_full[s], 1);
             mbar_init(&code_empty[s], 4);
         }
@@ -236,7 +247,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
     };
     // all threads of the cluster: sums are in place; and nobody leaves while they are read
     auto meet = [&]() {
-        if (ranks > 1) cluster.sync();
+        if constexpr (SHARED) cluster.sync();
         else __syncthreads();
     };
 
@@ -318,22 +329,30 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         mbar_wait_bounded(drain, 0u, nullptr);
     } else if (warp == 2) {
         if (lane == 0) {                                  // (row tiles past the last are zeros)
-            Turnstile<CODE_STAGES> at;
-            int64_t n = 0;
+            Turnstile<CODE_STAGES> at[2];                 // of either group
+            int64_t sent[2] = {0, 0};
+            int n = 0;                                    // stages so far
             bool ok = true;
             for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
                 const int row0 = tile % out_tiles * (kTileOut / kTileRows);
-                for (int u = begin; u < end; ++u, ++n) {
-                    ok = wait_on(&code_empty[at.s], at.phase ^ 1u, abort_flag);
-                    if (!ok) break;
-                    mbar_arrive_expect_tx(&code_full[at.s], CODES);
-                    tma_load_2d(&cmap, code_ring + at.s * CODES, &code_full[at.s], u * 32 * B, row0);
-                    at.next();
+                for (int u = begin; ok && u < end; u += 2, ++n) {
+                    const int group = n & 1;
+                    Turnstile<CODE_STAGES> &to = at[group];
+                    for (int k = 0; k < 2 && u + k < end; ++k) {
+                        const int place = group * CODE_STAGES + to.s;
+                        ok = wait_on(&code_empty[place], to.phase ^ 1u, abort_flag);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(&code_full[place], CODES);
+                        tma_load_2d(&cmap, code_ring + place * CODES, &code_full[place], (u + k) * 32 * B, row0);
+                        to.next();
+                        ++sent[group];
+                    }
                 }
             }
             if (!ok) give_up();
-            for (int64_t k = n > CODE_STAGES ? n - CODE_STAGES : 0; k < n; ++k)
-                mbar_wait_bounded(&code_full[k % CODE_STAGES], static_cast<uint32_t>(k / CODE_STAGES) & 1u, nullptr);
+            for (int group = 0; group < 2; ++group)
+                for (int64_t k = sent[group] > CODE_STAGES ? sent[group] - CODE_STAGES : 0; k < sent[group]; ++k)
+                    mbar_wait_bounded(&code_full[group * CODE_STAGES + k % CODE_STAGES], static_cast<uint32_t>(k / CODE_STAGES) & 1u, nullptr);
         }
     } else if (warp >= kTurnWarp && warp < kFoldWarp) {
         if constexpr (F::TURN_REGS < 96) fewer_registers<F::TURN_REGS>();
@@ -343,14 +362,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         Turnstile<CODE_STAGES> cs;                        // of the next unit's codes
         Turnstile<F::A_STAGES> as;
         bool ok = true;
-        // a unit's codes into registers; its place in the ring is free then
-        auto codes = [&]() {
-            ok = wait_warp_on(&code_full[cs.s], cs.phase, abort_flag);
+        auto codes = [&]() {                              // a unit's, into registers
+            const int place = odd * CODE_STAGES + cs.s;
+            ok = wait_warp_on(&code_full[place], cs.phase, abort_flag);
             if (!ok) return;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) read_unit<B>(code_ring + cs.s * CODES + (2 * quad + i) * (128 * B), lane, w[i]);
+            for (int i = 0; i < 2; ++i) read_unit<B>(code_ring + place * CODES + (2 * quad + i) * (128 * B), lane, w[i]);
+        };
+        // Their place in the ring is free once they have been turned, not once they have been asked for: TMA's writes are not
+        // held up by loads that are still on their way.
+        auto codes_done = [&]() {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&code_empty[cs.s]);
+            if (lane == 0) mbar_arrive(&code_empty[odd * CODE_STAGES + cs.s]);
             cs.next();
         };
         int n = 0;                                        // stages so far: this group has those with n mod 2 == odd
@@ -366,11 +389,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
             bool fresh = true;                            // (with one grid a row the first will do for all)
             for (int j = 0; ok && j < stages; ++j, ++n, as.next()) {
                 const int u0 = begin + 2 * j, both = u0 + 1 < end ? 2 : 1;
-                if ((n & 1) != odd) {
-                    cs.next();
-                    if (both == 2) cs.next();
-                    continue;
-                }
+                if ((n & 1) != odd) continue;
                 const uint32_t dst = to + static_cast<uint32_t>(2 * as.s * F::A_COLS);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -393,6 +412,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                     tmem_st_unit(dst + k * F::A_COLS, v);
                     TU::unit(w[1], zero[1], v);
                     tmem_st_unit(dst + k * F::A_COLS + (16u << 16), v);
+                    codes_done();
                 }
                 if (!ok) break;
                 if (a.g.groups > 1) load_zeros(u0 + 4);
@@ -440,19 +460,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 u = min((u / seg + 1) * seg, end);
             }
             if (!ok) break;
-            if (ranks > 1) {
+            if constexpr (SHARED) {
                 // every product has been taken: x's ring is free for the sums, [row of x][output]
                 float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
                 for (int i = 0; i < F::HALF; ++i)
                     if (i < cols) sums[(rows0 + i) * kTileOut + row] = acc[i];
-                continue;
+            } else {
+                const int64_t o = static_cast<int64_t>(out_tile) * kTileOut + row;
+                const int64_t left = min(a.rows - m0, static_cast<int64_t>(cols));   // rows of x that are there
+                leave<F>(a, acc, out_stage + (warp - kFoldWarp) * (F::OUT_COLS * 32) + lane, m0, static_cast<int>(left), o);
             }
-            const int64_t o = static_cast<int64_t>(out_tile) * kTileOut + row;
-            const int64_t left = min(a.rows - m0, static_cast<int64_t>(cols));   // rows of x that are there
-            with_activation(a.act, [&](auto act) {
-                leave<F, act.value>(a, acc, out_stage + (warp - kFoldWarp) * (F::OUT_COLS * 32) + lane, m0, static_cast<int>(left), o);
-            });
         }
         if (!ok && lane == 0) give_up();
     }
@@ -465,7 +483,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
     }
     tc_fence_before();
     meet();
-    if (ranks > 1 && first_tile < tiles) {                // the cluster's CTAs take rows of x in turn
+    if constexpr (SHARED) {                               // the cluster's CTAs take rows of x in turn
         const int64_t m0 = static_cast<int64_t>(first_tile / out_tiles) * bn, out0 = static_cast<int64_t>(first_tile % out_tiles) * kTileOut;
         const float *sums = reinterpret_cast<const float *>(smem);
         const int failed = *abort_flag;
@@ -479,19 +497,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 const int here = static_cast<int>(min(a.rows - m0, static_cast<int64_t>(bn)));
 #pragma unroll 1
                 for (int tok = (warp - kFoldWarp) * ranks + rank; tok < here; tok += 8 * ranks) {
-                    float4 part[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (q < ranks) part[q] = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(sums, q) + tok * kTileOut + 4 * lane);
                     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (q < ranks) {
-                            v[0] += part[q].x;
-                            v[1] += part[q].y;
-                            v[2] += part[q].z;
-                            v[3] += part[q].w;
-                        }
+#pragma unroll 4
+                    for (int q = 0; q < ranks; ++q) {
+                        const float4 x = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(sums, q) + tok * kTileOut + 4 * lane);
+                        v[0] += x.x;
+                        v[1] += x.y;
+                        v[2] += x.z;
+                        v[3] += x.w;
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         if (i0 + k < a.g.q) finish<act.value>(a, v[k], m0 + tok, i0 + k, bias[k]);
@@ -501,7 +515,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
     meet();
 }
 
-template <int B, int BN, bool HALF>
+template <int B, int BN, bool HALF, bool SHARED>
 cudaError_t launch_tiles_as(const LinearArgs &a, const TilesPlan &plan, cudaStream_t s) {
     using F = TilesOf<BN>;
     CUtensorMap map, codes;
@@ -510,7 +524,7 @@ cudaError_t launch_tiles_as(const LinearArgs &a, const TilesPlan &plan, cudaStre
         !make_tmap_words(&codes, a.g.codes, static_cast<uint64_t>(a.g.row_tiles), static_cast<uint64_t>(a.g.units) * 32 * B, 32 * B, kTileOut / kTileRows))
         return cudaErrorInvalidValue;
     static std::atomic<uint64_t> raised{0};
-    const void *kernel = reinterpret_cast<const void *>(k_linear_tiles<B, BN, HALF>);
+    const void *kernel = reinterpret_cast<const void *>(k_linear_tiles<B, BN, HALF, SHARED>);
     cudaError_t e = raise_limit(kernel, F::SMEM, raised);
     if (e != cudaSuccess) return e;
     const int64_t tiles = ceil_div(a.g.q, kTileOut) * ceil_div(a.rows, plan.rows), sms = linear_sms();
@@ -525,12 +539,13 @@ cudaError_t launch_tiles_as(const LinearArgs &a, const TilesPlan &plan, cudaStre
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_linear_tiles<B, BN, HALF>, a, plan.rows, map, codes);
+    return cudaLaunchKernelEx(&cfg, k_linear_tiles<B, BN, HALF, SHARED>, a, plan.rows, map, codes);
 }
 
 template <int B, int BN>
 cudaError_t launch_tiles_type(const LinearArgs &a, const TilesPlan &plan, cudaStream_t s) {
-    return a.half ? launch_tiles_as<B, BN, true>(a, plan, s) : launch_tiles_as<B, BN, false>(a, plan, s);
+    if (plan.ranks > 1) return a.half ? launch_tiles_as<B, BN, true, true>(a, plan, s) : launch_tiles_as<B, BN, false, true>(a, plan, s);
+    return a.half ? launch_tiles_as<B, BN, true, false>(a, plan, s) : launch_tiles_as<B, BN, false, false>(a, plan, s);
 }
 
 template <int B>
@@ -538,7 +553,7 @@ cudaError_t launch_tiles_bits(const LinearArgs &a, cudaStream_t s) {
     const TilesPlan plan = tiles_plan(a);
     if (plan.room == 64) return launch_tiles_type<B, 64>(a, plan, s);
     if (plan.room == 128) return launch_tiles_type<B, 128>(a, plan, s);
-    return launch_tiles_type<B, 256>(a, plan, s);
+    return launch_tiles_type<B, B == 8 ? 224 : 256>(a, plan, s);
 }
 
 }  // namespace

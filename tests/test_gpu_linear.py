@@ -118,6 +118,30 @@ def test_epilogue(dtype, rows, act):
     check(out, w64, x, None, act, residual)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_over_their_range(act, dtype):
+    """Sums from far below 0 to far above it, taken from one row of ones: fp32 functions off by 2^-19 of their value, plus
+    what one unit in the last place of the sum, its distance from 0, makes (steepness up to |y| times the value in the tails)."""
+    n = 4001
+    want = torch.linspace(-95.0, 95.0, n, device="cuda", dtype=torch.float64)
+    want[::3] *= 0.05
+    codes = torch.ones(n, 64, dtype=torch.uint8, device="cuda")
+    scales = (want / 64).float()
+    w = qe.QuantizedWeights(codes, scales, torch.zeros(n, device="cuda"), 4)
+    for rows in (1, 40):
+        x = torch.ones(rows, 64, device="cuda").to(dtype)
+        got = qe.qe_linear(w, x, activation=act)[0].double()
+        y = scales.double() * 64
+        f = {"none": lambda v: v, "relu": lambda v: v.clamp(min=0), "silu": lambda v: v * torch.exp(-torch.nn.functional.softplus(-v)),
+             "gelu": lambda v: 0.5 * v * torch.erfc(-v / math.sqrt(2.0)),
+             "gelu_tanh": lambda v: v * torch.exp(-torch.nn.functional.softplus(-2.0 * math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3)))}[act]
+        r = f(y)
+        off = 2.0 ** -19 + 2.0 ** -22 * (y * y + 1.0) * (1.0 if act in ("gelu", "gelu_tanh", "silu") else 0.0) * (1.0 + y.abs() * (act == "gelu_tanh"))
+        # below 2^-126 binary32's own exponentials end
+        assert bool(((got - r).abs() <= r.abs() * (1.01 * HALF_ULP[dtype] + off) + SMALLEST[dtype] + 2.0 ** -118).all())
+
+
 @pytest.mark.parametrize("rows", [1, 7, 30, 70, 260])
 def test_strides_and_alignment(rows):
     """x, residual and results inside wider arrays, at any alignment; what lies around the results stays."""
@@ -182,6 +206,20 @@ def test_same_answer_every_time(rows):
     first = qe.qe_linear(w, x)
     check(first, weights64(codes, scales, zeros, 128), x)
     for _ in range(20):
+        assert qe.qe_linear(w, x).equal(first)
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("q,p,rows,group", [(4096, 8320, 4000, 0), (4000, 2112, 5000, 64), (4096, 4160, 3000, 128), (2048, 20000, 300, 0), (30000, 320, 400, 0),
+                                            (40000, 200, 60, 0), (40000, 200, 100, 64)])
+def test_many_tiles(bits, q, p, rows, group):
+    """More tiles than there are CTAs, each with many steps: rings go round hundreds of times, and answers do not change."""
+    codes, scales, zeros = layer(q, p, bits, group, q + p + bits)
+    w = qe.QuantizedWeights(codes, scales, zeros, bits, group_size=group)
+    x = torch.randn(rows, p, generator=gen(bits), device="cuda").to(torch.bfloat16)
+    first = qe.qe_linear(w, x)
+    check(first, weights64(codes, scales, zeros, group), x)
+    for _ in range(5):
         assert qe.qe_linear(w, x).equal(first)
 
 
