@@ -206,7 +206,8 @@ struct TcCfg {
     static constexpr int SMEM_ASKED = SMEM > 120 * 1024 ? SMEM : 120 * 1024;
 };
 
-template <int C, int GC>
+// CARRY: what rounding P to fp16 leaves out is multiplied with V too (fp16 results of a batch with a shared prefix).
+template <int C, int GC, bool CARRY>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a) {
     using F = TcCfg<C, GC>;
     constexpr int D = F::D, NG = F::NG;
@@ -303,8 +304,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 const uint32_t pa = t0 + i * kTile, d = t0 + 2 * kTile + i * kTile;
                 const uint32_t sum = j > 0 ? 1u : 0u;
 #pragma unroll
-                for (int k = 0; k < kTile / 16; ++k)      // either half's P stands where its scores began
-                    mma_ts_one(d, pa + (k >> 2) * kHalf + 8 * (k & 3), vb + (k >> 2) * (D * 8) + 2 * (k & 3), id, k == 0 ? sum : 1u);
+                for (int k = 0; k < kTile / 16; ++k) {    // either half's P stands where its scores began
+                    const uint64_t v = vb + (k >> 2) * (D * 8) + 2 * (k & 3);
+                    if constexpr (CARRY) {                // (of each 32 tokens P, then what it left out)
+                        const uint32_t p = pa + (k >> 2) * kHalf + 32 * (k >> 1 & 1) + 8 * (k & 1);
+                        mma_ts_one(d, p, v, id, k == 0 ? sum : 1u);
+                        mma_ts_one(d, p + 16, v, id, 1u);
+                    } else {
+                        mma_ts_one(d, pa + (k >> 2) * kHalf + 8 * (k & 3), v, id, k == 0 ? sum : 1u);
+                    }
+                }
             };
             bool ok = wait_warp(q_full, 0u) && wait_warp(&k_full[0], 0u);
             tc_fence_after();
@@ -705,8 +714,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_tiles(const AttendArgs a
                 return total(sum) * in.val_down[c0 + c];
             };
             const int pair_bar = 1 + 4 * i + quad;        // this warp and the other group's warp of these rows
-            bool raise = j == 0;
-            if (j > 0) {
+            bool raise = !CARRY && j == 0;
+            if constexpr (CARRY) {
+                // P and its remainder take the place of their scores 32 tokens at a time, so the maximum comes first
+                float top = kFloor;
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    float v[32];
+                    fetch(c, v);
+                    top = fmaxf(top, highest(c, v) - kAbove);
+                }
+                row_max[grp * 2 * kTile + p] = ok ? top : CUDART_NAN_F;
+                sync_64(pair_bar);
+                const float theirs = row_max[(1 - grp) * 2 * kTile + p];
+                ok = ok && theirs == theirs;
+                if (!ok) break;                           // one of the two gave up: both leave at the same barrier
+                top = fmaxf(top, theirs);
+                if (any_of_64(pair_bar, j == 0 || top > m + kRaise)) {
+                    const float now = fmaxf(m, top), f = ex2(m - now);
+                    m = now;
+                    l *= f;
+                    if (j > 0) {                          // either group has half of the channels
+#pragma unroll 1
+                        for (int c = grp * (D / 32); c < (grp + 1) * (D / 32); ++c) {
+                            float o[16];
+                            tmem_ld_x16(to + 16 * c, o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] *= f;
+                            tmem_st_x16(to + 16 * c, o);
+                        }
+                    }
+                }
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    float v[32];
+                    uint32_t h[16];
+                    fetch(c, v);
+                    l += powers(c, v, h);                 // (v: the exponentials)
+                    tmem_st_x16(ts + 32 * c, h);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        h[e] = pack_f16(v[2 * e] - __low2float(as_half2(h[e])), v[2 * e + 1] - __high2float(as_half2(h[e])));
+                    tmem_st_x16(ts + 32 * c + 16, h);
+                }
+            } else if (j > 0) {
                 // taken at the old maximum at once; only where one exceeds 2^(kAbove + kRaise) (seldom) it is all done again
                 uint32_t h[32];
                 float v[32];
@@ -919,14 +970,19 @@ __global__ void __launch_bounds__(256) k_attend_join_tiles(const AttendArgs a) {
     }
 }
 
-template <int C, int GC>
-cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) {
+template <int C, int GC, bool CARRY>
+cudaError_t launch_tiles_as(const AttendArgs &a, const dim3 &grid, cudaStream_t s) {
     using F = TcCfg<C, GC>;
     static std::atomic<uint64_t> raised{0};
-    const cudaError_t e = raise_smem(reinterpret_cast<const void *>(k_attend_tiles<C, GC>), F::SMEM_ASKED, raised);
+    const cudaError_t e = raise_smem(reinterpret_cast<const void *>(k_attend_tiles<C, GC, CARRY>), F::SMEM_ASKED, raised);
     if (e != cudaSuccess) return e;
-    k_attend_tiles<C, GC><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
+    k_attend_tiles<C, GC, CARRY><<<grid, kThreads, F::SMEM_ASKED, s>>>(a);
     return cudaGetLastError();
+}
+
+template <int C, int GC>
+cudaError_t launch_tiles(const AttendArgs &a, const dim3 &grid, cudaStream_t s) {
+    return a.prefix > 0 && a.half ? launch_tiles_as<C, GC, true>(a, grid, s) : launch_tiles_as<C, GC, false>(a, grid, s);
 }
 
 }  // namespace
