@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -687,6 +688,19 @@ class PagePool:
         self.ring, self.state = ring, state
 
 
+# the structs of the calls that a serving step makes most often, as the library reads them (packed, they are made in a
+# third of the time that a ctypes structure takes)
+_GROWTH = struct.Struct("@4q11P")
+_HEADS = struct.Struct("@q5i4x2P4q2P4q2Pf4x2P")
+_PRODUCT = struct.Struct("@q2iPqPi4xPqPq")
+
+
+def _grow_index(cache: KVCache, t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> int:
+    if t.dtype is not dtype or t.get_device() != cache._index or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {n} entries on the cache's device")
+    return t.data_ptr()
+
+
 def qe_cache_grow_workspace(seqs: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load().qe_cache_grow_workspace(seqs, ctypes.byref(n)), "qe_cache_grow_workspace")
@@ -708,19 +722,15 @@ def qe_cache_grow(cache: KVCache, pool: PagePool, kv_len: torch.Tensor, new_toke
             return qe_cache_grow(cache, pool, kv_len, new_tokens, page_table, max_tokens, ends=ends, prefix=prefix, kv_len_out=kv_len_out,
                                  state_out=state_out, q_start=q_start, slots=slots, positions=positions, workspace=workspace)
     seqs = kv_len.shape[0]
-
-    def index(t, dtype, n, what):
-        at = _cache_index(cache, t, dtype, 1, what)
-        if t.shape[0] != n:
-            raise ValueError(f"{what}: expected {n} entries")
-        return at
-
-    if not page_table.is_contiguous() or page_table.shape[0] != seqs:
+    if not page_table.is_contiguous() or page_table.dim() != 2 or page_table.shape[0] != seqs:
         raise ValueError("page_table: expected a contiguous tensor of seqs rows")
     dev = cache.device
-    q_start = torch.empty(seqs + 1, dtype=torch.int32, device=dev) if q_start is None else q_start
-    slots = torch.empty(max_tokens, dtype=torch.int64, device=dev) if slots is None else slots
-    positions = torch.empty(max_tokens, dtype=torch.int32, device=dev) if positions is None else positions
+    if q_start is None:
+        q_start = torch.empty(seqs + 1, dtype=torch.int32, device=dev)
+    if slots is None:
+        slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+    if positions is None:
+        positions = torch.empty(max_tokens, dtype=torch.int32, device=dev)
     if ends is not None and ends.dtype is torch.bool:
         ends = ends.view(torch.uint8)
     ws, ws_bytes = None, 0
@@ -728,15 +738,16 @@ def qe_cache_grow(cache: KVCache, pool: PagePool, kv_len: torch.Tensor, new_toke
         if workspace.get_device() != cache._index or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous tensor on the cache's device")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    lens, state = index(kv_len, torch.int32, seqs, "kv_len"), index(pool.state, torch.int32, 2, "state")
-    gr = QEGrowth(seqs, max_tokens, prefix, page_table.shape[-1], index(new_tokens, torch.int32, seqs, "new_tokens"),
-                  None if ends is None else index(ends, torch.uint8, seqs, "ends"), lens,
-                  lens if kv_len_out is None else index(kv_len_out, torch.int32, seqs, "kv_len_out"),
-                  _cache_index(cache, page_table, torch.int32, 2, "page_table"), index(pool.ring, torch.int32, cache.pages, "ring"), state,
-                  state if state_out is None else index(state_out, torch.int32, 2, "state_out"),
-                  index(q_start, torch.int32, seqs + 1, "q_start"), index(slots, torch.int64, max_tokens, "slots"),
-                  index(positions, torch.int32, max_tokens, "positions"))
-    st = (_lib or load()).qe_cache_grow(cache._ref, ctypes.addressof(gr), ws, ws_bytes, _raw_stream(cache._index))
+    i32 = torch.int32
+    lens, state = _grow_index(cache, kv_len, i32, seqs, "kv_len"), _grow_index(cache, pool.state, i32, 2, "state")
+    gr = _GROWTH.pack(seqs, max_tokens, prefix, page_table.shape[1], _grow_index(cache, new_tokens, i32, seqs, "new_tokens"),
+                      0 if ends is None else _grow_index(cache, ends, torch.uint8, seqs, "ends"), lens,
+                      lens if kv_len_out is None else _grow_index(cache, kv_len_out, i32, seqs, "kv_len_out"),
+                      _cache_index(cache, page_table, i32, 2, "page_table"), _grow_index(cache, pool.ring, i32, cache.pages, "ring"), state,
+                      state if state_out is None else _grow_index(cache, state_out, i32, 2, "state_out"),
+                      _grow_index(cache, q_start, i32, seqs + 1, "q_start"), _grow_index(cache, slots, torch.int64, max_tokens, "slots"),
+                      _grow_index(cache, positions, i32, max_tokens, "positions"))
+    st = (_lib or load()).qe_cache_grow(cache._ref, gr, ws, ws_bytes, _raw_stream(cache._index))
     if st != QE_OK:
         raise QEError(st, "qe_cache_grow")
     return q_start, slots, positions
@@ -778,47 +789,55 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
             return qe_norm_rotate(q, k, positions, rope, q_weight=q_weight, k_weight=k_weight, eps=eps, q_out=q_out, k_out=k_out)
     if first.dim() != 3:
         raise ValueError("expected tokens x heads x head_dim")
-    n, dim, dtype = first.shape[0], first.shape[2], first.dtype
-    h = QEHeads(tokens=n, head_dim=dim, dtype=_cache_dtype(dtype), eps=eps)
-    weights = [w for w in (q_weight, k_weight) if w is not None]
-    for w in weights:
-        if w.shape != (dim,) or not w.is_contiguous() or w.get_device() != index or w.dtype is not weights[0].dtype:
-            raise ValueError("weights: expected contiguous tensors of head_dim entries on q's device, of one dtype")
-    if weights:
-        h.weight_dtype = _cache_dtype(weights[0].dtype)
+    n, _, dim = first.shape
+    dtype = first.dtype
+    code, weight_code, at, turns = _cache_dtype(dtype), 0, 0, 0
     if rope is not None:
-        if positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or not positions.is_contiguous() or \
-                positions.get_device() != index:
+        if positions is None or positions.dtype is not torch.int32 or positions.dim() != 1 or positions.shape[0] != n or \
+                not positions.is_contiguous() or positions.get_device() != index:
             raise ValueError("positions: expected a contiguous int32 tensor of tokens entries on q's device")
-        h.positions, h.rope = positions.data_ptr(), rope._ref
-
-    def heads(t, what, like=None):
-        if t.dim() != 3 or t.shape[0] != n or t.shape[2] != dim or (t.stride(2) != 1 and dim > 1) or t.dtype is not dtype or \
-                t.get_device() != index or (like is not None and t.shape != like.shape):
-            raise ValueError(f"{what}: expected {n} x heads x {dim} with contiguous channels, of one dtype and device")
-        return t.data_ptr(), t.stride(0), t.stride(1)
-
-    found = []
-    for name, t, out, w in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
-        if t is None:
-            if out is not None or w is not None:
-                raise ValueError(f"{name} is not given")
-            found.append(None)
-            continue
-        at, token, head = heads(t, name)
-        if out is None:
-            out = torch.empty(t.shape, dtype=dtype, device=t.device)
-        o_at, o_token, o_head = heads(out, name + "_out", t)
-        wp = None if w is None else w.data_ptr()
-        if name == "q":
-            h.q_heads, h.Q, h.q_token, h.q_head, h.q_out, h.qo_token, h.qo_head, h.q_weight = t.shape[1], at, token, head, o_at, o_token, o_head, wp
-        else:
-            h.k_heads, h.K, h.k_token, h.k_head, h.k_out, h.ko_token, h.ko_head, h.k_weight = t.shape[1], at, token, head, o_at, o_token, o_head, wp
-        found.append(out)
-    st = (_lib or load()).qe_norm_rotate(ctypes.addressof(h), _raw_stream(index))
+        at, turns = positions.data_ptr(), rope._ref
+    weight = q_weight if q_weight is not None else k_weight
+    if weight is not None:
+        weight_code = _cache_dtype(weight.dtype)
+    q_heads, q_at, q_token, q_head, q_to, qo_token, qo_head, q_w, q_out = \
+        _rotate_part("q", q, q_out, q_weight, n, dim, dtype, index, weight)
+    k_heads, k_at, k_token, k_head, k_to, ko_token, ko_head, k_w, k_out = \
+        _rotate_part("k", k, k_out, k_weight, n, dim, dtype, index, weight)
+    st = (_lib or load()).qe_norm_rotate(
+        _HEADS.pack(n, q_heads, k_heads, dim, code, weight_code, q_at, k_at, q_token, q_head, k_token, k_head, q_to, k_to, qo_token, qo_head,
+                    ko_token, ko_head, q_w, k_w, eps, at, turns), _raw_stream(index))
     if st != QE_OK:
         raise QEError(st, "qe_norm_rotate")
-    return tuple(found)
+    return q_out, k_out
+
+
+def _rotate_part(name, t, out, w, n, dim, dtype, index, weight):
+    """What the library wants to know of the queries or the keys, and where their results go."""
+    if t is None:
+        if out is not None or w is not None:
+            raise ValueError(f"{name} is not given")
+        return 0, 0, 0, 0, 0, 0, 0, 0, None
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != dim or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{name}: expected {n} x heads x {dim}, of one dtype and device")
+    token, head, channel = t.stride()
+    heads = shape[1]
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=t.device)
+        o_token, o_head, o_channel = heads * dim, dim, 1
+    else:
+        if out.shape != shape or out.dtype is not dtype or out.get_device() != index:
+            raise ValueError(f"{name}_out: expected {name}'s shape, dtype and device")
+        o_token, o_head, o_channel = out.stride()
+    if channel != 1 or o_channel != 1:
+        raise ValueError(f"{name}: expected contiguous channels")
+    at = 0
+    if w is not None:
+        if w.dim() != 1 or w.shape[0] != dim or not w.is_contiguous() or w.get_device() != index or w.dtype is not weight.dtype:
+            raise ValueError("weights: expected contiguous tensors of head_dim entries on q's device, of one dtype")
+        at = w.data_ptr()
+    return heads, t.data_ptr(), token, head, out.data_ptr(), o_token, o_head, at, out
 
 
 # ---- products with a quantized layer --------------------------------------------------------------------------------------
@@ -884,29 +903,36 @@ def qe_linear(weights: QuantizedWeights, x: torch.Tensor, *, bias: torch.Tensor 
     if x.dim() != 2 or x.shape[1] != p:
         raise ValueError(f"x: expected rows x {p}")
     rows = x.shape[0]
+    x_at, ldx = _linear_matrix(x, rows, p, dtype, index, "x")
     if out is None:
         out = torch.empty((rows, q), dtype=dtype, device=weights.device)
-
-    def matrix(t, cols, what):
-        if t.dim() != 2 or t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1) or t.dtype is not dtype or t.get_device() != index:
-            raise ValueError(f"{what}: expected {rows} x {cols} with contiguous columns, in x's dtype, on the layer's device")
-        return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
-
-    pr = QEProduct(rows=rows, dtype=_cache_dtype(dtype), act=act)
-    pr.X, pr.ldx = matrix(x, p, "x")
-    pr.Y, pr.ldy = matrix(out, q, "out")
+        y_at, ldy = out.data_ptr(), q
+    else:
+        y_at, ldy = _linear_matrix(out, rows, q, dtype, index, "out")
+    res_at = ldr = bias_at = bias_dtype = 0
     if residual is not None:
-        pr.residual, pr.ldr = matrix(residual, q, "residual")
+        res_at, ldr = _linear_matrix(residual, rows, q, dtype, index, "residual")
     if bias is not None:
-        if bias.shape != (q,) or not bias.is_contiguous() or bias.get_device() != index:
+        if bias.dim() != 1 or bias.shape[0] != q or not bias.is_contiguous() or bias.get_device() != index:
             raise ValueError(f"bias: expected a contiguous tensor of {q} values on the layer's device")
-        pr.bias, pr.bias_dtype = bias.data_ptr(), _cache_dtype(bias.dtype)
+        bias_at, bias_dtype = bias.data_ptr(), _cache_dtype(bias.dtype)
     ws, ws_bytes = None, 0
     if workspace is not None:
         if workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous tensor on the layer's device")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = (_lib or load()).qe_linear(weights._ref, ctypes.addressof(pr), ws, ws_bytes, _raw_stream(index))
+    st = (_lib or load()).qe_linear(weights._ref, _PRODUCT.pack(rows, _cache_dtype(dtype), bias_dtype, x_at, ldx, bias_at, act, res_at, ldr, y_at, ldy),
+                                    ws, ws_bytes, _raw_stream(index))
     if st != QE_OK:
         raise QEError(st, "qe_linear")
     return out
+
+
+def _linear_matrix(t: torch.Tensor, rows: int, cols: int, dtype, index: int, what: str):
+    """Address and pitch of a matrix with contiguous columns."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{what}: expected {rows} x {cols} in x's dtype, on the layer's device")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: expected contiguous columns")
+    return t.data_ptr(), ld if rows > 1 else cols

@@ -32,6 +32,17 @@ def test_structs_match_header(tmp_path, name, mirror):
     assert out == [ctypes.sizeof(mirror)] + [getattr(mirror, f).offset for f in fields]
 
 
+@pytest.mark.parametrize("packed,mirror", [(qe._GROWTH, qe.QEGrowth), (qe._HEADS, qe.QEHeads), (qe._PRODUCT, qe.QEProduct)])
+def test_packed_structs_match_their_mirrors(packed, mirror):
+    """Field by field: a number in one of them comes out of the mirror under its name, and nowhere else."""
+    assert packed.size <= ctypes.sizeof(mirror) <= packed.size + 4
+    for i, (name, kind) in enumerate(mirror._fields_):
+        values = [0.0 if k is ctypes.c_float else 0 for _, k in mirror._fields_]
+        values[i] = 2.0 if kind is ctypes.c_float else 77
+        got = mirror.from_buffer_copy(packed.pack(*values) + b"\0" * 8)
+        assert {n: getattr(got, n) or 0 for n, _ in mirror._fields_} == {n: v for (n, _), v in zip(mirror._fields_, values)}
+
+
 def filled(struct, values):
     s = struct()
     for k, v in values.items():
