@@ -2,10 +2,11 @@
 
     python examples/quantized_attention.py            # needs the GPU and the built libqe.so
 
-The four projections of an attention layer are quantized from calibration inputs.  A batch of prompts
-then goes through the layer in one ragged call (append its keys and values, attend over them), after which
-every sequence is decoded token by token.  The same is computed with the unquantized layer and keys and
-values in binary32, and the relative distance of the results is printed for each stage.
+The four projections of an attention layer are quantized from calibration inputs and stay quantized: their products are
+formed from the codes.  A prompt that all sequences share goes through the layer once; then a batch of prompts behind it in
+one ragged call (pages and slots for their tokens, projections, norms and rotation of queries and keys, attention), after
+which every sequence is decoded token by token.  The same is computed with the unquantized layer and keys and values in
+binary32, and the relative distance of the results is printed for each stage.
 """
 from __future__ import annotations
 
@@ -18,32 +19,19 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2309_01885_gb300 import inputs, qe  # noqa: E402
 
 
-class PagedSequences:
-    """Pages handed out to sequences as they grow: the page table and the slots of new tokens."""
-
-    def __init__(self, cache: qe.KVCache, seqs: int, max_len: int):
-        self.page = cache.page_size
-        self.table = torch.full((seqs, -(-max_len // self.page)), -1, dtype=torch.int32)
-        self.length = [0] * seqs
-        self.free = list(range(cache.pages))
-        self.device = cache.device
-
-    def grow(self, seq: int, tokens: int) -> torch.Tensor:
-        """Slots of the next `tokens` tokens of sequence `seq`."""
-        j = torch.arange(self.length[seq], self.length[seq] + tokens)
-        for p in range(-(-self.length[seq] // self.page), -(-(self.length[seq] + tokens) // self.page)):
-            self.table[seq, p] = self.free.pop()
-        self.length[seq] += tokens
-        return self.table[seq, j // self.page].long() * self.page + j % self.page
-
-    def lengths(self) -> torch.Tensor:
-        return torch.tensor(self.length, dtype=torch.int32, device=self.device)
+def quantized(W: torch.Tensor, X: torch.Tensor, bits: int, iters: int) -> dict:
+    """Codes, scales and zeros that QuantEase leaves."""
+    return qe.qe_quantize_layer(W, qe.qe_build_sigma(X), bits, iters)
 
 
-def quantized_projection(W: torch.Tensor, X: torch.Tensor, bits: int, iters: int) -> torch.Tensor:
-    """The weights that QuantEase leaves, in bf16."""
-    out = qe.qe_quantize_layer(W, qe.qe_build_sigma(X), bits, iters)
-    return (out["scales"][:, None] * (out["codes"].float() - out["zeros"][:, None])).to(torch.bfloat16)
+def normed_and_rotated(x, positions, theta=10000.0):
+    """Heads over their root mean square, then pair (i, i + dim / 2) turned by position theta^(-2 i / dim), in binary32."""
+    x = x.float()
+    x = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    half = x.shape[-1] // 2
+    angle = (positions.double()[:, None] * theta ** (-torch.arange(half, device=x.device, dtype=torch.float64) / half)).float()[:, None]
+    a, b = x[..., :half], x[..., half:]
+    return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
 
 
 def plain_attention(q, k, v, heads_per_kv):
@@ -55,48 +43,62 @@ def plain_attention(q, k, v, heads_per_kv):
     return torch.einsum("hij,jhd->ihd", torch.softmax(s, -1), v)
 
 
-def run(width: int = 512, heads: int = 8, kv_heads: int = 2, bits: int = 4, prompts=(200, 75, 33), steps: int = 8,
+def run(width: int = 512, heads: int = 8, kv_heads: int = 2, bits: int = 4, shared: int = 320, prompts=(200, 75, 33), steps: int = 8,
         group: int = 32, seed: int = 0) -> dict:
-    dev, dim = "cuda", width // heads
+    dev, dim, page = "cuda", width // heads, 32
     sizes = dict(q=heads * dim, k=kv_heads * dim, v=kv_heads * dim)
     X = inputs.calib_inputs(width, 4096, dtype=torch.bfloat16, seed=seed, device=dev, heavy_frac=0.02, heavy_mult=10.0)
     W = {n: inputs.layer_weights(r, width, dtype=torch.bfloat16, seed=seed + i, device=dev, std=width ** -0.5)
          for i, (n, r) in enumerate(dict(sizes, o=width).items())}
-    What = {n: quantized_projection(w, X, bits, 10) for n, w in W.items() if n != "o"}
-    fused = torch.cat([What["q"], What["k"], What["v"]])
+    parts = [quantized(W[n], X, bits, 10) for n in ("q", "k", "v")]
+    What = {"qkv": qe.QuantizedWeights(*(torch.cat([p[x] for p in parts]) for x in ("codes", "scales", "zeros")), bits)}
+    ones, rope = torch.ones(dim, dtype=torch.bfloat16, device=dev), qe.Rope(dim)
 
-    cache = qe.KVCache(64, 32, kv_heads, dim, group)
-    paged = PagedSequences(cache, len(prompts), max(prompts) + steps)
+    cache = qe.KVCache(64, page, kv_heads, dim, group)
+    pool = qe.PagePool(cache)
     g = torch.Generator(device=dev).manual_seed(seed)
-    kept = [[] for _ in prompts]                   # the hidden states so far, for the unquantized layer
     errors = {}
 
-    def layer(hidden: list, what: str):
-        """One call for the whole batch: `hidden` holds each sequence's new rows."""
-        rows = [h.shape[0] for h in hidden]
-        h = torch.cat(hidden)
-        qkv = (h @ fused.T).unflatten(-1, (heads + 2 * kv_heads, dim))     # sliced below, not copied
-        slots = torch.cat([paged.grow(b, n) for b, n in enumerate(rows)]).to(dev)
-        qe.qe_cache_append(cache, qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:], slots)
-        start = torch.tensor([0] + rows, device=dev).cumsum(0).to(torch.int32)
-        out = qe.qe_cache_attention(cache, qkv[:, :heads], start, paged.lengths(), paged.table.to(dev), max(rows), max(paged.length))
+    def layer(h, table, kv_len, new, max_q, max_kv, past, prefix_pages=None, prefix=0, what="prompt"):
+        """One call for the whole batch: h holds each sequence's new[b] rows, `past` what came before them."""
+        start, slots, positions = qe.qe_cache_grow(cache, pool, kv_len, new, table, h.shape[0], prefix=prefix)
+        qkv = qe.qe_linear(What["qkv"], h).unflatten(-1, (heads + 2 * kv_heads, dim))          # sliced below, not copied
+        q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+        qe.qe_norm_rotate(q, k, positions, rope, q_weight=ones, k_weight=ones, q_out=q, k_out=k)
+        qe.qe_cache_append(cache, k, v, slots)
+        if prefix:
+            out = qe.qe_cache_attention_shared(cache, q, start, kv_len, table, max_q, max_kv, prefix_pages, prefix)
+        else:
+            out = qe.qe_cache_attention(cache, q, start, kv_len, table, max_q, max_kv)
         y = out.flatten(1)
-        if what == "prompt":                       # the output projection sees what attention gives
-            What["o"] = quantized_projection(W["o"], y.T.contiguous(), bits, 10)
-        y = y @ What["o"].T
-        want = []
-        for b, n in enumerate(rows):
-            kept[b].append(hidden[b])
-            past = torch.cat(kept[b])
-            q, k, v = ((x @ W[m].T).unflatten(-1, (-1, dim)) for x, m in ((hidden[b], "q"), (past, "k"), (past, "v")))
-            want.append(plain_attention(q, k, v, heads // kv_heads).flatten(1) @ W["o"].float().T)
+        if "o" not in What:                        # the output projection is quantized for what attention gives
+            o = quantized(W["o"], y.T.contiguous(), bits, 10)
+            What["o"] = qe.QuantizedWeights(o["codes"], o["scales"], o["zeros"], bits)
+        y, want, at = qe.qe_linear(What["o"], y), [], 0
+        for b, n in enumerate(new.tolist()):
+            past[b] = torch.cat([past[b], h[at:at + n]])
+            at, j = at + n, torch.arange(past[b].shape[0], device=dev)
+            q, k, v = ((x @ W[m].T).unflatten(-1, (-1, dim)) for x, m in ((past[b][-n:], "q"), (past[b], "k"), (past[b], "v")))
+            want.append(plain_attention(normed_and_rotated(q, j[-n:]), normed_and_rotated(k, j), v, heads // kv_heads).flatten(1)
+                        @ W["o"].float().T)
         want = torch.cat(want)
         errors[what] = max(errors.get(what, 0.0), ((y.float() - want).norm() / want.norm()).item())
-        return y
 
-    layer([torch.randn(n, width, generator=g, device=dev).to(torch.bfloat16) for n in prompts], "prompt")
-    for _ in range(steps):
-        layer([torch.randn(1, width, generator=g, device=dev).to(torch.bfloat16) for _ in prompts], "step")
+    def rows(n):
+        return torch.randn(n, width, generator=g, device=dev).to(torch.bfloat16)
+
+    def integers(x):
+        return torch.tensor(x, dtype=torch.int32, device=dev)
+
+    past = [rows(0)]
+    first = torch.full((1, -(-shared // page)), -1, dtype=torch.int32, device=dev)
+    layer(rows(shared), first, integers([0]), integers([shared]), shared, shared, past)
+    past, longest = past * len(prompts), shared + max(prompts)
+    table = torch.full((len(prompts), -(-(longest + steps) // page)), -1, dtype=torch.int32, device=dev)
+    kv_len = integers([shared] * len(prompts))
+    layer(rows(sum(prompts)), table, kv_len, integers(prompts), max(prompts), longest, past, first[0], shared)
+    for i in range(steps):
+        layer(rows(len(prompts)), table, kv_len, integers([1] * len(prompts)), 1, longest + 1 + i, past, first[0], shared, "step")
     status = qe.qe_sync_status()
     assert status == qe.QE_OK, qe.qe_status_string(status)
     return errors
