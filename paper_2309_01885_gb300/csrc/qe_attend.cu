@@ -14,6 +14,7 @@ __global__ void __launch_bounds__(N) k_attend_join(const AttendArgs a, int unit,
     __shared__ int64_t sums[N + 1];
     __shared__ float4 meet_v[N];
     __shared__ float2 meet_s[N];
+    if (a.first_pass) let_next_begin();
     int64_t share;
     scan_units<N>(a, unit, sums, share);
     const int64_t total = sums[N], per = worker_units(a, total);
@@ -50,7 +51,7 @@ __global__ void __launch_bounds__(N) k_attend_join(const AttendArgs a, int unit,
             cut = begin < border && begin >= border - per;
         }
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");    // every block waits: the grid ends after the workers' grid
+    wait_for_last();                                      // every block waits: the grid ends after the workers' grid
     if (!cut) return;
     const int count = 1 + static_cast<int>((per > 0x7fffffff ? (end - 1) / per : div_small(end - 1, static_cast<int>(per))) - worker);
     const int D = a.g.D, R = a.rows_cap;

@@ -145,6 +145,10 @@ __device__ __forceinline__ void q_powers(float big, float &down, float &up) {
     up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
 }
 
+// The next kernel in the stream may begin, if it was launched so; and waiting for the last one's end and its writes.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Where the first pass keeps a row's head: sums, and the offsets of maxima and totals behind all of them.
 struct First {
     float *sums, *most, *total;

@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
     uint8_t *ring = smem + warp * F::WARP_BYTES;
     uint64_t *full = reinterpret_cast<uint64_t *>(smem + kWarps * F::WARP_BYTES) + warp * STAGES;
     int64_t *sums = reinterpret_cast<int64_t *>(smem + kWarps * F::WARP_BYTES + kWarps * STAGES * 8);
-    if constexpr (!WHOLE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!WHOLE || a.first_pass) let_next_begin();
     if (lane == 0) {
         for (int s = 0; s < STAGES; ++s) mbar_init(&full[s], 1);
         fence_mbar_init();
@@ -198,7 +198,10 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
         at.v = seq_view(a, at.seq, blockIdx.x == at.seq * of_seq && threadIdx.x == 0);
         at.w = seq_work(a, at.v, kRowsUnit);
         cta_begin = static_cast<int64_t>(blockIdx.x - at.seq * of_seq) * at.w.steps;
-        if (cta_begin >= at.w.units) return;
+        if (cta_begin >= at.w.units) {
+            wait_for_last();
+            return;
+        }
         cta_end = cta_begin + at.w.steps;
     } else {
         scan_units<kWarps * 32>(a, kRowsUnit, sums, share);
@@ -651,6 +654,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
                 }
             }
         }
+        wait_for_last();                                  // what the prefix's pass left is read, or its workers' slots written, from here on
         __syncthreads();
         const bool whole = WHOLE || take == at.w.steps;
         float *slot = a.part + (2 * static_cast<int64_t>(blockIdx.x) + (step0 == 0 ? 1 : 0)) * (F::ROWS * (D + 2));
@@ -689,6 +693,7 @@ __global__ void __launch_bounds__(kWarps * 32, WHOLE ? whole_blocks(C, GC, NT, k
             __syncthreads();
         }
     }
+    wait_for_last();                                      // (a block without work too: this grid ends after the last one's)
     if (stuck) {                                          // a wait gave up: leave no copy in flight behind
         for (unsigned s = 0; s < STAGES && s < turn; ++s) {
             const unsigned last = turn - 1 - (turn - 1 - s) % STAGES;
@@ -704,7 +709,21 @@ cudaError_t launch_rows_as(const AttendArgs &a, cudaStream_t s) {
     static std::atomic<uint64_t> raised{0};
     const cudaError_t e = raise_smem(reinterpret_cast<const void *>(k_attend_rows<C, GC, NT, W, WHOLE, HALF>), F::SMEM, raised);
     if (e != cudaSuccess) return e;
-    k_attend_rows<C, GC, NT, W, WHOLE, HALF><<<static_cast<unsigned>(WHOLE ? a.items : a.ctas), W * 32, F::SMEM, s>>>(a);
+    const unsigned blocks = static_cast<unsigned>(WHOLE ? a.items : a.ctas);
+    if (a.prefix > 0 && !a.first_pass) {                  // behind the prefix's pass: begins while that one's last blocks run
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(blocks);
+        cfg.blockDim = dim3(W * 32);
+        cfg.dynamicSmemBytes = F::SMEM;
+        cfg.stream = s;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, k_attend_rows<C, GC, NT, W, WHOLE, HALF>, a);
+    }
+    k_attend_rows<C, GC, NT, W, WHOLE, HALF><<<blocks, W * 32, F::SMEM, s>>>(a);
     return cudaGetLastError();
 }
 
