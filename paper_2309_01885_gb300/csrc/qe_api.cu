@@ -783,7 +783,7 @@ const char *qe_status_string(qe_status st) {
         case QE_ERR_INVALID_ARG: return "invalid argument";
         case QE_ERR_CUDA: return "CUDA error";
         case QE_ERR_OOM: return "workspace allocation failed or too small";
-        case QE_ERR_NUMERIC: return "non-finite value in W or Sigma";
+        case QE_ERR_NUMERIC: return "non-finite value in W, Sigma, keys, values or a layer's grids";
         case QE_ERR_TIMEOUT: return "a device-side wait gave up";
         case QE_ERR_UNSUPPORTED: return "option or layout not implemented";
         default: return "unknown status";

@@ -784,7 +784,9 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
     if first is None:
         raise ValueError("q or k is given")
     index = first.get_device()
-    if stream is not None or (index >= 0 and _current_device() != index):   # what is made here belongs to the stream
+    if index < 0:
+        raise ValueError("expected device tensors")
+    if stream is not None or _current_device() != index:   # what is made here belongs to the stream
         with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(index):
             return qe_norm_rotate(q, k, positions, rope, q_weight=q_weight, k_weight=k_weight, eps=eps, q_out=q_out, k_out=k_out)
     if first.dim() != 3:

@@ -131,7 +131,12 @@ def test_norm_rotate_refuses(lib):
     assert call(tokens=0, Q=None) == qe.QE_OK and call(q_heads=0, k_heads=0, Q=None) == qe.QE_OK
 
 
-def test_norm_rotate_python_refuses():
+def test_norm_rotate_python_refuses(monkeypatch):
+    x = torch.zeros(3, 4, 64)
+    with pytest.raises(ValueError):                      # not on a device
+        qe.qe_norm_rotate(x, x)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(qe, "_current_device", lambda: 0)
     x, pos, rope = torch.zeros(3, 4, 64), torch.zeros(3, dtype=torch.int32), qe.Rope(64)
     for bad in (dict(q=None, k=None), dict(q=x[0], k=None), dict(q=x, k=torch.zeros(2, 4, 64)), dict(q=x, k=x.half()),
                 dict(q=x, k=x.transpose(1, 2).contiguous().transpose(1, 2)), dict(q=x, k=None, positions=None),
