@@ -299,6 +299,13 @@ cudaError_t launch_plan(AttendArgs a, const AttendPlan &p, cudaStream_t s) {
                           : launch_attend_rows(a, p.tiles, s);
 }
 
+// A prefix that sequences share is read once for all of them.  Attention over it, all rows of the batch as one sequence's
+// without a mask, leaves unnormalised sums, maxima and totals in binary32; the pass over what is behind it joins them as it
+// finishes its rows:  m = max(m1, m2),  o = (2^(m1 - m) o1 + 2^(m2 - m) o2) / (2^(m1 - m) l1 + 2^(m2 - m) l2).  The second pass
+// does not need the first until it finishes: it is launched to begin while the first one's last blocks run.  Measured (us, 32
+// heads of 128 on 8, one row each): 64 sequences behind 8192 tokens with up to 1000 of their own 64, with up to 100 48 (81 and 67
+// one after the other); 200 behind 16000 with 500 .. 6000 304 (310).
+
 // The prefix's pass, all rows of the batch as one sequence's, and the one over what is behind it.
 qe_attention front_of(const qe_attention &at, int64_t prefix) {
     qe_attention f = at;

@@ -34,7 +34,10 @@
 // them and an E of theirs (seldom).  The running maximum is one of score + E, of what a token
 // adds, and raised only when one exceeds it by 8 (a factor of 2^8), so the accumulator in
 // tensor memory is rarely rescaled; P is taken 2^7 above it, keeps its bits down to 2^-21
-// of the greatest and vanishes 2^10 further down.  Sums are fp32.
+// of the greatest and vanishes 2^10 further down.  Sums are fp32.  CARRY (fp16 results behind a
+// shared prefix, which average many tokens): what P's rounding leaves out is a second operand that
+// is multiplied with V too.  6 sequences of 40 .. 100 rows behind 12000 tokens, 232 heads of 64: the
+// largest error against binary64 0.00023 instead of 0.00031, 767 us instead of 542.
 #include <cuda_fp16.h>
 #include <math_constants.h>
 

@@ -131,8 +131,10 @@ RowsPlan rows_plan(const LinearArgs &a) {
         const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * ceil_div(a.rows, 8 * nt);
         for (int ranks = 1; ranks <= 8; ++ranks) {
             // An SM's time goes by the units it turns: its CTAs', each with what a CTA costs besides; one CTA alone leaves
-            // pauses.  Measured (5 x 14848 x 59392, 4 bits, one or two row tiles a warp, us): 1: 2 ranks 139, 4 133, 8 115;
-            // 2: 2 ranks 172 (116 CTAs), 3 176, 5 110 (290), 7 115, 8 129.
+            // pauses.  Measured (us, 4 bits, one / two row tiles a warp): 5 x 14848 x 59392 1 rank 176 / 283, 2 125 / 152 (116
+            // CTAs), 4 121 / 118, 5 119 / 98 (290), 6 102 / 115, 7 107 / 102, 8 109 / 115; 1 x 4096 x 11008 39 / 66, 27 / 37,
+            // 18 / 25, 18 / 20, 16 / 20, 16 / 23, 16 / 20; 24 x 11008 x 4096 in groups of 128 (one row tile) 39, 27 with 2,
+            // 23 with 3 (258), 29 with 4 and more.
             const int64_t an_sm = ceil_div(groups * ranks, linear_sms());
             const int64_t cost = an_sm * (tiles * ceil_div(a.g.units, ranks) + 10) * (an_sm == 1 ? 4 : 3);
             if (least < 0 || cost < least) {
@@ -148,7 +150,9 @@ TilesPlan tiles_plan(const LinearArgs &a) {
     const int64_t outs = ceil_div(a.g.q, 128), sms = linear_sms();
     TilesPlan best{64, 64, 1};
     if (a.rows > 64) {
-        // a group's end stops a tile of 256, which has one accumulator
+        // As many rows a tile as the rounds over the SMs ask for; a tile costs its rows and some 32 more, which it takes to
+        // begin and to leave.  Measured (us, 4 bits, tiles of 128 / 160 / 192 / 224 / 256 rows): 4095 x 4096 x 11008 324 / 285 /
+        // 248 / 215 / 229, 2048 x 4096 x 4096 88 / 74 / 74 / 68 / 59, 4095 x 14848 x 4096 516 / 434 / 375 / 338 / 311.
         const int room = a.rows <= 128 ? 128 : a.g.bits == 8 ? 224 : 256;   // (8 bits' codes take shared memory from x)
         int64_t least = -1;
         for (int rows = room; rows >= room / 2; rows -= 32) {
@@ -160,6 +164,8 @@ TilesPlan tiles_plan(const LinearArgs &a) {
         }
     }
     const int64_t tiles = outs * ceil_div(a.rows, best.rows);
+    // A cluster shares a tile's columns out while one of twice its size finds SMs.  Measured (us, 1 / 2 / 4 / 8 CTAs): 64 x 4096 x
+    // 4096 (32 tiles) 25 / 18 / 14 / 27, 128 x 4096 x 4096 (64) 29 / 18 / 25 / 45, 300 x 4096 x 4096 (96) 33 / 33 / 37 / 68.
     while (best.ranks < 8 && tiles * best.ranks * 2 <= sms && a.g.units >= 8 * best.ranks) best.ranks *= 2;
     return best;
 }
@@ -184,7 +190,9 @@ cudaError_t launch_tiles(const LinearArgs &a, cudaStream_t s) {
     }
 }
 
-// Rows of x up to which the few-rows kernel takes a call.
+// Rows of x up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles): 4 bits, 4096 x 4096 24 rows 12 / 14,
+// 32 14 / 14, 64 16 / 14; 14848 x 59392 24 rows 156 / 231, 32 180 / 231, 64 346 / 231; 32 x 11008 x 4096 in groups of 128
+// 27 / 31; 8 bits, 32 x 4096 x 4096 18 / 16.
 constexpr int kFewRows = 32;
 
 }  // namespace
