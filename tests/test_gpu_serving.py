@@ -154,3 +154,37 @@ def test_a_captured_step_advances_as_an_eager_one():
         assert torch.equal(out, want[i])
     assert all(torch.equal(t, was) for t, was in zip(state, after))
     assert qe.qe_sync_status() == qe.QE_OK
+
+
+def test_two_streams_at_once():
+    """Two batches on two streams, their launches in turn with nothing in between to wait for, against one after the other."""
+    width = 264
+
+    def made():
+        blocks, rows = [], []
+        for seed in (21, 22):
+            g = products.gen(seed)
+            block = Block(torch.bfloat16, 4, 32, 4, width, seed=seed)
+            begun(block, g, width)
+            blocks.append(block)
+            rows.append([torch.randn(n, width, generator=g, device="cuda").to(torch.bfloat16) for n in (4, 4, 80, 4, 160, 4)])
+        return blocks, rows
+
+    def step(block, x):
+        n = x.shape[0] // 4
+        return block.step(x, block.table, block.kv_len, n_of[n], 32, n, 200)["out"]
+
+    n_of = {n: integers([n] * 4) for n in (1, 20, 40)}
+    blocks, rows = made()
+    want = [[step(block, x) for x in xs] for block, xs in zip(blocks, rows)]
+    torch.cuda.synchronize()
+    blocks, rows = made()
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for i in range(6):
+        for b in range(2):
+            with torch.cuda.stream(streams[b]):
+                got[b].append(step(blocks[b], rows[b][i]))
+    torch.cuda.synchronize()
+    assert qe.qe_sync_status() == qe.QE_OK
+    assert all(torch.equal(x, y) for b in range(2) for x, y in zip(got[b], want[b]))

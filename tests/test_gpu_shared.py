@@ -172,3 +172,12 @@ def test_two_captured_graphs_and_a_stream():
     got = b.attend(stream=s)
     s.synchronize()
     assert got.equal(want)
+
+
+@pytest.mark.parametrize("max_kv", [0, 1, 50, 3000, 1 << 20])
+@pytest.mark.parametrize("shape", [[(1, 101), (1, 300), (1, 0), (1, 150)], [(40, 150), (33, 400)]])
+def test_the_longest_sequence_only_plans_the_work(shape, max_kv):
+    """max_kv below the prefix, below what is there, or far above it."""
+    b = Batch(shape, 100, seed=31)
+    b.max_kv = max_kv
+    b.check()
