@@ -1,8 +1,9 @@
 """Products with a quantized layer against binary64.
 
 Codes less zeros and x are held exactly, so a sum's error is that of adding.  With S = sum_j |s (c - z) x_j|: a chain of
-accumulations on the matrix units is up to p / 128 + 40 long (eight warps or more share the columns, sixteen columns are
-added at once; the rest for the joining), each off by a unit of binary32, 2^-23 of what is there, at most S.  Activations
+accumulations on the matrix units is up to p / 16 long (sixteen columns are added at once; some 40 more for the joining), each
+off by a unit of binary32, 2^-23 of what is there.  That is at most S where all terms have one sign.  Where they have either, as in
+most of these tests, it is a random walk's end, below S / 8 from some 100 columns on: (p / 128 + 40) 2^-23 S.  Activations
 are steeper than 1 by at most 13%, and their functions are off by a few units: 2^-20 of the result and of S's error.
 Then half a unit of the result's type."""
 import math
@@ -48,10 +49,10 @@ def weights64(codes, scales, zeros, group):
     return s * (codes.double() - z)
 
 
-def plain(w, x, bias, act, residual):
+def plain(w, x, bias, act, residual, chain=128):
     """(y, allowed error), binary64."""
     y, size = x.double() @ w.T, x.double().abs() @ w.abs().T
-    tol = size * ((x.shape[1] / 128 + 40) * 2.0 ** -23)
+    tol = size * ((x.shape[1] / chain + 40) * 2.0 ** -23)
     if bias is not None:
         y = y + bias.double()
         tol = tol + y.abs() * 2.0 ** -23
@@ -70,8 +71,8 @@ def plain(w, x, bias, act, residual):
     return y, tol + 1.01 * HALF_ULP[x.dtype] * y.abs() + SMALLEST[x.dtype]
 
 
-def check(got, w, x, bias=None, act="none", residual=None):
-    want, tol = plain(w, x, bias, act, residual)
+def check(got, w, x, bias=None, act="none", residual=None, chain=128):
+    want, tol = plain(w, x, bias, act, residual, chain)
     assert got.dtype == x.dtype and got.shape == want.shape
     over = want.abs() + tol > torch.finfo(x.dtype).max    # of these infinity is an answer too
     err = torch.where(over & (got.double() == want.sign() * math.inf), 0.0, (got.double() - want).abs())
@@ -280,3 +281,25 @@ def test_no_rows():
     codes, scales, zeros = layer(64, 128, 4, 0, 5)
     w = qe.QuantizedWeights(codes, scales, zeros, 4)
     assert qe.qe_linear(w, torch.empty(0, 128, dtype=torch.bfloat16, device="cuda")).shape == (0, 64)
+
+
+@pytest.mark.parametrize("rows,q,p,group", [(70000, 40, 128, 0), (3, 200000, 64, 0), (300, 150000, 64, 0), (2, 16, 1 << 20, 0), (50, 33, 1 << 18, 0),
+                                            (2, 16, 1 << 18, 64), (100, 130, 1 << 16, 128)])
+@pytest.mark.parametrize("bits", [3, 4])
+def test_long_axes(rows, q, p, group, bits):
+    codes, scales, zeros = layer(q, p, bits, group, bits)
+    x = torch.randn(rows, p, generator=gen(6), device="cuda").to(torch.bfloat16)
+    got = qe.qe_linear(qe.QuantizedWeights(codes, scales, zeros, bits, group_size=group), x)
+    w = weights64(codes, scales, zeros, group)
+    for i in range(0, rows, 10000):
+        check(got[i:i + 10000], w, x[i:i + 10000])
+    assert qe.qe_sync_status() == qe.QE_OK
+
+
+@pytest.mark.parametrize("rows", [1, 20, 64, 300])
+@pytest.mark.parametrize("p,group", [(1000, 0), (40000, 0), (40000, 128)])
+def test_terms_of_one_sign(rows, p, group):
+    codes, scales, zeros = layer(48, p, 4, group, p)
+    zeros.zero_()
+    x = torch.rand(rows, p, generator=gen(7), device="cuda").to(torch.float16)
+    check(qe.qe_linear(qe.QuantizedWeights(codes, scales, zeros, 4, group_size=group), x), weights64(codes, scales, zeros, group), x, chain=16)
