@@ -272,8 +272,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
             const int tok = e / F::ROWS, row = e % F::ROWS;
             const int64_t i = static_cast<int64_t>(tile0) * kTileRows + row;
             if (i >= a.g.q) continue;
-            float v = 0.0f;
-            for (int k = 0; k < ranks; ++k) v += (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row];
+            float v = 0.0f, of[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) of[k] = k < ranks ? (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v += of[k];       // in order
             finish<act.value>(a, v, m0 + tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
         }
     });
