@@ -623,7 +623,7 @@ typedef struct {
     qe_dtype dtype;              /* of X, residual and Y: bf16 or fp16 (fp32 is QE_ERR_UNSUPPORTED) */
     qe_dtype bias_dtype;
     const void *X;               /* device, rows x p, leading dimension ldx >= p; where it and ldx are multiples of 16
-                                  * bytes the loads are wide */
+                                  * bytes the loads are wide (many rows are copied to the workspace otherwise) */
     int64_t ldx;
     const void *bias;            /* device, q values, or NULL */
     qe_activation act;

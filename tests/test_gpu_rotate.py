@@ -153,3 +153,20 @@ def test_nothing_to_do():
     q, k = qe.qe_norm_rotate(torch.empty(0, 4, 64, device="cuda"), torch.empty(0, 2, 64, device="cuda"),
                              torch.empty(0, dtype=torch.int32, device="cuda"), qe.Rope(64))
     assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("tokens", [608, 1215, 1216, 1300, 1900, 2440, 3100, 3700, 4300, 4863, 4864, 4870])
+def test_tokens_a_block(tokens):
+    """Every number of tokens that a block may take, with a last block that lacks some, and tokens that are left as they were."""
+    g = gen(tokens)
+    q, k = (torch.randn(tokens, n, 64, generator=g, device="cuda").to(torch.bfloat16) for n in (3, 1))
+    pos = torch.randint(-3, 1 << 16, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    pos[-2:] = torch.tensor([-1, 5], dtype=torch.int32)
+    w = (1 + torch.randn(64, generator=g, device="cuda")).to(torch.bfloat16)
+    freq = [10000.0 ** (-2.0 * i / 64) for i in range(32)]
+    out = [torch.full_like(x, 7.0) for x in (q, k)]
+    qe.qe_norm_rotate(q, k, pos, qe.Rope(64), q_weight=w, k_weight=w, q_out=out[0], k_out=out[1])
+    on = pos >= 0
+    for x, y in zip((q, k), out):
+        assert (y[~on] == 7.0).all()
+        check(y[on], x[on], pos[on], freq, False, w, 1e-6)
