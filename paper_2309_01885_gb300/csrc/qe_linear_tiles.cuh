@@ -464,9 +464,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 if (lane == 0) mbar_arrive(&acc_empty[part + buf.s]);
                 u = min((u / seg + 1) * seg, end);
             }
+            if constexpr (SHARED) {
+                // x's ring is free for the sums, [row of x][output], once every product of the tile has been taken: either side
+                // has waited for its own part's, so they meet (and where a wait gave up too, lest the other side wait for ever)
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
             if (!ok) break;
             if constexpr (SHARED) {
-                // every product has been taken: x's ring is free for the sums, [row of x][output]
                 float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
                 for (int i = 0; i < F::HALF; ++i)
