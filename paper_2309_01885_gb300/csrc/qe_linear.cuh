@@ -31,6 +31,12 @@ namespace qe {
 
 constexpr int kUnitCols = 64, kTileRows = 16;
 
+// Units that the matrix units' accumulators add up before their sums go to registers (or shared memory): 8192 columns (up to
+// twice as many where a CTA of the few-rows kernel has no more).  They lose up to a unit in the last place with each addition,
+// of 16 columns, always towards zero: 512 of them make 2^-14 of a sum of one sign at most (measured: a tenth of that), which 16
+// bits do not show; those of 2^20 columns, shared by eight CTAs, 2^-10, more than fp16's rounding.
+constexpr int kSegmentUnits = 128;
+
 struct LinearGeom {
     const uint8_t *codes;
     const float *scales;

@@ -6,8 +6,11 @@
 // streams straight into registers, two to four units of 64 columns ahead, turns each pair of codes
 // with two or three instructions into 16-bit floats c - z (exact) and multiplies them with up
 // to 8 NT rows of x on m16n8k16, the outputs in the 16-high side.  Products are exact and sums
-// binary32; the scale comes in at the end, or at the end of every group.  The eight warps of a CTA share
-// x, which passes through shared memory 256 columns at a time (swizzled by 16 bytes, read by
+// binary32; the scale comes in at the end, or at the end of every group.  Accumulators are emptied
+// every kSegmentUnits units: those of long groups into registers; with one grid a row, where a CTA has
+// more than twice as many units (LONG), into shared memory, a place of the thread's own for each.
+// (Where it has fewer too, the first size below took 100 us instead of 97.)  The eight warps of a CTA
+// share x, which passes through shared memory 256 columns at a time (swizzled by 16 bytes, read by
 // ldmatrix).  The CTAs of a cluster share a layer's columns out among them: their sums meet in
 // shared memory, in order, so that results do not depend on who is first.
 //
@@ -25,6 +28,7 @@ namespace qe {
 namespace {
 
 constexpr int kRowWarps = 8, kChunk = 4;   // kChunk: units of x in a stage
+constexpr int kSegmentChunks = kSegmentUnits / kChunk;
 
 template <bool HALF>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -63,6 +67,7 @@ struct RowsOf {
     static constexpr int UNIT_BYTES = TOKENS * 128, STAGE = kChunk * UNIT_BYTES, STAGES = 3;
     static constexpr int SUMS = TOKENS * LD * 4;
     static constexpr int SMEM = STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS;
+    static constexpr int KEPT = RT * NT * 4 * kRowWarps * 32 * 4;           // sums of earlier segments
     static constexpr int PIECES = TOKENS * 8 * kChunk / (kRowWarps * 32);   // 16-byte pieces of a stage a thread brings
 };
 
@@ -74,7 +79,7 @@ __device__ __forceinline__ void cp_async16_part(uint32_t dst, const void *src, i
 // CTAs that an SM holds, by registers.
 __host__ __device__ constexpr int rows_ctas(int NT) { return NT == 1 ? 3 : 2; }
 
-template <int B, int RT, int NT, bool HALF, bool GROUPED>
+template <int B, int RT, int NT, bool HALF, bool GROUPED, bool LONG>
 __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(const LinearArgs a) {
     using F = RowsOf<RT, NT>;
     using TU = Turn<B, HALF>;
@@ -196,10 +201,23 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
         }
     };
     if constexpr (!GROUPED) turn_grids();
+    float *kept = reinterpret_cast<float *>(smem + F::SMEM) + threadIdx.x;   // one grid a row: sums of the segments before
+    auto keep = [&](bool first) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float *place = kept + ((i * NT + n) * 4 + e) * (kRowWarps * 32);
+                    *place = first ? sum[i][n][e] : *place + sum[i][n][e];
+                    sum[i][n][e] = 0.0f;
+                }
+    };
     // matrix j of an ldmatrix: rows' piece 4 c + j; lane 8 j + i addresses row i
     const int mrow = lane & 7, mpiece = lane >> 3;
     const uint32_t mat0 = ring + mrow * 128 + ((mpiece ^ mrow) << 4), mat1 = ring + mrow * 128 + (((4 + mpiece) ^ mrow) << 4);
-    for (int c = 0; c < chunks; ++c) {
+    auto chunk = [&](int c) {
         asm volatile("cp.async.wait_group %0;" ::"n"(F::STAGES - 2) : "memory");
         __syncthreads();                                  // the chunk is there, and everyone has done with the one before
         bring(c + F::STAGES - 1);
@@ -245,9 +263,15 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
             });
 #pragma unroll
         for (int i = 0; i < RT; ++i) code[i] += kChunk * 128 * B;
-    }
-    if constexpr (GROUPED) {
-        if (begin < end) fold();
+    };
+    if constexpr (GROUPED || LONG) {
+        for (int c = 0; c < chunks;) {
+            for (const int stop = min(chunks, c + kSegmentChunks); c < stop; ++c) chunk(c);
+            if constexpr (LONG) keep(c <= kSegmentChunks);
+            else if (a.g.group_units > kSegmentUnits || c == chunks) fold();
+        }
+    } else {
+        for (int c = 0; c < chunks; ++c) chunk(c);
     }
 
     // ---- the cluster's sums meet ----
@@ -260,7 +284,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float v = GROUPED ? total[GROUPED ? i : 0][GROUPED ? n : 0][e] : begin < end ? sum[i][n][e] * scale[i][e >> 1] : 0.0f;
+                const float all = LONG ? kept[((i * NT + n) * 4 + e) * (kRowWarps * 32)] : sum[i][n][e];
+                const float v = GROUPED ? total[GROUPED ? i : 0][GROUPED ? n : 0][e] : begin < end ? all * scale[i][e >> 1] : 0.0f;
                 met[(8 * n + 2 * t + (e & 1)) * F::LD + kTileRows * (warp * RT + i) + r + 8 * (e >> 1)] = v;
             }
     if (ranks > 1) cluster.sync();
@@ -283,20 +308,21 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
     if (ranks > 1) cluster.sync();                        // nobody leaves while its sums are read
 }
 
-template <int B, int RT, int NT, bool HALF, bool GROUPED>
+template <int B, int RT, int NT, bool HALF, bool GROUPED, bool LONG = false>
 cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
     using F = RowsOf<RT, NT>;
     const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps), blocks = ceil_div(a.rows, F::TOKENS);
+    constexpr int smem = F::SMEM + (LONG ? F::KEPT : 0);
     static std::atomic<uint64_t> raised{0};
-    const void *kernel = reinterpret_cast<const void *>(k_linear_rows<B, RT, NT, HALF, GROUPED>);
-    if (F::SMEM > 48 * 1024) {
-        const cudaError_t e = raise_limit(kernel, F::SMEM, raised);
+    const void *kernel = reinterpret_cast<const void *>(k_linear_rows<B, RT, NT, HALF, GROUPED, LONG>);
+    if (smem > 48 * 1024) {
+        const cudaError_t e = raise_limit(kernel, smem, raised);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks), static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(kRowWarps * 32);
-    cfg.dynamicSmemBytes = F::SMEM;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -304,12 +330,14 @@ cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_linear_rows<B, RT, NT, HALF, GROUPED>, a);
+    return cudaLaunchKernelEx(&cfg, k_linear_rows<B, RT, NT, HALF, GROUPED, LONG>, a);
 }
 
 template <int B, int RT, int NT>
 cudaError_t launch_rows_type(const LinearArgs &a, int ranks, cudaStream_t s) {
     if (a.g.groups > 1) return a.half ? launch_rows_as<B, RT, NT, true, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, true>(a, ranks, s);
+    if (ceil_div(a.g.units, ranks) > 2 * kSegmentUnits)
+        return a.half ? launch_rows_as<B, RT, NT, true, false, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false, true>(a, ranks, s);
     return a.half ? launch_rows_as<B, RT, NT, true, false>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false>(a, ranks, s);
 }
 

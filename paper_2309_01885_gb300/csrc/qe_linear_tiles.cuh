@@ -37,7 +37,6 @@ namespace qe {
 namespace {
 
 constexpr int kTileOut = 128;
-constexpr int kSegmentUnits = 128;         // 8192 columns
 constexpr int kTileThreads = 640;
 constexpr int kTurnWarp = 4, kFoldWarp = 12;
 

@@ -30,3 +30,39 @@ def test_halves_of_a_shared_tile(rows, q, p, group, bits):
     for _ in range(30):
         assert qe.qe_linear(w, x).equal(first)
     assert qe.qe_sync_status() == qe.QE_OK
+
+
+# ---- sums of one sign ----
+
+# Products are exact.  The matrix units add sixteen columns at a time, each addition off by a unit of binary32 at most, 2^-23 of
+# what is there, and hand their sums on every 8192 columns (where a CTA of the few-rows form has up to 16384, at their end), or
+# every group: 512 (1024) units of S = sum_j |s (c - z) x_j| at most, or group / 16.  These sums are added up in binary32, half a
+# unit each, a CTA's share and then eight CTAs'; scales and the bias come in with half a unit each: 40 for all but the first.  The
+# bias takes the sum away again, so that the result's own rounding counts for nothing.
+def one_sign_units(p, group, rows):
+    chain = min(p, 16384 if not group and rows <= 32 and p <= 8 * 16384 else 8192, group or p)
+    return chain / 16 + p / chain / 2 + 40
+
+
+def check_one_sign(rows, q, p, group, bits, dtype):
+    codes, scales, zeros = layer(q, p, bits, group, p + rows)
+    zeros.zero_()
+    x = torch.rand(1, p, generator=gen(rows), device="cuda").to(dtype)
+    w64 = weights64(codes, scales, zeros, group)
+    sums = (w64 @ x[0].double())
+    del w64
+    bias = -sums.float()
+    w = qe.QuantizedWeights(codes, scales, zeros, bits, group_size=group)
+    got = qe.qe_linear(w, x.expand(rows, p).contiguous(), bias=bias).double()
+    off = (got - (sums + bias.double())).abs() * 2.0 ** 23 / sums
+    most = one_sign_units(p, group, rows) * (1.0 + 2.0 ** -8) + (2.0 ** -25 * 2.0 ** 23 / sums.min().item())
+    assert off.max().item() <= most, f"{off.max().item():.0f} units of the sum off, of {most:.0f} allowed"
+    assert qe.qe_sync_status() == qe.QE_OK
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [1, 12, 20, 32])
+@pytest.mark.parametrize("p,group,bits", [(8192, 0, 4), (1 << 17, 0, 4), (1 << 18, 0, 4), (1 << 20, 0, 4), (1 << 20, 0, 3), (1 << 20, 0, 8), ((3 << 18) + 200, 0, 4), (1 << 22, 0, 4),
+                                          (1 << 20, 1 << 13, 4), (1 << 20, 1 << 17, 4), (1 << 20, 1 << 19, 3), (600000, 65600, 4)])
+def test_sums_of_one_sign_few_rows(p, group, bits, rows, dtype):
+    check_one_sign(rows, 40, p, group, bits, dtype)
