@@ -14,10 +14,8 @@
 //                  (exact).  Four warps take the even pairs of steps and four the odd ones, the
 //                  two row tiles of 16 outputs that stand in a warp's 32 lanes of tensor memory;
 //   warps 12-19    fold accumulators into registers, times the scale: at the end of each
-//                  group, or every kSegment columns with one grid a row (the tensor cores'
-//                  accumulators lose up to a unit in the last place with each addition, a
-//                  short chain's worth of which binary32 does not show).  Two accumulators take
-//                  turns where there is room for two.
+//                  group, and every kSegmentUnits units of a longer one, or of a row with one
+//                  grid.  Two accumulators take turns where there is room for two.
 // A CTA takes tile after tile, the next one's products running while the last one leaves.
 // Where there are few tiles the CTAs of a cluster share a tile's columns; their sums meet in
 // shared memory in order.
@@ -211,7 +209,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
     const int begin = static_cast<int>(static_cast<int64_t>(a.g.units) * rank / ranks),
               end = static_cast<int>(static_cast<int64_t>(a.g.units) * (rank + 1) / ranks);
     const int steps = end - begin, stages = (steps + 1) / 2;    // of a tile: units, and pairs of them (the last may lack one)
-    const int seg = a.g.groups > 1 ? a.g.group_units : kSegmentUnits;
+    // A segment is what a group, or kSegmentUnits of it, has left (one grid a row: the row is the group).
+    const int first_group_end = (begin / a.g.group_units + 1) * a.g.group_units;
+    auto segment_end = [&](int u, int group_end) { return min(min(u + kSegmentUnits, group_end), end); };
     // groups with one accumulator: a tile's two halves of rows take turns, one's products running while the other is folded
     const int parts = F::BUFS == 1 && a.g.groups > 1 ? 2 : 1;
 
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
         Turnstile<F::BUFS> acc[2];                        // of either part
         bool ok = true;
         for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
-            int seg_end[2] = {begin, begin};
+            int seg_end[2] = {begin, begin}, group_end[2] = {first_group_end, first_group_end};
             for (int u = begin; ok && u < end; u += 2) {
                 ok = wait_warp_on(&x_full[xs.s], xs.phase, abort_flag) && wait_warp_on(&a_full[as.s], as.phase, abort_flag);
                 if (!ok) break;
@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                         if (u + k == seg_end[part]) {     // a segment begins: its accumulator has been folded
                             ok = ok && wait_warp_on(&acc_empty[part + acc[part].s], acc[part].phase ^ 1u, abort_flag);
                             tc_fence_after();
-                            seg_end[part] = min(((u + k) / seg + 1) * seg, end);
+                            if (u + k == group_end[part]) group_end[part] += a.g.group_units;
+                            seg_end[part] = segment_end(u + k, group_end[part]);
                             add = 0u;
                         }
                         if (!ok) break;
@@ -445,9 +446,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
             const float *scales = a.g.scales + row_tile * a.g.groups * kTileRows + row % kTileRows;
             int g = a.g.groups > 1 ? begin / a.g.group_units : 0;
             float ahead = scales[g * kTileRows];          // of the next segment
-            for (int u = begin; u < end; buf.next()) {
+            for (int u = begin, group_end = first_group_end; u < end; buf.next()) {
                 const float scale = ahead;
-                if (g + 1 < a.g.groups) ahead = scales[++g * kTileRows];
+                u = segment_end(u, group_end);
+                if (u == group_end) {
+                    group_end += a.g.group_units;
+                    if (g + 1 < a.g.groups) ahead = scales[++g * kTileRows];
+                }
                 ok = wait_warp_on(&acc_full[part + buf.s], buf.phase, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
@@ -461,7 +466,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_linear_tiles(const LinearAr
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&acc_empty[part + buf.s]);
-                u = min((u / seg + 1) * seg, end);
             }
             if constexpr (SHARED) {
                 // x's ring is free for the sums, [row of x][output], once every product of the tile has been taken: either side

@@ -66,3 +66,11 @@ def check_one_sign(rows, q, p, group, bits, dtype):
                                           (1 << 20, 1 << 13, 4), (1 << 20, 1 << 17, 4), (1 << 20, 1 << 19, 3), (600000, 65600, 4)])
 def test_sums_of_one_sign_few_rows(p, group, bits, rows, dtype):
     check_one_sign(rows, 40, p, group, bits, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [33, 64, 120, 300])
+@pytest.mark.parametrize("p,group,bits", [(8192, 0, 4), (1 << 18, 0, 4), (1 << 20, 0, 8), (1 << 20, 1 << 13, 4), (1 << 20, 1 << 17, 4), (1 << 20, 1 << 19, 3), (600000, 65600, 4),
+                                          (600000, 10048, 8)])
+def test_sums_of_one_sign_many_rows(p, group, bits, rows, dtype):
+    check_one_sign(rows, 40, p, group, bits, dtype)
