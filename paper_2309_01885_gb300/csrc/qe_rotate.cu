@@ -379,11 +379,11 @@ bool aligned16(const void *p, int64_t a, int64_t b, size_t size) {
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && a % n == 0 && b % n == 0;
 }
 
-// t modulo 1, times 2^64.
+// t modulo 1, times 2^64, to the nearest.  A magnitude's fraction is exact, which 1 less a small one's would not be.
 uint64_t fraction(double t) {
-    t = ldexp(t - floor(t), 32);                          // 0 .. 2^32 (the end: by rounding, no turn at all)
-    const double upper = floor(t);
-    return (static_cast<uint64_t>(upper) << 32) + static_cast<uint64_t>(ldexp(t - upper, 32));
+    const double m = fabs(t), part = ldexp(m - floor(m), 32), upper = floor(part);
+    const uint64_t turns = (static_cast<uint64_t>(upper) << 32) + static_cast<uint64_t>(rint(ldexp(part - upper, 32)));
+    return t < 0.0 ? 0 - turns : turns;
 }
 
 }  // namespace
