@@ -777,8 +777,8 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
                    q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
                    q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None) -> tuple:
     """(q, k), tokens x heads x head_dim with any token and head strides, each head normed (x w / sqrt(mean x^2 + eps), where
-    a weight is given) and rotated by its token's position (int32; where a Rope is given; a negative one leaves the token's
-    results as they were).  Written into q_out and k_out where given (q and k themselves are allowed).  Either of q and k
+    a weight is given) and rotated by its token's position (int32; where a Rope is given).  A token with a negative position is
+    passed over, with a Rope or without: its results stay as they were.  Written into q_out and k_out where given (q and k themselves are allowed).  Either of q and k
     may be None."""
     first = q if q is not None else k
     if first is None:
@@ -794,11 +794,11 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
     n, _, dim = first.shape
     dtype = first.dtype
     code, weight_code, at, turns = _cache_dtype(dtype), 0, 0, 0
-    if rope is not None:
+    if rope is not None or positions is not None:
         if positions is None or positions.dtype is not torch.int32 or positions.dim() != 1 or positions.shape[0] != n or \
                 not positions.is_contiguous() or positions.get_device() != index:
             raise ValueError("positions: expected a contiguous int32 tensor of tokens entries on q's device")
-        at, turns = positions.data_ptr(), rope._ref
+        at, turns = positions.data_ptr(), 0 if rope is None else rope._ref
     weight = q_weight if q_weight is not None else k_weight
     if weight is not None:
         weight_code = _cache_dtype(weight.dtype)
