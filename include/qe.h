@@ -565,7 +565,8 @@ typedef struct {
     int64_t qo_token, qo_head, ko_token, ko_head;
     const void *q_weight, *k_weight;   /* device, head_dim each; NULL: not normed */
     float eps;                   /* >= 0 */
-    const int32_t *positions;    /* device, tokens; a negative one leaves the token's results as they were */
+    int clear;                   /* bit 0 (1): Q's (K's) results of tokens with a negative position are set to zero */
+    const int32_t *positions;    /* device, tokens; a negative one leaves the token's results as they were, or cleared */
     const qe_rope *rope;         /* host, 2 * pairs <= head_dim; NULL: not rotated (positions may then be NULL) */
 } qe_heads;
 

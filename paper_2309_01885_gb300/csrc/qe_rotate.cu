@@ -38,6 +38,7 @@ struct RotateArgs {
     int dim, block_tokens, weight_dtype;
     float eps, per_dim;
     const int32_t *positions;
+    int clear[2];             // whether tokens that are passed over get zeros
     int pairs, interleaved, facing;   // facing: pairs half a head apart face each other lane by lane
     uint64_t turns[kMostPairs];
 };
@@ -236,6 +237,13 @@ __global__ void __launch_bounds__(256, FORM == kAny ? 3 : 4) k_norm_rotate(const
     }
     unsigned live = 0u;                                   // tokens whose position is not negative
     for (int t = 0; t < toks; ++t) live |= static_cast<unsigned>(!a.positions || a.positions[tok0 + t] >= 0) << t;
+    if (a.clear[part] && live != (1u << toks) - 1u) {     // (beside the loop: in it, 109 us for the first size's 105)
+        Walk at = to;
+        for (int it = first; it < items; it += step, at.next(sets))
+            if (mine && !(live >> at.t & 1u))
+                for (int j = 0; j < kHeads<T> && kHeads<T> * at.h + j < heads; ++j)
+                    store_eight<T, SPLIT>(out + at.at + j * a.o_head[part], (a.vec & 2) != 0, upper_at, Eight<T>{});
+    }
     Two w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -353,6 +361,7 @@ cudaError_t launch_lanes(const RotateArgs &a, cudaStream_t s) {
     RotateArgs b = a;
     if (first == 1) {
         b.x[0] = a.x[1]; b.out[0] = a.out[1]; b.weight[0] = a.weight[1]; b.heads[0] = a.heads[1];
+        b.clear[0] = a.clear[1];
         b.x_token[0] = a.x_token[1]; b.x_head[0] = a.x_head[1]; b.o_token[0] = a.o_token[1]; b.o_head[0] = a.o_head[1];
         b.heads[1] = 0;
     }
@@ -416,7 +425,7 @@ qe_status qe_norm_rotate(const qe_heads *h, qe_stream_t stream) {
     if (h->head_dim < 8) return QE_ERR_INVALID_ARG;
     if (h->head_dim > 256 || h->head_dim % 8 != 0) return QE_ERR_UNSUPPORTED;
     if ((h->dtype != QE_F32 && h->dtype != QE_BF16 && h->dtype != QE_F16) ||
-        (h->weight_dtype != QE_F32 && h->weight_dtype != QE_BF16 && h->weight_dtype != QE_F16) || !(h->eps >= 0.0f) || isinf(h->eps))
+        (h->weight_dtype != QE_F32 && h->weight_dtype != QE_BF16 && h->weight_dtype != QE_F16) || !(h->eps >= 0.0f) || isinf(h->eps) || (h->clear & ~3) != 0)
         return QE_ERR_INVALID_ARG;
     if (h->rope && (h->rope->pairs < 1 || h->rope->pairs > kMostPairs || 2 * h->rope->pairs > h->head_dim)) return QE_ERR_INVALID_ARG;
     if (h->tokens == 0 || (h->q_heads == 0 && h->k_heads == 0)) return QE_OK;
@@ -427,6 +436,7 @@ qe_status qe_norm_rotate(const qe_heads *h, qe_stream_t stream) {
     a.x_token[0] = h->q_token; a.x_token[1] = h->k_token; a.x_head[0] = h->q_head; a.x_head[1] = h->k_head;
     a.o_token[0] = h->qo_token; a.o_token[1] = h->ko_token; a.o_head[0] = h->qo_head; a.o_head[1] = h->ko_head;
     a.heads[0] = h->q_heads; a.heads[1] = h->k_heads;
+    a.clear[0] = h->clear & 1; a.clear[1] = h->clear >> 1 & 1;
     a.vec = 3;
     for (int i = 0; i < 2; ++i) {
         if (a.heads[i] == 0) continue;

@@ -89,7 +89,8 @@ class QEHeads(ctypes.Structure):
                 ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64), ("k_token", ctypes.c_int64), ("k_head", ctypes.c_int64),
                 ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("qo_token", ctypes.c_int64), ("qo_head", ctypes.c_int64),
                 ("ko_token", ctypes.c_int64), ("ko_head", ctypes.c_int64), ("q_weight", ctypes.c_void_p),
-                ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p)]
+                ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("clear", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p)]
 
 
 class QELayer(ctypes.Structure):
@@ -691,7 +692,7 @@ class PagePool:
 # the structs of the calls that a serving step makes most often, as the library reads them (packed, they are made in a
 # third of the time that a ctypes structure takes)
 _GROWTH = struct.Struct("@4q11P")
-_HEADS = struct.Struct("@q5i4x2P4q2P4q2Pf4x2P")
+_HEADS = struct.Struct("@q5i4x2P4q2P4q2Pfi2P")
 _PRODUCT = struct.Struct("@q2iPqPi4xPqPq")
 
 
@@ -778,8 +779,8 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
                    q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None) -> tuple:
     """(q, k), tokens x heads x head_dim with any token and head strides, each head normed (x w / sqrt(mean x^2 + eps), where
     a weight is given) and rotated by its token's position (int32; where a Rope is given).  A token with a negative position is
-    passed over, with a Rope or without: its results stay as they were.  Written into q_out and k_out where given (q and k themselves are allowed).  Either of q and k
-    may be None."""
+    passed over, with a Rope or without: its results stay as they were in q_out and k_out, and are zeros where these are not given.
+    Either of q and k may be None; q and k themselves may be q_out and k_out."""
     first = q if q is not None else k
     if first is None:
         raise ValueError("q or k is given")
@@ -799,6 +800,7 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
                 not positions.is_contiguous() or positions.get_device() != index:
             raise ValueError("positions: expected a contiguous int32 tensor of tokens entries on q's device")
         at, turns = positions.data_ptr(), 0 if rope is None else rope._ref
+    clear = 0 if positions is None else int(q_out is None) + 2 * int(k_out is None)
     weight = q_weight if q_weight is not None else k_weight
     if weight is not None:
         weight_code = _cache_dtype(weight.dtype)
@@ -808,7 +810,7 @@ def qe_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: to
         _rotate_part("k", k, k_out, k_weight, n, dim, dtype, index, weight)
     st = (_lib or load()).qe_norm_rotate(
         _HEADS.pack(n, q_heads, k_heads, dim, code, weight_code, q_at, k_at, q_token, q_head, k_token, k_head, q_to, k_to, qo_token, qo_head,
-                    ko_token, ko_head, q_w, k_w, eps, at, turns), _raw_stream(index))
+                    ko_token, ko_head, q_w, k_w, eps, clear, at, turns), _raw_stream(index))
     if st != QE_OK:
         raise QEError(st, "qe_norm_rotate")
     return q_out, k_out
