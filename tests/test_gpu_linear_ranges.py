@@ -74,3 +74,58 @@ def test_sums_of_one_sign_few_rows(p, group, bits, rows, dtype):
                                           (600000, 10048, 8)])
 def test_sums_of_one_sign_many_rows(p, group, bits, rows, dtype):
     check_one_sign(rows, 40, p, group, bits, dtype)
+
+
+# ---- long axes with exact sums: a column, a unit, a stage or a CTA's share that is missing or counted twice shows ----
+
+def borders(p):
+    """Columns on either side of units (64), stages (256 and 128), segments (8192) and CTAs' shares of two to eight."""
+    units, at = -(-p // 64), {0, 1, p - 2, p - 1, p // 2}
+    for step in (64, 128, 256, 8192, 16384):
+        at |= {step - 1, step, p // step * step - 1, p // step * step, p // (2 * step) * step}
+    for ranks in range(2, 9):
+        for r in range(1, ranks):
+            at |= {units * r // ranks * 64 - 1, units * r // ranks * 64}
+    return sorted(j for j in at if 0 <= j < p)
+
+
+AXES = [(130, 64, 0), (130, 1000, 0), (48, 40000, 0), (40, 100000, 0), (16, 1 << 18, 0), (16, (1 << 20) + 72, 0), (40, 40000, 128), (40, 40000, 64), (40, 200000, 16384),
+        (2000, 4096, 64), (2000, 4096, 0)]
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("rows", [1, 7, 13, 20, 32, 33, 64, 100, 200])
+@pytest.mark.parametrize("q,p,group", AXES)
+def test_every_column_once(q, p, group, rows, bits):
+    """Differences of one everywhere and x of ones: p, to the last one, which the bias takes away."""
+    codes, scales, zeros = layer(q, p, bits, group, bits)
+    groups = 1 if zeros.dim() == 1 else zeros.shape[1]
+    zeros.clamp_(max=2.0 ** bits - 2.0)
+    z = zeros.view(q, groups)
+    codes = (z.repeat_interleave(group, 1)[:, :p] if groups > 1 else z.expand(q, p)).to(torch.uint8) + 1
+    w = qe.QuantizedWeights(codes, torch.ones_like(scales), zeros, bits, group_size=group)
+    bias = torch.full((q,), -float(p), device="cuda")
+    x = torch.ones(rows, p, dtype=(torch.bfloat16, torch.float16)[bits % 2], device="cuda")
+    assert (qe.qe_linear(w, x, bias=bias) == 0).all()
+    x[:, p // 3] = 2.0                                    # and one of them twice
+    assert (qe.qe_linear(w, x, bias=bias) == 1).all()
+    assert qe.qe_sync_status() == qe.QE_OK
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("rows", [1, 8, 32, 33, 64, 200])
+@pytest.mark.parametrize("q,p,group", AXES)
+def test_every_column_in_its_place(q, p, group, rows, bits):
+    """Rows of x with a single 1, at every border: the column itself comes out, s (c - z) rounded once."""
+    codes, scales, zeros = layer(q, p, bits, group, p + bits)
+    w, w64 = qe.QuantizedWeights(codes, scales, zeros, bits, group_size=group), weights64(codes, scales, zeros, group)
+    at = torch.tensor(borders(p), device="cuda")
+    dtype = (torch.bfloat16, torch.float16)[bits % 2]
+    for lo in range(0, len(at), rows):
+        cols = at[lo:lo + rows]
+        x = torch.zeros(rows, p, dtype=dtype, device="cuda")
+        x[torch.arange(len(cols), device="cuda"), cols] = 1.0
+        got = qe.qe_linear(w, x)
+        # the product of a scale and a whole number is rounded to binary32, then to the result's type
+        assert got[:len(cols)].equal(w64[:, cols].T.float().to(dtype)) and (got[len(cols):] == 0).all()
+    assert qe.qe_sync_status() == qe.QE_OK
