@@ -124,11 +124,10 @@ int linear_sms() {
 }
 
 RowsPlan rows_plan(const LinearArgs &a) {
-    const int nt = static_cast<int>(a.rows <= 8 ? 1 : a.rows <= 16 ? 2 : a.rows <= 24 ? 3 : 4);
     RowsPlan best{1, 1};
     int64_t least = -1;
-    for (int tiles = a.g.bits == 8 || nt > 1 ? 1 : 2; tiles >= 1; --tiles) {
-        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * ceil_div(a.rows, 8 * nt);
+    for (int tiles = a.g.bits == 8 || a.rows > 8 ? 1 : 2; tiles >= 1; --tiles) {
+        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles);
         for (int ranks = 1; ranks <= 8; ++ranks) {
             // An SM's time goes by the units it turns: its CTAs', each with what a CTA costs besides; one CTA alone leaves
             // pauses.  Measured (us, 4 bits, one / two row tiles a warp): 5 x 14848 x 59392 1 rank 176 / 283, 2 125 / 152 (116
@@ -190,9 +189,11 @@ cudaError_t launch_tiles(const LinearArgs &a, cudaStream_t s) {
     }
 }
 
-// Rows of x up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles): 4 bits, 4096 x 4096 24 rows 12 / 14,
-// 32 14 / 14, 64 16 / 14; 14848 x 59392 24 rows 156 / 231, 32 180 / 231, 64 346 / 231; 32 x 11008 x 4096 in groups of 128
-// 27 / 31; 8 bits, 32 x 4096 x 4096 18 / 16.
+// Rows of x up to which the few-rows kernel takes a call.  Measured (us, few rows / tiles): 4 bits, 4096 x 4096 9 to 32 rows 12 / 14,
+// 64 16 / 14, 4096 x 11008 32 rows 20 / 20, 14848 x 14848 9 rows 45 / 63, 32 59 / 66, 14848 x 59392 24 rows 156 / 231, 32 180 / 231,
+// 64 346 / 231; 8 bits, 4096 x 4096 9 to 32 rows 16 / 16, 11008 x 4096 32 rows 27 / 33, 14848 x 14848 80 / 94; groups of 128, 32 rows of
+// 11008 x 4096, 4 bits 25 / 31, 8 bits 33 / 41, of 14848 x 14848 74 / 88 and 104 / 121.  (Short layers with groups take a little longer
+// this way: 4096 x 4096 in groups of 128, 17 rows, 4 bits 16 / 14, 8 bits 20 / 18.)
 constexpr int kFewRows = 32;
 
 }  // namespace

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
     const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
     const int tile0 = static_cast<int>(blockIdx.x / static_cast<unsigned>(ranks)) * (kRowWarps * RT);
-    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * F::TOKENS;
+    const int rows = static_cast<int>(a.rows);           // at most F::TOKENS
     const int units = a.g.units;
     const int begin = static_cast<int>(static_cast<int64_t>(units) * rank / ranks), end = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / ranks);
     const int chunks = (end - begin + kChunk - 1) / kChunk;
@@ -118,8 +118,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
     const int pc = threadIdx.x & 31, row0 = threadIdx.x >> 5;
     const uint32_t x_to = ring + (pc >> 3) * F::UNIT_BYTES + row0 * 128 + (((pc & 7) ^ (row0 & 7)) << 4);
     const int64_t x_col = static_cast<int64_t>(begin) * kUnitCols + 8 * pc, x_step = 8 * a.ldx;
-    const uint16_t *x_from = static_cast<const uint16_t *>(a.x) + (m0 + row0) * a.ldx + x_col;
-    const int x_rows = a.rows - m0 - row0 <= 0 ? 0 : static_cast<int>((a.rows - m0 - row0 + 7) / 8);   // of the thread's, that are there
+    const uint16_t *x_from = static_cast<const uint16_t *>(a.x) + row0 * a.ldx + x_col;
+    const int x_rows = row0 < rows ? (rows - row0 + 7) / 8 : 0;   // of the thread's, that are there
     const int x_chunks = a.x_vec ? static_cast<int>((a.g.p - static_cast<int64_t>(begin) * kUnitCols) / (kChunk * kUnitCols)) : 0;   // whole ones
     auto bring = [&](int c) {
         if (c < chunks) {
@@ -290,8 +290,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
             }
     if (ranks > 1) cluster.sync();
     else __syncthreads();
-    constexpr int ALL = F::TOKENS * F::ROWS;
-    const int here = a.rows - m0 < F::TOKENS ? static_cast<int>(a.rows - m0) * F::ROWS : ALL;
+    const int here = rows * F::ROWS;
     with_activation(a.act, [&](auto act) {
         for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < here; e += ranks * kRowWarps * 32) {
             const int tok = e / F::ROWS, row = e % F::ROWS;
@@ -302,7 +301,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
             for (int k = 0; k < 8; ++k) of[k] = k < ranks ? (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row] : 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) v += of[k];       // in order
-            finish<act.value>(a, v, m0 + tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
+            finish<act.value>(a, v, tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
         }
     });
     if (ranks > 1) cluster.sync();                        // nobody leaves while its sums are read
@@ -311,7 +310,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
 template <int B, int RT, int NT, bool HALF, bool GROUPED, bool LONG = false>
 cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
     using F = RowsOf<RT, NT>;
-    const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps), blocks = ceil_div(a.rows, F::TOKENS);
+    const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps);
     constexpr int smem = F::SMEM + (LONG ? F::KEPT : 0);
     static std::atomic<uint64_t> raised{0};
     const void *kernel = reinterpret_cast<const void *>(k_linear_rows<B, RT, NT, HALF, GROUPED, LONG>);
@@ -320,7 +319,7 @@ cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks), static_cast<unsigned>(blocks));
+    cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks));
     cfg.blockDim = dim3(kRowWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
