@@ -124,10 +124,11 @@ int linear_sms() {
 }
 
 RowsPlan rows_plan(const LinearArgs &a) {
+    const int nt = static_cast<int>(a.rows <= 8 ? 1 : a.rows <= 16 ? 2 : a.rows <= 24 ? 3 : 4);
     RowsPlan best{1, 1};
     int64_t least = -1;
-    for (int tiles = a.g.bits == 8 || a.rows > 8 ? 1 : 2; tiles >= 1; --tiles) {
-        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles);
+    for (int tiles = a.g.bits == 8 || nt > 1 ? 1 : 2; tiles >= 1; --tiles) {
+        const int64_t groups = ceil_div(a.g.row_tiles, 8 * tiles) * ceil_div(a.rows, 8 * nt);
         for (int ranks = 1; ranks <= 8; ++ranks) {
             // An SM's time goes by the units it turns: its CTAs', each with what a CTA costs besides; one CTA alone leaves
             // pauses.  Measured (us, 4 bits, one / two row tiles a warp): 5 x 14848 x 59392 1 rank 176 / 283, 2 125 / 152 (116

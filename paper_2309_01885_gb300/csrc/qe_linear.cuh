@@ -309,7 +309,7 @@ TilesPlan tiles_plan(const LinearArgs &a);
 
 int linear_sms();                         // of the current device
 
-// up to 32 rows of x, and more: x's address and pitch are then multiples of 16 bytes
+// few rows of x (and, slowly, any number of them), and many: x's address and pitch are then multiples of 16 bytes
 cudaError_t launch_linear_rows_2(const LinearArgs &a, cudaStream_t s);
 cudaError_t launch_linear_rows_3(const LinearArgs &a, cudaStream_t s);
 cudaError_t launch_linear_rows_4(const LinearArgs &a, cudaStream_t s);

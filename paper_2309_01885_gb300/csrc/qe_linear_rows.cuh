@@ -7,12 +7,13 @@
 // with two or three instructions into 16-bit floats c - z (exact) and multiplies them with up
 // to 8 NT rows of x on m16n8k16, the outputs in the 16-high side.  Products are exact and sums
 // binary32; the scale comes in at the end, or at the end of every group.  Accumulators are emptied
-// every kSegmentUnits units: those of long groups into registers; with one grid a row, where a CTA has
-// more than twice as many units (LONG), into shared memory, a place of the thread's own for each.
-// (Where it has fewer too, the first size below took 100 us instead of 97.)  The eight warps of a CTA
-// share x, which passes through shared memory 256 columns at a time (swizzled by 16 bytes, read by
-// ldmatrix).  The CTAs of a cluster share a layer's columns out among them: their sums meet in
-// shared memory, in order, so that results do not depend on who is first.
+// every kSegmentUnits units (LONG): of groups that are longer into registers; with one grid a row, where
+// a CTA has more than twice as many units, into shared memory, a place of the thread's own for each.
+// (In one kernel for all calls it took 100 us instead of 97 for the first size below, and 319 instead
+// of 291 for it in groups of 128 at 8 bits.)  The eight warps of a CTA share x, which passes through
+// shared memory 256 columns at a time (swizzled by 16 bytes, read by ldmatrix).  The CTAs of a cluster
+// share a layer's columns out among them: their sums meet in shared memory, in order, so that results
+// do not depend on who is first.
 //
 // Measured (us, caches out of L2; of codes read): 5 x 14848 x 59392, 4 bits 98 (4.5 TB/s), 3 bits 101 (3.3 TB/s: a unit's turning is
 // the same work for fewer bytes); 1 x 4096 x 11008, 4 bits 16, 1 x 4096 x 4096, 3 bits 10 to 12 (the launch, a cluster's meeting
@@ -89,7 +90,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
     const int rank = static_cast<int>(cluster.block_rank()), ranks = static_cast<int>(cluster.num_blocks());
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
     const int tile0 = static_cast<int>(blockIdx.x / static_cast<unsigned>(ranks)) * (kRowWarps * RT);
-    const int rows = static_cast<int>(a.rows);           // at most F::TOKENS
+    // (of calls that are made, 0; without the grid's second axis the main loop is compiled to something up to 11% slower:
+    // 30 x 14848 x 14848, 4 bits, fp16 57 / 63 us)
+    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * F::TOKENS;
     const int units = a.g.units;
     const int begin = static_cast<int>(static_cast<int64_t>(units) * rank / ranks), end = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / ranks);
     const int chunks = (end - begin + kChunk - 1) / kChunk;
@@ -118,8 +121,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
     const int pc = threadIdx.x & 31, row0 = threadIdx.x >> 5;
     const uint32_t x_to = ring + (pc >> 3) * F::UNIT_BYTES + row0 * 128 + (((pc & 7) ^ (row0 & 7)) << 4);
     const int64_t x_col = static_cast<int64_t>(begin) * kUnitCols + 8 * pc, x_step = 8 * a.ldx;
-    const uint16_t *x_from = static_cast<const uint16_t *>(a.x) + row0 * a.ldx + x_col;
-    const int x_rows = row0 < rows ? (rows - row0 + 7) / 8 : 0;   // of the thread's, that are there
+    const uint16_t *x_from = static_cast<const uint16_t *>(a.x) + (m0 + row0) * a.ldx + x_col;
+    const int x_rows = a.rows - m0 - row0 <= 0 ? 0 : static_cast<int>((a.rows - m0 - row0 + 7) / 8);   // of the thread's, that are there
     const int x_chunks = a.x_vec ? static_cast<int>((a.g.p - static_cast<int64_t>(begin) * kUnitCols) / (kChunk * kUnitCols)) : 0;   // whole ones
     auto bring = [&](int c) {
         if (c < chunks) {
@@ -264,14 +267,17 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
 #pragma unroll
         for (int i = 0; i < RT; ++i) code[i] += kChunk * 128 * B;
     };
-    if constexpr (GROUPED || LONG) {
+    if constexpr (LONG) {
         for (int c = 0; c < chunks;) {
             for (const int stop = min(chunks, c + kSegmentChunks); c < stop; ++c) chunk(c);
-            if constexpr (LONG) keep(c <= kSegmentChunks);
-            else if (a.g.group_units > kSegmentUnits || c == chunks) fold();
+            if constexpr (GROUPED) fold();
+            else keep(c <= kSegmentChunks);
         }
     } else {
         for (int c = 0; c < chunks; ++c) chunk(c);
+        if constexpr (GROUPED) {
+            if (begin < end) fold();
+        }
     }
 
     // ---- the cluster's sums meet ----
@@ -284,13 +290,14 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float all = LONG ? kept[((i * NT + n) * 4 + e) * (kRowWarps * 32)] : sum[i][n][e];
+                const float all = LONG && !GROUPED ? kept[((i * NT + n) * 4 + e) * (kRowWarps * 32)] : sum[i][n][e];
                 const float v = GROUPED ? total[GROUPED ? i : 0][GROUPED ? n : 0][e] : begin < end ? all * scale[i][e >> 1] : 0.0f;
                 met[(8 * n + 2 * t + (e & 1)) * F::LD + kTileRows * (warp * RT + i) + r + 8 * (e >> 1)] = v;
             }
     if (ranks > 1) cluster.sync();
     else __syncthreads();
-    const int here = rows * F::ROWS;
+    constexpr int ALL = F::TOKENS * F::ROWS;
+    const int here = a.rows - m0 < F::TOKENS ? static_cast<int>(a.rows - m0) * F::ROWS : ALL;
     with_activation(a.act, [&](auto act) {
         for (int e = rank * (kRowWarps * 32) + threadIdx.x; e < here; e += ranks * kRowWarps * 32) {
             const int tok = e / F::ROWS, row = e % F::ROWS;
@@ -301,17 +308,17 @@ __global__ void __launch_bounds__(kRowWarps * 32, rows_ctas(NT)) k_linear_rows(c
             for (int k = 0; k < 8; ++k) of[k] = k < ranks ? (ranks > 1 ? cluster.map_shared_rank(met, k) : met)[tok * F::LD + row] : 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) v += of[k];       // in order
-            finish<act.value>(a, v, tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
+            finish<act.value>(a, v, m0 + tok, i, a.bias ? to_f32(a.bias, a.bias_dtype, i) : 0.0f);
         }
     });
     if (ranks > 1) cluster.sync();                        // nobody leaves while its sums are read
 }
 
-template <int B, int RT, int NT, bool HALF, bool GROUPED, bool LONG = false>
+template <int B, int RT, int NT, bool HALF, bool GROUPED, bool LONG>
 cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
     using F = RowsOf<RT, NT>;
-    const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps);
-    constexpr int smem = F::SMEM + (LONG ? F::KEPT : 0);
+    const int64_t groups = ceil_div(a.g.row_tiles, RT * kRowWarps), blocks = ceil_div(a.rows, F::TOKENS);
+    constexpr int smem = F::SMEM + (LONG && !GROUPED ? F::KEPT : 0);
     static std::atomic<uint64_t> raised{0};
     const void *kernel = reinterpret_cast<const void *>(k_linear_rows<B, RT, NT, HALF, GROUPED, LONG>);
     if (smem > 48 * 1024) {
@@ -319,7 +326,7 @@ cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks));
+    cfg.gridDim = dim3(static_cast<unsigned>(groups * ranks), static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(kRowWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -334,10 +341,14 @@ cudaError_t launch_rows_as(const LinearArgs &a, int ranks, cudaStream_t s) {
 
 template <int B, int RT, int NT>
 cudaError_t launch_rows_type(const LinearArgs &a, int ranks, cudaStream_t s) {
-    if (a.g.groups > 1) return a.half ? launch_rows_as<B, RT, NT, true, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, true>(a, ranks, s);
+    if (a.g.groups > 1) {
+        if (a.g.group_units > kSegmentUnits)
+            return a.half ? launch_rows_as<B, RT, NT, true, true, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, true, true>(a, ranks, s);
+        return a.half ? launch_rows_as<B, RT, NT, true, true, false>(a, ranks, s) : launch_rows_as<B, RT, NT, false, true, false>(a, ranks, s);
+    }
     if (ceil_div(a.g.units, ranks) > 2 * kSegmentUnits)
         return a.half ? launch_rows_as<B, RT, NT, true, false, true>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false, true>(a, ranks, s);
-    return a.half ? launch_rows_as<B, RT, NT, true, false>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false>(a, ranks, s);
+    return a.half ? launch_rows_as<B, RT, NT, true, false, false>(a, ranks, s) : launch_rows_as<B, RT, NT, false, false, false>(a, ranks, s);
 }
 
 template <int B, int RT>
