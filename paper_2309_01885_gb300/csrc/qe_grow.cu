@@ -12,7 +12,8 @@
 // started early and waits on the device.
 //
 // Bound by latency: a few kilobytes are read and written, through a chain of dependent
-// steps (read lengths, scan, look up, write).  64 sequences of a token each 8 us, 1500 of 100
+// steps (read lengths, scan, bisection over q_start: 6 reads for 64 sequences, 11 for 1500, read the
+// ring, write).  64 sequences of a token each 8 us, 1500 of 100
 // (150000 tokens) 14 us.
 #include "qe_cache.cuh"
 #include "qe_internal.h"

@@ -220,8 +220,9 @@ __device__ __forceinline__ float to_f32(const void *p, int dtype, int64_t i) {
     return __half2float(static_cast<const __half *>(p)[i]);
 }
 
-// Activations without branches, of the hardware's base-2 exponential: off by a few 2^-20 of the result at most, which 16 bits
-// do not show.  (With the library's erfc and quotients a tile's results took three times as long to leave as its products.)
+// Activations without branches, of __expf: by its stated bound off by (2 + 1.2 |a|) 2^-23 of the result for an exponent a, and the
+// exponent's own rounding adds |a| 2^-24: 2^-20 of the result near 0, 2^-18 at a = -25, 2^-16 at -88, where binary32's exponentials end
+// (a is y for SiLU, y^2 / 2 for GELU).  16 bits do not show it.  (With the library's erfc and quotients a tile's results took three times as long to leave as its products.)
 // 1 / (1 + exp(-y)); far below 0 the 1 no longer counts and exp(-y) would leave binary32's range.
 __device__ __forceinline__ float logistic(float y) { return y < -30.0f ? __expf(y) : __fdividef(1.0f, 1.0f + __expf(-y)); }
 

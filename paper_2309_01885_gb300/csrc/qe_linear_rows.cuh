@@ -15,9 +15,10 @@
 // share a layer's columns out among them: their sums meet in shared memory, in order, so that results
 // do not depend on who is first.
 //
-// Measured (us, caches out of L2; of codes read): 5 x 14848 x 59392, 4 bits 98 (4.5 TB/s), 3 bits 101 (3.3 TB/s: a unit's turning is
-// the same work for fewer bytes); 1 x 4096 x 11008, 4 bits 16, 1 x 4096 x 4096, 3 bits 10 to 12 (the launch, a cluster's meeting
-// and the first loads' way take most of it); 24 x 11008 x 4096, 4 bits in groups of 128 20.
+// Measured (us, caches out of L2; of codes read): 5 x 14848 x 59392, fp16, 4 bits 94 (4.7 TB/s), 3 bits 98 (3.4 TB/s: a unit's turning
+// is the same work for fewer bytes; the integer pipe is busy 66% of the time, issue slots 58%), 8 bits 162 (5.4 TB/s), bf16 104, 104
+// and 229 (five instructions for two 8-bit codes); 1 x 4096 x 11008, 4 bits 14, 1 x 4096 x 4096, 3 bits 10 to 13 (the launch, a cluster's
+// meeting and the first loads' way take most of it); 24 x 11008 x 4096, 4 bits in groups of 128 19 to 22.
 #pragma once
 
 #include <cooperative_groups.h>

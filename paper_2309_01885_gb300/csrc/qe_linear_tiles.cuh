@@ -20,9 +20,10 @@
 // Where there are few tiles the CTAs of a cluster share a tile's columns; their sums meet in
 // shared memory in order.
 //
-// Measured (us; of the products' 2 rows q p): 4095 x 4096 x 11008, 4 bits 209 to 215 (1.7 to 1.8 PFLOP/s), with bias, GELU and
-// residual 255, 8 bits 332, grids for groups of 256, 128 and 64 columns 322, 385 and 743 (every group's sums are folded in
-// registers); 4095 x 14848 x 4096 309, 2048 x 4096 x 4096 59, 64 x 4096 x 4096 14.  Turned codes through shared memory, the
+// Measured (us; of the products' 2 rows q p): 4095 x 4096 x 11008, 4 bits 209 to 215 (1.7 to 1.8 PFLOP/s), with GELU 229, a residual
+// 225, both 238, 8 bits 301 (five instructions turn two codes for bf16, and tiles have 224 rows), grids for groups of 256, 128 and 64
+// columns 299, 336 and 610 (every group's sums pass from tensor memory through registers, 16 columns a wait); 4095 x 14848 x 4096
+// 311, 2048 x 4096 x 4096 59, in groups of 128 86, 64 x 4096 x 4096 14.  Turned codes through shared memory, the
 // products' other form, were slower: both operands and the codes pass through it then.
 #pragma once
 

@@ -11,7 +11,7 @@
 // neighbouring channels (16 bytes of a 16-bit type) of a head in 8, 16 or 32 lanes, or four of either half where halves face each
 // other; the mean meets in shuffles.  Two heads of a token go together (in 16 bits), binary32 arithmetic is on pairs, a block's
 // tokens have their sines and cosines worked out once, for all heads.  Measured (us, TB/s read and written): 16384 tokens of 64
-// heads of 128, bf16 107 (5.0), neighbouring pairs 113 (4.8); 8192 of 64, binary32 88 (6.1); 8192 of 240 heads of 64, fp16 94 (5.3);
+// heads of 128, bf16 105 (5.1), neighbouring pairs 107 (5.0); 8192 of 64, binary32 88 (6.1); 8192 of 240 heads of 64, fp16 90 (5.6);
 // 8192 of 40 heads of 128 of which 36 channels turn 59 (2.8).  A head at a time and addresses by products: 122, 143, 86, 107, 107;
 // blocks of 1, 2, 4, 8 and 16 tokens 137, 122, 113, 107, 107 (the first).
 #include <cuda_fp16.h>
